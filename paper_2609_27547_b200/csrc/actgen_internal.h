@@ -24,6 +24,7 @@ struct EnvMeta {
     const float *noise;  // device: the environment's [H][A] state on entry
     float *out;          // device: where its [H][A] result goes
     const void *hid;   // hidden-state prefixes: device [P][d_ctx] as given by the caller (kv then points into the projected planes)
+    float *weight;     // 8-bit prefixes: where the attention weights of its tokens are added up, or NULL
 };
 
 // Opaque storage of a CUtensorMap (the driver's 128-byte TMA descriptor).

@@ -1,0 +1,209 @@
+// The weight each prefix token got (include/ebrl_prefix8.h): w[t] = sum over heads and query rows of exp(scale q k_t - lse).
+//
+// Bound: HBM -- the key codes are read once, a token's weight is written once.  A second pass over the keys is half of the
+// attention's own traffic; gathering the weights inside attention would need either the scores of all heads in memory
+// (16 rows x 4 B per token and head against 128 B of codes) or atomics across heads, whose order changes the last bits.
+//
+// A CTA owns 128 x TW tokens of one environment and walks every (key/value head, row tile): its eight warps are HW
+// parallel heads x TW token groups (HW = 8 with eight heads or more).  A warp keeps its head's queries in registers for
+// four tiles -- the query rows then cost a quarter of the keys' L2 traffic at 16 rows -- and the weights of its 128 tokens
+// in 16 registers per lane over all of its heads.  Only at the end are they summed over the lanes of a quad and, in
+// warp order, over the parallel heads: a fixed order, no atomics.  The key tiles of a warp's heads are one stream through a
+// ring of cp.async slots, so the ring stays full across heads.
+#include "prefix8_tile.cuh"
+
+namespace ebrl {
+namespace p8 {
+
+template <int HD, int NT, bool F32> struct WeighCfg {
+    static constexpr int TILE = BLOCK * HD, RING = HD == 32 ? 8192 : 12288, SLOTS = RING / TILE;
+    static constexpr int CTAS = (NT == 4 || F32) ? 1 : 2;
+    static constexpr int SMEM = 8 * RING;
+};
+
+template <int HD, int NT, bool F32>
+__global__ void __launch_bounds__(256, WeighCfg<HD, NT, F32>::CTAS)
+weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs ev, int hw_log2, int n_chunk)
+{
+    using C = WeighCfg<HD, NT, F32>;
+    constexpr int KS = HD / 16;
+    extern __shared__ __align__(128) char smem[];
+    __shared__ float red[8][128];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    const uint32_t ring_u = ptx::smem_u32(smem + (size_t)warp * C::RING);
+    const int G = a.r.G, R = a.r.H * G, RT = (R + NT * 8 - 1) / (NT * 8), kvh = a.r.rec.kvh, units = kvh * RT;
+    const int HW = 1 << hw_log2, TW = 8 >> hw_log2, hw = warp & (HW - 1), tw = warp >> hw_log2;
+    const int n_envs = a.r.meta ? a.r.n_envs : ev.n;
+    const long long items = (long long)n_envs * n_chunk;
+    uint32_t koff[2];
+    KeyWords<HD>::offsets(koff, g, t);
+    pdl_launch_dependents();
+    pdl_wait();
+
+    for (long long item = blockIdx.x; item < items; item += gridDim.x) {
+        const int env = (int)(item / n_chunk), chunk = (int)(item - (long long)env * n_chunk);
+        const char *rec;
+        float *wp;
+        int len;
+        if (a.r.meta) { rec = (const char *)a.r.meta[env].kv; len = a.r.meta[env].P; wp = a.r.meta[env].weight; }
+        else {
+            rec = a.r.pool + (size_t)ev.slot[env] * a.r.rec.bytes;
+            len = ev.len[env];
+            wp = a.weight + (size_t)ev.slot[env] * a.stride;
+        }
+        const int c0 = chunk * TW * 128;                     // first token of the CTA
+        if (c0 >= len || !wp) continue;                      // (the same for the whole CTA)
+        const int b0 = c0 + tw * 128;                        // ... and of the warp
+        const int live = b0 >= len ? 0 : min(4, (len - b0 + BLOCK - 1) / BLOCK);
+        const int mine = hw < units ? (units - hw + HW - 1) >> hw_log2 : 0;   // this warp's (head, row tile) units: hw, hw + HW, ...
+        const int loads = mine * live;
+        // load j of the warp's stream: tile j % live of its unit j / live
+        int iu = hw, it = 0;
+        auto issue = [&](int j, int slot) {
+            if (j < loads) {
+                const char *src = rec + a.r.rec.head(a.r.layer, 0, iu / RT) + (size_t)(b0 + it * BLOCK) * HD;
+                request_tile<HD>(ring_u + (uint32_t)(slot * C::TILE), src, min(BLOCK, len - b0 - it * BLOCK), lane);
+                if (++it == live) { it = 0; iu += HW; }
+            }
+            cp_commit();
+        };
+#pragma unroll
+        for (int j = 0; j < C::SLOTS - 1; ++j) issue(j, j);
+
+        uint32_t seen = 0;   // lane l: visible tokens of tile l
+        if (lane < live) {
+            seen = reinterpret_cast<const uint32_t *>(rec + a.r.rec.mask)[b0 / BLOCK + lane];
+            const int v = len - b0 - lane * BLOCK;
+            if (v < BLOCK) seen &= (1u << v) - 1u;
+        }
+        float acc[4][2][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) acc[i][h][0] = acc[i][h][1] = 0.f;
+
+        int slot = 0, j = 0;
+        for (int u = 0; u < mine; ++u) {
+            if (live == 0) break;
+            const int unit = hw + u * HW, kh = unit / RT, rt = unit - kh * RT;
+            uint32_t qh[NT][KS][2], ql[F32 ? NT : 1][KS][2];
+            float fr[NT][2], ls[NT][2];
+            const float ks_l = lane < live ? read_scale(reinterpret_cast<const float *>(rec + a.r.rec.head_scales(a.r.layer, 0, kh))[b0 / BLOCK + lane]) : 0.f;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                const int r = rt * NT * 8 + nt * 8 + g, tok = r / G, head = kh * G + r - tok * G;
+                const size_t off = (size_t)env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)head * HD;
+                const void *p = F32 ? (const void *)((const float *)a.r.q + off) : (const void *)((const __nv_bfloat16 *)a.r.q + off);
+                const float f = load_q<HD, F32>(p, r < R, t, qh[nt], ql[F32 ? nt : 0]) * (a.r.scale * LOG2E);
+                // rows that saw nothing (lse = -inf) and rows past the last one add 2^-inf
+                float l = r < R ? a.lse[(size_t)env * a.l_env + (size_t)tok * a.l_tok + (size_t)head * a.l_head] : -INFINITY;
+                l = l == -INFINITY ? INFINITY : l * LOG2E;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    fr[nt][c] = __shfl_sync(FULL, f, 8 * t + 4 * c);
+                    ls[nt][c] = __shfl_sync(FULL, l, 8 * t + 4 * c);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (i < live) {
+                    const float ks = __shfl_sync(FULL, ks_l, i);
+                    cp_wait<C::SLOTS - 2>();
+                    __syncwarp();
+                    issue(j + C::SLOTS - 1, slot == 0 ? C::SLOTS - 1 : slot - 1);
+                    const uint32_t at = ring_u + (uint32_t)(slot * C::TILE);
+                    slot = slot + 1 == C::SLOTS ? 0 : slot + 1;
+                    ++j;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        KeyWords<HD> kw;
+                        kw.load(at, koff, h);
+                        float s[NT][4];
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) s[nt][c] = 0.f;
+#pragma unroll
+                        for (int st = 0; st < KS; ++st) {
+                            uint32_t f[4];
+                            key_operand(st, kw.a[st], kw.b[st], f);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma(s[nt], f[0], f[1], f[2], f[3], qh[nt][st][0], qh[nt][st][1]);
+                                if constexpr (F32) mma(s[nt], f[0], f[1], f[2], f[3], ql[nt][st][0], ql[nt][st][1]);
+                            }
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            acc[i][h][0] += ex2(fmaf(s[nt][0], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[nt][1], ks * fr[nt][1], -ls[nt][1]));
+                            acc[i][h][1] += ex2(fmaf(s[nt][2], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[nt][3], ks * fr[nt][1], -ls[nt][1]));
+                        }
+                    }
+                }
+            }
+        }
+        cp_wait<0>();
+        // over the quad's row pairs, then over the parallel heads
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float v = acc[i][h][c];
+                    v += __shfl_xor_sync(FULL, v, 1);
+                    v += __shfl_xor_sync(FULL, v, 2);
+                    const uint32_t m = __shfl_sync(FULL, seen, i);
+                    const int tok = 16 * h + 8 * c + g;
+                    if (t == 0) red[warp][i * 32 + tok] = (m >> tok) & 1 ? v : 0.f;
+                }
+        __syncthreads();
+        for (int k = threadIdx.x; k < TW * 128; k += 256) {
+            const int tok = c0 + k, first = (k >> 7) << hw_log2;
+            if (tok < len) {
+                float v = 0.f;
+                for (int h = 0; h < HW; ++h) v += red[first + h][k & 127];
+                wp[tok] = a.accumulate ? wp[tok] + v : v;
+            }
+        }
+        __syncthreads();   // red and the rings are free
+    }
+}
+
+namespace {
+
+template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Envs &e, int max_len, int grid, cudaStream_t st)
+{
+    using C = WeighCfg<HD, NT, F32>;
+    static bool set[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!set[dev]) {
+        cudaError_t err = cudaFuncSetAttribute(weigh_kernel<HD, NT, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (err != cudaSuccess) return err;
+        set[dev] = true;
+    }
+    const int units = a.r.rec.kvh * ((a.r.H * a.r.G + NT * 8 - 1) / (NT * 8));
+    const int hw = units >= 8 ? 3 : (units >= 4 ? 2 : (units >= 2 ? 1 : 0));
+    const int n_chunk = (max_len + (128 << (3 - hw)) - 1) / (128 << (3 - hw));
+    const long long items = (long long)(a.r.meta ? a.r.n_envs : e.n) * n_chunk, cap = grid ? grid : 1 << 20;
+    if (items == 0) return cudaSuccess;
+    return launch_kernel(weigh_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), 256, (size_t)C::SMEM, st, 1, a, e, hw, n_chunk);
+}
+
+template <int HD> cudaError_t pick(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st)
+{
+    const int nt = row_tile(a.r.H * a.r.G) / 8;
+    if (f32) return nt == 1 ? go<HD, 1, true>(a, e, max_len, grid, st) : (nt == 2 ? go<HD, 2, true>(a, e, max_len, grid, st) : go<HD, 4, true>(a, e, max_len, grid, st));
+    return nt == 1 ? go<HD, 1, false>(a, e, max_len, grid, st) : (nt == 2 ? go<HD, 2, false>(a, e, max_len, grid, st) : go<HD, 4, false>(a, e, max_len, grid, st));
+}
+
+}  // namespace
+
+cudaError_t launch_weigh(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st)
+{
+    return a.r.rec.hd == 128 ? pick<128>(a, e, f32, max_len, grid, st) : (a.r.rec.hd == 64 ? pick<64>(a, e, f32, max_len, grid, st) : pick<32>(a, e, f32, max_len, grid, st));
+}
+
+}  // namespace p8
+}  // namespace ebrl
