@@ -141,8 +141,8 @@ int longest(const int32_t *len, int n)
 }
 
 // How prefixes are cut: tokens per piece and pieces of the longest prefix.  Left to itself, a call is cut only when its
-// (environment, head, row tile) items are at most half of the teams that the SMs hold, into as many pieces as there
-// are teams for (never more: a second wave would double the time) and not below 256 tokens.
+// (environment, head, row tile) items are at most half of the warps that the SMs hold, into as many pieces as there
+// are warps for (never more: a second wave would double the time) and not below 256 tokens.
 // Measured on two 65 k-token prefixes with 4 heads: whole 2.4 ms, pieces of 2048 36 us, this rule (896) 29 us.
 void cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int heads, int asked, int sms, bool f32, int *split, int *n_split)
 {
@@ -158,9 +158,9 @@ void cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int h
     for (int i = 0; i < n; ++i) items += len[i] > 0;
     const int rows = H * (heads / l.n_kv_heads), tile = row_tile(rows);
     items *= (long long)l.n_kv_heads * ((rows + tile - 1) / tile);
-    const long long teams = (long long)sms * attend_teams(l.head_dim, rows, f32);
-    if (items == 0 || items * 2 > teams) return;
-    const long long parts = teams / items;
+    const long long warps = (long long)sms * attend_warps(rows, f32);
+    if (items == 0 || items * 2 > warps) return;
+    const long long parts = warps / items;
     const long long piece = std::max(256LL, ((most + parts - 1) / parts + 127) / 128 * 128);
     if (piece >= most) return;
     *split = (int)piece;
@@ -299,7 +299,7 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
                 a.part_o = (float *)workspace + at * layout->head_dim;
                 a.part_ml = (float *)workspace + pr * layout->head_dim + at * 2;
             }
-            if ((st = launched(launch_attend(a, e, f32, longest(e.len, e.n), sm_quota, (cudaStream_t)stream))) != EBRL_OK) return st;
+            if ((st = launched(launch_attend(a, e, f32, sm_quota, (cudaStream_t)stream))) != EBRL_OK) return st;
             if (n_split > 1 && (st = launched(launch_attend_join(a, e, f32, sm_quota, sms, (cudaStream_t)stream))) != EBRL_OK) return st;
         }
         return EBRL_OK;

@@ -5,16 +5,13 @@
 // no more:
 //     S^T [tokens x rows] = K [tokens x hd] Q^T          A = keys,     B = queries
 //     O^T [hd x rows]     = V^T [hd x tokens] P^T        A = values^T, B = weights
-// Every e4m3 value is an f16 value (3 mantissa bits, exponents -9 .. 8), so codes are widened exactly, straight from the words a
-// lane reads from shared memory, in two ways that run side by side:
-//   widen   the conversion instruction, one pair each; it runs on the quarter-rate unit at 8 pairs a clock and SM (measured: with it
-//           alone that unit is 82 % busy and the stream stops at half of the copy bandwidth, which needs 11.5 pairs)
-//   spread  integer instructions: sign and magnitude put at their places in the f16 give the value times 2^-8 (subnormals
-//           included), 3 to 4 instructions a pair on the full-rate units
-// A quarter of the pairs take the first way.  The 2^8 between them is taken up by the queries' and the output's factors.  The order of the contracted index is free as long
-// as both operands agree: lane (g = lane / 4, t = lane % 4) takes the HD / 4 consecutive columns t * HD / 4 .. of tokens g
-// and g + 8 as its key operand (so its queries are HD / 4 consecutive elements, too), and the HD / 8 consecutive columns
-// g * HD / 8 .. of tokens 2t, 2t + 1, 2t + 8, 2t + 9 as its value operand (so its outputs are consecutive).
+// Every e4m3 value is an f16 value (3 mantissa bits, exponents -9 .. 8): codes are widened exactly, two per instruction, straight
+// from the words a lane reads from shared memory (the conversion runs at 63 pairs a clock and SM, the product at 957 MAC;
+// mma.sync on e4m3 operands is no way around it: it is that same conversion and product inside, 2.5 times the instructions).
+// The order of the contracted index is free as long as both operands agree: lane (g = lane / 4, t = lane % 4) takes the
+// HD / 4 consecutive columns t * HD / 4 .. of tokens g and g + 8 as its key operand (so its queries are HD / 4 consecutive
+// elements, too), and the HD / 8 consecutive columns g * HD / 8 .. of tokens 2t, 2t + 1, 2t + 8, 2t + 9 as its value
+// operand (so its outputs are consecutive).
 #pragma once
 #include "prefix8_internal.h"
 #include "ptx_helpers.cuh"
@@ -34,13 +31,6 @@ __device__ __forceinline__ uint32_t widen(uint32_t two)   // the e4m3 pair in th
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
     return r;
 }
-// Bytes 0 and 2 (even) or 1 and 3 (odd) of four codes as f16x2, times 2^-8: exponent and mantissa of e4m3 are the low seven bits,
-// those of f16 bits 13 .. 7 once the exponent's top bit is 0, and the biases differ by 8.
-__device__ __forceinline__ uint32_t spread_even(uint32_t w) { return ((w << 7) & 0x3f803f80u) | ((w << 8) & 0x80008000u); }
-__device__ __forceinline__ uint32_t spread_odd(uint32_t w) { return ((w >> 1) & 0x3f803f80u) | (w & 0x80008000u); }
-// Which steps of the contraction over head_dim (keys) and which 16-column tiles of the output (values) take the conversion unit.
-__host__ __device__ constexpr bool by_unit(int i) { return (i & 3) == 3; }
-
 __device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
 {
     uint32_t r;
@@ -80,6 +70,14 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void *src, uint32_t nby
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(nbytes) : "memory");
 }
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void *src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -94,6 +92,14 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
     uint2 v;
     asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(a));
     return v;
+}
+__device__ __forceinline__ void sts128(uint32_t a, uint32_t x, uint32_t y, uint32_t z, uint32_t w)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+__device__ __forceinline__ void sts64(uint32_t a, uint32_t x, uint32_t y)
+{
+    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(a), "r"(x), "r"(y) : "memory");
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t a)
 {
@@ -120,20 +126,30 @@ template <int HD> __device__ __forceinline__ uint32_t tile_addr(int tok, int off
 template <int HD> __device__ __forceinline__ void request_tile(uint32_t dst, const char *src, int valid, int lane)
 {
     constexpr int N = 2 * HD / 32;                 // 16-byte pieces per lane
-    const int bytes = valid * HD;
+    if (valid >= BLOCK) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int lin = (i * 32 + lane) * 16;
-        const uint32_t at = dst + tile_addr<HD>(lin / HD, lin % HD);
-        cp16(at, lin < bytes ? src + lin : src, lin < bytes ? 16u : 0u);
+        for (int i = 0; i < N; ++i) {
+            const int lin = (i * 32 + lane) * 16;
+            cp16(dst + tile_addr<HD>(lin / HD, lin % HD), src + lin);
+        }
+    } else {
+        const int bytes = valid * HD;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int lin = (i * 32 + lane) * 16;
+            cp16(dst + tile_addr<HD>(lin / HD, lin % HD), lin < bytes ? src + lin : src, lin < bytes ? 16u : 0u);
+        }
     }
 }
 
-// One lane's share of the queries of a row tile as B operands: row g of each column tile, columns t * HD / 4 .., scaled by a
-// power of two so that the row's largest element lies in [2^6, 2^7) where keys are widened by the conversion unit and in [2^14, 2^15)
-// where they come 2^8 smaller.  bf16 queries then are f16 values exactly unless they are 2^20 smaller than the row's largest
-// (then 2^-31 of it is lost); fp32 queries are split into two f16 terms (22 bits).  Returns the factor that undoes it.
-template <int HD, bool F32> __device__ __forceinline__ float load_q(const void *q, bool there, int t, uint32_t (*hi)[2], uint32_t (*lo)[2])
+// One lane's share of a column tile of queries as B operands: row g, columns t * HD / 4 .., scaled by a power of two so that the
+// row's largest element lies in [2^14, 2^15).  bf16 queries then are f16 values exactly unless they are 2^28 smaller than the row's
+// largest (then 2^-40 of that is lost); fp32 queries are split into two f16 terms (22 bits).
+// q[s]: the operands of step s (16 columns): {b0, b1 of the first term, of the second}.
+// `negate` puts the sign of the softmax scale into the queries, so that what scores are multiplied by is never negative.
+// Returns the factor that undoes the scaling.
+template <bool F32> constexpr int QW = F32 ? 4 : 2;   // words per step
+template <int HD, bool F32> __device__ __forceinline__ float load_q(const void *q, bool there, bool negate, int t, uint32_t (*out)[QW<F32>])
 {
     constexpr int N = HD / 4;
     float x[N];
@@ -168,26 +184,19 @@ template <int HD, bool F32> __device__ __forceinline__ float load_q(const void *
     m = fmaxf(m, __shfl_xor_sync(FULL, m, 1));
     m = fmaxf(m, __shfl_xor_sync(FULL, m, 2));
     const int e = (int)(__float_as_uint(m) >> 23);            // biased exponent of the largest
-    const int up = (m == 0.f || e == 255) ? 0 : min(6 + 127 - e, 119);
+    const int up = (m == 0.f || e == 255) ? 0 : min(14 + 127 - e, 127);
     const float mul = __uint_as_float((uint32_t)(up + 127) << 23);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] *= negate ? -mul : mul;
 #pragma unroll
     for (int s = 0; s < HD / 16; ++s)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            // the two columns that share a register of the keys: neighbours, or (spread) every other one
-            const float k = by_unit(s) ? mul : mul * 256.f;
-            const float a = x[4 * s + (by_unit(s) ? 2 * j : j)] * k, b = x[4 * s + (by_unit(s) ? 2 * j + 1 : j + 2)] * k;
-            hi[s][j] = pack_f16(a, b);
-            if constexpr (F32) lo[s][j] = pack_rest(a, b, hi[s][j]);
+            const float a = x[4 * s + 2 * j], b = x[4 * s + 2 * j + 1];
+            out[s][j] = pack_f16(a, b);
+            if constexpr (F32) out[s][2 + j] = pack_rest(a, b, out[s][j]);
         }
     return 1.f / mul;   // a power of two: exact
-}
-
-// A pair of keys' words -> the A operand of one step.
-__device__ __forceinline__ void key_operand(int step, uint32_t a, uint32_t b, uint32_t *f)
-{
-    if (by_unit(step)) { f[0] = widen(a); f[1] = widen(b); f[2] = widen(a >> 16); f[3] = widen(b >> 16); }
-    else { f[0] = spread_even(a); f[1] = spread_even(b); f[2] = spread_odd(a); f[3] = spread_odd(b); }
 }
 
 // One lane's words of the keys g and g + 8 of a 16-token half tile; kaddr = the tile's slot + tile_addr(g, t * HD / 4).
@@ -219,6 +228,26 @@ template <int HD> struct KeyWords {
         off[1] = HD == 128 ? tile_addr<HD>(g, t * (HD / 4) + 16) : 0u;
     }
 };
+
+// Raw scores of 16 tokens and NT column tiles: s = keys x queries.  q(step, nt, w) hands out the queries' operands.
+template <int HD, int NT, bool F32, typename Q> __device__ __forceinline__ void score(float (*s)[4], const KeyWords<HD> &k, Q &&q)
+{
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) s[nt][c] = 0.f;
+#pragma unroll
+    for (int st = 0; st < HD / 16; ++st) {
+        const uint32_t a0 = widen(k.a[st]), a1 = widen(k.b[st]), a2 = widen(k.a[st] >> 16), a3 = widen(k.b[st] >> 16);
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            uint32_t w[QW<F32>];
+            q(st, nt, w);
+            if constexpr (F32) mma(s[nt], a0, a1, a2, a3, w[2], w[3]);
+            mma(s[nt], a0, a1, a2, a3, w[0], w[1]);
+        }
+    }
+}
 
 }  // namespace p8
 }  // namespace ebrl

@@ -26,7 +26,6 @@ __global__ void __launch_bounds__(256, WeighCfg<HD, NT, F32>::CTAS)
 weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs ev, int hw_log2, int n_chunk)
 {
     using C = WeighCfg<HD, NT, F32>;
-    constexpr int KS = HD / 16;
     extern __shared__ __align__(128) char smem[];
     __shared__ float red[8][128];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -86,7 +85,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
         for (int u = 0; u < mine; ++u) {
             if (live == 0) break;
             const int unit = hw + u * HW, kh = unit / RT, rt = unit - kh * RT;
-            uint32_t qh[NT][KS][2], ql[F32 ? NT : 1][KS][2];
+            uint32_t q[NT][HD / 16][QW<F32>];
             float fr[NT][2], ls[NT][2];
             const float ks_l = lane < live ? read_scale(reinterpret_cast<const float *>(rec + a.r.rec.head_scales(a.r.layer, 0, kh))[b0 / BLOCK + lane]) : 0.f;
 #pragma unroll
@@ -94,7 +93,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                 const int r = rt * NT * 8 + nt * 8 + g, tok = r / G, head = kh * G + r - tok * G;
                 const size_t off = (size_t)env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)head * HD;
                 const void *p = F32 ? (const void *)((const float *)a.r.q + off) : (const void *)((const __nv_bfloat16 *)a.r.q + off);
-                const float f = load_q<HD, F32>(p, r < R, t, qh[nt], ql[F32 ? nt : 0]) * (a.r.scale * LOG2E);
+                const float f = load_q<HD, F32>(p, r < R, a.r.scale < 0.f, t, q[nt]) * (fabsf(a.r.scale) * LOG2E);
                 // rows that saw nothing (lse = -inf) and rows past the last one add 2^-inf
                 float l = r < R ? a.lse[(size_t)env * a.l_env + (size_t)tok * a.l_tok + (size_t)head * a.l_head] : -INFINITY;
                 l = l == -INFINITY ? INFINITY : l * LOG2E;
@@ -119,20 +118,10 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                         KeyWords<HD> kw;
                         kw.load(at, koff, h);
                         float s[NT][4];
+                        score<HD, NT, F32>(s, kw, [&](int st, int nt, uint32_t *w) {
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) s[nt][c] = 0.f;
-#pragma unroll
-                        for (int st = 0; st < KS; ++st) {
-                            uint32_t f[4];
-                            key_operand(st, kw.a[st], kw.b[st], f);
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                mma(s[nt], f[0], f[1], f[2], f[3], qh[nt][st][0], qh[nt][st][1]);
-                                if constexpr (F32) mma(s[nt], f[0], f[1], f[2], f[3], ql[nt][st][0], ql[nt][st][1]);
-                            }
-                        }
+                            for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
+                        });
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             acc[i][h][0] += ex2(fmaf(s[nt][0], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[nt][1], ks * fr[nt][1], -ls[nt][1]));
