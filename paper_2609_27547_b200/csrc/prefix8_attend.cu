@@ -4,7 +4,7 @@
 // what counts is that bytes are always in flight and that a code costs few instructions.
 //
 //   Item = (environment, piece of its prefix, key/value head, row tile), worked on by ONE WARP: its own running softmax, its
-//   own ring of tile slots (keys and values alternate) filled by cp.async, no barrier, no partial results to join unless a prefix is
+//   own ring of stages (a key and a value tile each) filled by cp.async, no barrier, no partial results to join unless a prefix is
 //   cut.  A record's head is contiguous, so a tile is one straight 4 KB run at head_dim 128.
 //   SMs hold 16 warps at 8 rows, 12 at 16, 8 at 32 (what registers allow); 130 - 190 KB of tiles are in flight per SM, three
 //   times what HBM latency asks for.  With all SMs to itself the launch is one CTA per item, which lets the hardware even out
@@ -12,10 +12,15 @@
 //   (Four warps per item, joined in shared memory, were 1.6 times slower on 512 x 768 tokens x 16 heads: an item was
 //   over before its set-up and join were paid for.)
 //
+//   With the cache in L2 (arithmetic alone) 512 x 768 tokens x 16 heads of 128 take 143 us at 8 rows, 240 at 16, 460 at 32; from
+//   HBM 241 us (6.7 TB/s of codes), 296 (5.4) and 492.  Half of the cycles of the 16-row kernel are dependent-instruction waits
+//   at two warps per scheduler; removing any one kind of work (products, exponentials, conversions, transposes) saves 1 - 5 %.
+//
 //   Running maximum, lazily: a row's reference is raised only when a score exceeds it by 2^14 / 2^6; until then the weights
 //   2^(s - ref) stay below 2^14, which f16 holds with the same 11 bits.  The common tile needs one vote and no
 //   shuffles.  Weights aim at 2^6 rather than 1, so that those 2^-20 of the largest are still normal f16 numbers.
-//   A block's value scale is applied in fp32 to the block's own product (tmp), not to the weights: any finite scales work.
+//   Value scales are never put into the weights: outputs change their unit where neighbouring blocks' scales differ (exact for
+//   powers of two), and where they differ by more than 2^20 the block's product is scaled by itself.  Any finite scales work.
 //
 //   bf16 queries are exact (prefix8_tile.cuh), weights are rounded to f16: 11 bits, an eighth of the output's own rounding.  fp32 queries: queries and weights in two f16 terms each (22 bits).  Sums are fp32.
 #include "prefix8_tile.cuh"
@@ -27,15 +32,17 @@ namespace ebrl {
 namespace p8 {
 
 template <int HD, int NT, bool F32> struct AttendCfg {
-    static constexpr int WARPS = HD == 128 ? (NT == 1 ? 12 : (F32 && NT == 4 ? 7 : 8)) : (NT == 1 ? (F32 ? 12 : 16) : (NT == 2 ? (F32 ? 8 : 10) : (F32 ? 7 : 8)));    // per SM
+    // per SM: as many as their registers allow (168 a thread at 12, 255 at 8)
+    static constexpr int WARPS = NT == 4 ? (F32 && HD == 128 ? 6 : 8) : (NT == 2 ? (HD == 128 || F32 ? 8 : 12) : (HD == 128 || F32 ? 12 : 16));
     static constexpr int TILE = BLOCK * HD;
     // queries in shared memory where registers hold the outputs of 32 rows, or of 16 beside two f16 terms: per warp
-    static constexpr bool QS = NT == 4 || (F32 && NT == 2);
+    static constexpr bool QS = NT == 4 || (NT == 2 && F32);
     static constexpr int QBYTES = QS ? HD / 16 * NT * 32 * 4 * QW<F32> : 0;
-    static constexpr int ROOM = (224 * 1024 / WARPS - QBYTES - 128) / TILE;
-    static constexpr int SLOTS = ROOM < 8 ? ROOM : 8;                 // 3 .. 8 tiles per warp
-    static constexpr int WARP_BYTES = SLOTS * TILE + QBYTES + 128;    // ring, queries, and per slot the tile's scale and mask
-    static_assert(SLOTS >= 3, "ring");
+    static constexpr int ROOM = (224 * 1024 / WARPS - QBYTES) / (2 * TILE);
+    static constexpr int STAGES = ROOM < 4 ? ROOM : 4;                // 2 .. 4 pairs of a key and a value tile per warp
+    static constexpr int WARP_BYTES = STAGES * 2 * TILE + QBYTES;     // ring, queries
+    static constexpr int PSTRIDE = HD + 4;                            // floats per staged output row
+    static_assert(STAGES >= 2 && 8 * PSTRIDE * 4 <= STAGES * 2 * TILE, "ring");
 };
 
 template <int HD, int NT, bool F32>
@@ -48,14 +55,13 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const uint32_t ring_u = ptx::smem_u32(smem + (size_t)warp * C::WARP_BYTES);
-    const uint32_t q_u = ring_u + C::SLOTS * C::TILE, tail_u = q_u + C::QBYTES;
+    const uint32_t q_u = ring_u + C::STAGES * 2 * C::TILE;
     const int G = a.r.G, R = a.r.H * G, RT = (R + NT * 8 - 1) / (NT * 8), kvh = a.r.rec.kvh;
     const int n_envs = a.r.meta ? a.r.n_envs : ev.n;
     const long long items = (long long)n_envs * kvh * a.n_split * RT;
-    uint32_t koff[2], voff[2];
+    uint32_t koff[KeyWords<HD>::OFFS];
     KeyWords<HD>::offsets(koff, g, t);
-    voff[0] = tile_addr<HD>(2 * t, g * (HD / 8));
-    voff[1] = tile_addr<HD>(2 * t + 1, g * (HD / 8));
+    const uint32_t voff = tile_addr<HD>(lane & 15, (lane >> 4) * 16);   // a row of the value tile, column pieces 2 p of it at voff ^ 32 p
     pdl_launch_dependents();
     pdl_wait();
 
@@ -73,24 +79,22 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         if (sp > 0 && t0 >= len) continue;
         const int ntile = (t1 - t0 + BLOCK - 1) / BLOCK;
         const char *kp = rec + a.r.rec.head(a.r.layer, 0, kh) + (size_t)t0 * HD, *vp = rec + a.r.rec.head(a.r.layer, 1, kh) + (size_t)t0 * HD;
-        const char *ksp = rec + a.r.rec.head_scales(a.r.layer, 0, kh) + t0 / BLOCK * 4, *vsp = rec + a.r.rec.head_scales(a.r.layer, 1, kh) + t0 / BLOCK * 4;
-        const char *mkp = rec + a.r.rec.mask + t0 / BLOCK * 4;
 
-        // position j of the item's stream: keys (even) or values (odd) of tile j / 2 with their scale and, beside the keys, the
-        // mask word; one commit group each, empty past the end
-        int jt = 0;
-        auto issue = [&](int plane, int slot) {
-            if (jt < ntile) {
-                const uint32_t dst = ring_u + (uint32_t)(slot * C::TILE), tail = tail_u + (uint32_t)(slot * 8);
-                request_tile<HD>(dst, (plane ? vp : kp) + (size_t)jt * C::TILE, t1 - t0 - jt * BLOCK, lane);
-                if (lane == 0) cp4(tail, (plane ? vsp : ksp) + (size_t)jt * 4);
-                if (lane == 1 && plane == 0) cp4(tail + 4, mkp + (size_t)jt * 4);
-                jt += plane;
+        // requests the item's next tile (keys and values) into a stage of the ring; one commit group, empty past the end
+        int left = t1 - t0;
+        auto issue = [&](int stage) {
+            if (left > 0) {
+                const uint32_t dst = ring_u + (uint32_t)(stage * 2 * C::TILE);
+                request_tile<HD>(dst, kp, left, lane);
+                request_tile<HD>(dst + C::TILE, vp, left, lane);
+                kp += C::TILE;
+                vp += C::TILE;
+                left -= BLOCK;
             }
             cp_commit();
         };
 #pragma unroll
-        for (int j = 0; j < C::SLOTS - 1; ++j) issue(j & 1, j);
+        for (int j = 0; j < C::STAGES - 1; ++j) issue(j);
 
         // queries
         uint32_t q[C::QS ? 1 : NT][ST][QW<F32>];
@@ -128,7 +132,9 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
             }
         };
 
-        float o[MT][NT][4], mr[NT][2], l[NT][2];
+        float o[MT][NT][4];   // column m * 16 + g of rows 2t, 2t + 1, column + 8 of the same; in units of `unit`
+        float unit = 1.f;
+        float mr[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             mr[nt][0] = mr[nt][1] = -FLT_MAX;
@@ -138,32 +144,50 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[m][nt][c] = 0.f;
         }
-        int slot = 0;
+        float ks_l = 0.f, vs_l = 0.f;      // scales and visible tokens of tile (i & ~31) + lane
+        uint32_t mk_l = 0;
+        int stage = 0;
         for (int i = 0; i < ntile; ++i) {
-            cp_wait<C::SLOTS - 2>();
-            __syncwarp();            // the tile is there for every lane, and every lane is done with the slot requested next
-            issue((C::SLOTS - 1) & 1, slot == 0 ? C::SLOTS - 1 : slot - 1);
-            const uint32_t kslot = ring_u + (uint32_t)(slot * C::TILE);
-            const uint2 tail = lds64(tail_u + (uint32_t)(slot * 8));
-            slot = slot + 1 == C::SLOTS ? 0 : slot + 1;
-            const float ks = read_scale(__uint_as_float(tail.x));
-            uint32_t mk = tail.y;
-            if (i == ntile - 1 && ((t1 - t0) & (BLOCK - 1))) mk &= (1u << ((t1 - t0) & (BLOCK - 1))) - 1u;
+            if ((i & 31) == 0) {
+                const int tile = t0 / BLOCK + i + lane;
+                mk_l = 0;
+                if (i + lane < ntile) {
+                    ks_l = read_scale(reinterpret_cast<const float *>(rec + a.r.rec.head_scales(a.r.layer, 0, kh))[tile]);
+                    vs_l = read_scale(reinterpret_cast<const float *>(rec + a.r.rec.head_scales(a.r.layer, 1, kh))[tile]);
+                    mk_l = reinterpret_cast<const uint32_t *>(rec + a.r.rec.mask)[tile];
+                    const int v = t1 - tile * BLOCK;
+                    if (v < BLOCK) mk_l &= (1u << v) - 1u;
+                }
+            }
+            const float ks = __shfl_sync(FULL, ks_l, i & 31), vs = __shfl_sync(FULL, vs_l, i & 31);
+            const uint32_t mk = __shfl_sync(FULL, mk_l, i & 31);
+            cp_wait<C::STAGES - 2>();
+            __syncwarp();            // the tile is there for every lane, and every lane is done with the stage requested next
+            issue(stage == 0 ? C::STAGES - 1 : stage - 1);
+            const uint32_t kslot = ring_u + (uint32_t)(stage * 2 * C::TILE), vslot = kslot + C::TILE;
+            stage = stage + 1 == C::STAGES ? 0 : stage + 1;
 
-            uint32_t pb[2][NT][2], pl[F32 ? 2 : 1][NT][2];
             if (mk) {
+                uint32_t pb[2][NT][2], pl[F32 ? 2 : 1][NT][2];
                 float s[2][NT][4];
+                if constexpr (NT <= 2) {
+                    KeyWords<HD> kw[2];
+                    kw[0].load(kslot, koff, 0);
+                    kw[1].load(kslot, koff, 1);
+                    score<HD, NT, F32, 2>(s, kw, query);
+                } else {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    KeyWords<HD> kw;
-                    kw.load(kslot, koff, h);
-                    score<HD, NT, F32>(s[h], kw, query);
+                    for (int h = 0; h < 2; ++h) {
+                        KeyWords<HD> kw;
+                        kw.load(kslot, koff, h);
+                        score<HD, NT, F32, 1>(s + h, &kw, query);
+                    }
                 }
                 const bool hides = mk != FULL;
                 if (hides) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const bool s0 = (mk >> (16 * h + g)) & 1, s1 = (mk >> (16 * h + 8 + g)) & 1;
+                        const bool s0 = (mk >> (16 * h + row_token(g))) & 1, s1 = (mk >> (16 * h + row_token(g) + 2)) & 1;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             if (!s0) s[h][nt][0] = s[h][nt][1] = -FLT_MAX;
@@ -209,8 +233,8 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                         float p0 = ex2(fmaf(s[h][nt][0], c[nt][0], -mr[nt][0])), p1 = ex2(fmaf(s[h][nt][1], c[nt][1], -mr[nt][1]));
                         float p2 = ex2(fmaf(s[h][nt][2], c[nt][0], -mr[nt][0])), p3 = ex2(fmaf(s[h][nt][3], c[nt][1], -mr[nt][1]));
                         if (hides) {   // (their scores are no more than very low: a factor of 0 makes them 0)
-                            if (!((mk >> (16 * h + g)) & 1)) p0 = p1 = 0.f;
-                            if (!((mk >> (16 * h + 8 + g)) & 1)) p2 = p3 = 0.f;
+                            if (!((mk >> (16 * h + row_token(g))) & 1)) p0 = p1 = 0.f;
+                            if (!((mk >> (16 * h + row_token(g) + 2)) & 1)) p2 = p3 = 0.f;
                         }
                         l[nt][0] += p0 + p2;
                         l[nt][1] += p1 + p3;
@@ -222,99 +246,104 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                         pb[h][nt][0] = transpose8(w0);
                         pb[h][nt][1] = transpose8(w1);
                     }
-            }
 
-            cp_wait<C::SLOTS - 2>();
-            __syncwarp();
-            issue(C::SLOTS & 1, slot == 0 ? C::SLOTS - 1 : slot - 1);
-            const uint32_t vslot = ring_u + (uint32_t)(slot * C::TILE);
-            const float vs = read_scale(__uint_as_float(lds32(tail_u + (uint32_t)(slot * 8))));
-            slot = slot + 1 == C::SLOTS ? 0 : slot + 1;
-            if (mk) {
-                uint32_t v[2][4][W];   // tokens 2t, 2t + 1, 2t + 8, 2t + 9 of each half
+                // outputs are kept in units of the last block's value scale: neighbours mostly share it (a power of two), and then the
+                // products add up in place
+                auto values = [&](auto &&take) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                    for (int p = 0; p < W; ++p) {       // 32 columns
+                        uint32_t v[2][4];
+                        load_columns(vslot + (voff ^ (uint32_t)(32 * p)), v[0]);
+                        load_columns(vslot + (voff ^ (uint32_t)(32 * p)) + 16 * HD, v[1]);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t at = vslot + voff[k & 1] + (uint32_t)((16 * h + 8 * (k >> 1)) * HD);
-                        if constexpr (W == 4) { const uint4 u = lds128(at); v[h][k][0] = u.x; v[h][k][1] = u.y; v[h][k][2] = u.z; v[h][k][3] = u.w; }
-                        else if constexpr (W == 2) { const uint2 u = lds64(at); v[h][k][0] = u.x; v[h][k][1] = u.y; }
-                        else v[h][k][0] = lds32(at);
-                    }
-#pragma unroll
-                for (int wd = 0; wd < W; ++wd)
-#pragma unroll
-                    for (int sub = 0; sub < 2; ++sub) {
-                        const int m = 2 * wd + sub;
-                        uint32_t f[2][4];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            // two columns, the codes of two tokens side by side
-                            const uint32_t p = prmt(v[h][0][wd], v[h][1][wd], sub ? 0x7362u : 0x5140u), r = prmt(v[h][2][wd], v[h][3][wd], sub ? 0x7362u : 0x5140u);
-                            f[h][0] = widen(p); f[h][1] = widen(p >> 16); f[h][2] = widen(r); f[h][3] = widen(r >> 16);
-                        }
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            float tmp[4] = {0.f, 0.f, 0.f, 0.f};
+                        for (int sub = 0; sub < 2; ++sub) {
+                            uint32_t f[2][4];
 #pragma unroll
                             for (int h = 0; h < 2; ++h) {
-                                if constexpr (F32) mma(tmp, f[h][0], f[h][1], f[h][2], f[h][3], pl[h][nt][0], pl[h][nt][1]);
-                                mma(tmp, f[h][0], f[h][1], f[h][2], f[h][3], pb[h][nt][0], pb[h][nt][1]);
+                                f[h][0] = widen(v[h][2 * sub]); f[h][1] = widen(v[h][2 * sub + 1]);
+                                f[h][2] = widen(v[h][2 * sub] >> 16); f[h][3] = widen(v[h][2 * sub + 1] >> 16);
                             }
 #pragma unroll
-                            for (int k = 0; k < 4; ++k) o[m][nt][k] = fmaf(vs, tmp[k], o[m][nt][k]);
+                            for (int nt = 0; nt < NT; ++nt) take(2 * p + sub, nt, f);
                         }
                     }
+                };
+                auto product = [&](float *c, int nt, uint32_t (*f)[4]) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if constexpr (F32) mma(c, f[h][0], f[h][1], f[h][2], f[h][3], pl[h][nt][0], pl[h][nt][1]);
+                        mma(c, f[h][0], f[h][1], f[h][2], f[h][3], pb[h][nt][0], pb[h][nt][1]);
+                    }
+                };
+                auto rescale = [&](float by) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) o[m][nt][c] *= by;
+                };
+                bool near = true;
+                if (vs != unit) {
+                    const float by = unit / vs;
+                    near = by >= 1.f / 1048576.f && by <= 1048576.f;
+                    rescale(near ? by : unit);
+                    unit = near ? vs : 1.f;
+                }
+                if (near) values([&](int m, int nt, uint32_t (*f)[4]) { product(o[m][nt], nt, f); });
+                else   // far apart, zero, or not a number: outputs as they are, the block's own product scaled and added
+                    values([&](int m, int nt, uint32_t (*f)[4]) {
+                        float tmp[4] = {0.f, 0.f, 0.f, 0.f};
+                        product(tmp, nt, f);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) o[m][nt][c] = fmaf(vs, tmp[c], o[m][nt][c]);
+                    });
             }
         }
         cp_wait<0>();      // only empty groups are left; the ring is free
         __syncwarp();
 
-        // rows 2t and 2t + 1 of each column tile, columns g * HD / 8 ..
+        // one column tile of rows at a time through the ring, so that rows leave in whole 128-byte runs
+        float *rows = reinterpret_cast<float *>(smem + (size_t)warp * C::WARP_BYTES);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
+        for (int nt = 0; nt < NT; ++nt) {
+            float L[2], inv[2];
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float L = l[nt][j];
-                L += __shfl_xor_sync(FULL, L, 4);
-                L += __shfl_xor_sync(FULL, L, 8);
-                L += __shfl_xor_sync(FULL, L, 16);
-                const int r = rt * NT * 8 + nt * 8 + 2 * t + j, tok = r / G, head = kh * G + r - tok * G;
-                if (r >= R) continue;
-                if (a.n_split > 1) {
-                    const size_t at = ((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + (size_t)tok * a.r.heads + head;
-                    float *dst = a.part_o + at * HD + g * (HD / 8);
-#pragma unroll
-                    for (int k = 0; k < HD / 32; ++k)
-                        *reinterpret_cast<float4 *>(dst + 4 * k) = make_float4(o[2 * k][nt][j], o[2 * k][nt][j + 2], o[2 * k + 1][nt][j], o[2 * k + 1][nt][j + 2]);
-                    if (g == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(mr[nt][j], L);
-                    continue;
+                L[j] = l[nt][j];
+                L[j] += __shfl_xor_sync(FULL, L[j], 4);
+                L[j] += __shfl_xor_sync(FULL, L[j], 8);
+                L[j] += __shfl_xor_sync(FULL, L[j], 16);
+                inv[j] = a.n_split > 1 ? unit : (L[j] == 0.f ? 0.f : unit / L[j]);
+                const int r = rt * NT * 8 + nt * 8 + 2 * t + j, tok = r / G, row = tok * a.r.heads + kh * G + r - tok * G;
+                if (g == 0 && r < R) {
+                    if (a.n_split > 1) *reinterpret_cast<float2 *>(a.part_ml + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + row) * 2) = make_float2(mr[nt][j], L[j]);
+                    else if (a.lse) a.lse[(size_t)env * a.r.H * a.r.heads + row] = L[j] == 0.f ? -INFINITY : (mr[nt][j] + log2f(L[j])) * LN2;
                 }
-                const float inv = L == 0.f ? 0.f : 1.f / L;
-                const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + g * (HD / 8);
-                if constexpr (F32) {
-#pragma unroll
-                    for (int k = 0; k < HD / 32; ++k) {
-                        const float4 u = make_float4(o[2 * k][nt][j] * inv, o[2 * k][nt][j + 2] * inv, o[2 * k + 1][nt][j] * inv, o[2 * k + 1][nt][j + 2] * inv);
-                        if (a.split_out) store_split4(a.out, a.out_t1, a.out_t2, off + 4 * k, u.x, u.y, u.z, u.w);
-                        else *reinterpret_cast<float4 *>((float *)a.out + off + 4 * k) = u;
-                    }
-                } else {
-                    uint32_t w[HD / 16];
-#pragma unroll
-                    for (int k = 0; k < HD / 16; ++k) {
-                        const __nv_bfloat162 u = __floats2bfloat162_rn(o[k][nt][j] * inv, o[k][nt][j + 2] * inv);
-                        w[k] = *reinterpret_cast<const uint32_t *>(&u);
-                    }
-                    __nv_bfloat16 *dst = (__nv_bfloat16 *)a.out + off;
-                    if constexpr (HD == 128) {
-                        *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-                        *reinterpret_cast<uint4 *>(dst + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-                    } else if constexpr (HD == 64) *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-                    else *reinterpret_cast<uint2 *>(dst) = make_uint2(w[0], w[1]);
-                }
-                if (a.lse && g == 0) a.lse[((size_t)env * a.r.H + tok) * a.r.heads + head] = L == 0.f ? -INFINITY : (mr[nt][j] + log2f(L)) * LN2;
             }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    rows[(2 * t) * C::PSTRIDE + m * 16 + 8 * k + g] = o[m][nt][2 * k] * inv[0];
+                    rows[(2 * t + 1) * C::PSTRIDE + m * 16 + 8 * k + g] = o[m][nt][2 * k + 1] * inv[1];
+                }
+            __syncwarp();
+#pragma unroll
+            for (int v = 0; v < HD / 16; ++v) {
+                const int row = (v * 32 + lane) / (HD / 4), col = (v * 32 + lane) % (HD / 4) * 4, r = rt * NT * 8 + nt * 8 + row, tok = r / G, head = kh * G + r - tok * G;
+                if (r < R) {
+                    const float4 u = *reinterpret_cast<const float4 *>(rows + row * C::PSTRIDE + col);
+                    const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + col;
+                    if (a.n_split > 1)
+                        *reinterpret_cast<float4 *>(a.part_o + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + (size_t)tok * a.r.heads + head) * HD + col) = u;
+                    else if constexpr (!F32) store4<__nv_bfloat16>((__nv_bfloat16 *)a.out + off, u.x, u.y, u.z, u.w);
+                    else if (a.split_out) store_split4(a.out, a.out_t1, a.out_t2, off, u.x, u.y, u.z, u.w);
+                    else store4<float>((float *)a.out + off, u.x, u.y, u.z, u.w);
+                }
+            }
+            __syncwarp();
+        }
     }
 }
 

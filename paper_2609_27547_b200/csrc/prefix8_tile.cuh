@@ -8,10 +8,11 @@
 // Every e4m3 value is an f16 value (3 mantissa bits, exponents -9 .. 8): codes are widened exactly, two per instruction, straight
 // from the words a lane reads from shared memory (the conversion runs at 63 pairs a clock and SM, the product at 957 MAC;
 // mma.sync on e4m3 operands is no way around it: it is that same conversion and product inside, 2.5 times the instructions).
-// The order of the contracted index is free as long as both operands agree: lane (g = lane / 4, t = lane % 4) takes the
-// HD / 4 consecutive columns t * HD / 4 .. of tokens g and g + 8 as its key operand (so its queries are HD / 4 consecutive
-// elements, too), and the HD / 8 consecutive columns g * HD / 8 .. of tokens 2t, 2t + 1, 2t + 8, 2t + 9 as its value
-// operand (so its outputs are consecutive).
+// The order of the contracted index is free as long as both operands agree.
+//   Keys: lane (g = lane / 4, t = lane % 4) takes the HD / 4 consecutive columns t * HD / 4 .. of two tokens, so its queries
+//   are HD / 4 consecutive elements, too.  Rows g and g + 8 of the A operand are tokens row_token(g) and row_token(g) + 2 ...
+//   Values: ... because ldmatrix (16 x 16 bytes, transposed) gives lane (g, t) the codes of tokens 4t .. 4t + 3 of columns g and
+//   g + 8: widened pairwise they are the A operand as they stand, if contraction slots 2t, 2t + 1, 2t + 8, 2t + 9 are these tokens.
 #pragma once
 #include "prefix8_internal.h"
 #include "ptx_helpers.cuh"
@@ -31,11 +32,11 @@ __device__ __forceinline__ uint32_t widen(uint32_t two)   // the e4m3 pair in th
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
     return r;
 }
-__device__ __forceinline__ uint32_t prmt(uint32_t a, uint32_t b, uint32_t sel)
+// Two 16 x 16 byte matrices, transposed: lanes 0 - 15 give the row addresses of the first, 16 - 31 of the second.  Lane (g, t) gets
+// rows 4t .. 4t + 3 of columns g and g + 8 of each.
+__device__ __forceinline__ void load_columns(uint32_t a, uint32_t *r)
 {
-    uint32_t r;
-    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(sel));
-    return r;
+    asm volatile("ldmatrix.sync.aligned.m16n16.x2.trans.shared.b8 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
 __device__ __forceinline__ uint32_t transpose8(uint32_t v)   // an 8 x 8 matrix of 16-bit values held two per lane
 {
@@ -112,13 +113,16 @@ __device__ __forceinline__ uint32_t lds32(uint32_t a)
 // integer way of widening would take a NaN code for 480).
 __device__ __forceinline__ float read_scale(float s) { return __float_as_uint(s) >> 31 ? __uint_as_float(0x7fffffffu) : s; }
 
+// The token (of 16) that is row g of the keys' operand; row g + 8 is the one two further on.
+__device__ __forceinline__ int row_token(int g) { return 4 * (g >> 1) + (g & 1); }
+
 // Where byte `off` of token `tok` of a tile stands in shared memory: 128-byte lines whose eight 16-byte pieces are permuted
-// so that the key reads (one or two tokens per phase) and the value reads (tokens 0, 2, 4, 6 per phase) touch every bank
-// once.  The pattern repeats every 8 tokens: address(tok + 8 k, off) = address(tok, off) + 8 k HD.
+// so that the key reads (two tokens per phase, four at head_dim 32) and the value reads (the same columns of eight tokens)
+// touch every bank once.  The pattern repeats every 8 tokens.
 template <int HD> __device__ __forceinline__ uint32_t tile_addr(int tok, int off)
 {
     const int lin = tok * HD + off, line = lin >> 7, piece = (lin >> 4) & 7;
-    const int sw = HD == 128 ? (line & 7) : (HD == 64 ? (line & 3) << 1 : (line & 1) << 1);
+    const int sw = HD == 128 ? (line & 7) : (HD == 64 ? (line & 3) : (line & 1) * 5);
     return (uint32_t)(line * 128 + ((piece ^ sw) << 4) + (lin & 15));
 }
 
@@ -199,52 +203,66 @@ template <int HD, bool F32> __device__ __forceinline__ float load_q(const void *
     return 1.f / mul;   // a power of two: exact
 }
 
-// One lane's words of the keys g and g + 8 of a 16-token half tile; kaddr = the tile's slot + tile_addr(g, t * HD / 4).
+// One lane's words of two keys of a 16-token half tile: its rows g and g + 8 of the A operand.
 template <int HD> struct KeyWords {
     uint32_t a[HD / 16], b[HD / 16];
+    static constexpr int OFFS = HD == 128 ? 4 : 2;
     __device__ __forceinline__ void load(uint32_t slot, const uint32_t *off, int half)
     {
         const uint32_t base = slot + (uint32_t)(half * 16 * HD);
         if constexpr (HD == 128) {
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const uint4 x = lds128(base + off[j]), y = lds128(base + off[j] + 8 * HD);
+                const uint4 x = lds128(base + off[j]), y = lds128(base + off[2 + j]);
                 a[4 * j] = x.x; a[4 * j + 1] = x.y; a[4 * j + 2] = x.z; a[4 * j + 3] = x.w;
                 b[4 * j] = y.x; b[4 * j + 1] = y.y; b[4 * j + 2] = y.z; b[4 * j + 3] = y.w;
             }
         } else if constexpr (HD == 64) {
-            const uint4 x = lds128(base + off[0]), y = lds128(base + off[0] + 8 * HD);
+            const uint4 x = lds128(base + off[0]), y = lds128(base + off[1]);
             a[0] = x.x; a[1] = x.y; a[2] = x.z; a[3] = x.w;
             b[0] = y.x; b[1] = y.y; b[2] = y.z; b[3] = y.w;
         } else {
-            const uint2 x = lds64(base + off[0]), y = lds64(base + off[0] + 8 * HD);
+            const uint2 x = lds64(base + off[0]), y = lds64(base + off[1]);
             a[0] = x.x; a[1] = x.y;
             b[0] = y.x; b[1] = y.y;
         }
     }
     static __device__ __forceinline__ void offsets(uint32_t *off, int g, int t)
     {
-        off[0] = tile_addr<HD>(g, t * (HD / 4));
-        off[1] = HD == 128 ? tile_addr<HD>(g, t * (HD / 4) + 16) : 0u;
+#pragma unroll
+        for (int i = 0; i < OFFS; ++i) {
+            const int tok = row_token(g) + 2 * (i / (OFFS / 2)), piece = OFFS == 4 ? i % 2 : 0;
+            off[i] = tile_addr<HD>(tok, t * (HD / 4) + 16 * piece);
+        }
     }
 };
 
-// Raw scores of 16 tokens and NT column tiles: s = keys x queries.  q(step, nt, w) hands out the queries' operands.
-template <int HD, int NT, bool F32, typename Q> __device__ __forceinline__ void score(float (*s)[4], const KeyWords<HD> &k, Q &&q)
+// Raw scores of N half tiles (16 tokens each) and NT column tiles: s = keys x queries.  q(step, nt, w) hands out the queries'
+// operands.  Half tiles side by side: N * NT independent chains of products hide one another's latency.
+template <int HD, int NT, bool F32, int N, typename Q> __device__ __forceinline__ void score(float (*s)[NT][4], const KeyWords<HD> *k, Q &&q)
 {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int h = 0; h < N; ++h)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) s[nt][c] = 0.f;
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) s[h][nt][c] = 0.f;
 #pragma unroll
     for (int st = 0; st < HD / 16; ++st) {
-        const uint32_t a0 = widen(k.a[st]), a1 = widen(k.b[st]), a2 = widen(k.a[st] >> 16), a3 = widen(k.b[st] >> 16);
+        uint32_t a[N][4];
+#pragma unroll
+        for (int h = 0; h < N; ++h) {
+            a[h][0] = widen(k[h].a[st]); a[h][1] = widen(k[h].b[st]); a[h][2] = widen(k[h].a[st] >> 16); a[h][3] = widen(k[h].b[st] >> 16);
+        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             uint32_t w[QW<F32>];
             q(st, nt, w);
-            if constexpr (F32) mma(s[nt], a0, a1, a2, a3, w[2], w[3]);
-            mma(s[nt], a0, a1, a2, a3, w[0], w[1]);
+#pragma unroll
+            for (int h = 0; h < N; ++h) {
+                if constexpr (F32) mma(s[h][nt], a[h][0], a[h][1], a[h][2], a[h][3], w[2], w[3]);
+                mma(s[h][nt], a[h][0], a[h][1], a[h][2], a[h][3], w[0], w[1]);
+            }
         }
     }
 }

@@ -34,7 +34,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
     const int HW = 1 << hw_log2, TW = 8 >> hw_log2, hw = warp & (HW - 1), tw = warp >> hw_log2;
     const int n_envs = a.r.meta ? a.r.n_envs : ev.n;
     const long long items = (long long)n_envs * n_chunk;
-    uint32_t koff[2];
+    uint32_t koff[KeyWords<HD>::OFFS];
     KeyWords<HD>::offsets(koff, g, t);
     pdl_launch_dependents();
     pdl_wait();
@@ -117,11 +117,12 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                     for (int h = 0; h < 2; ++h) {
                         KeyWords<HD> kw;
                         kw.load(at, koff, h);
-                        float s[NT][4];
-                        score<HD, NT, F32>(s, kw, [&](int st, int nt, uint32_t *w) {
+                        float sh[1][NT][4];
+                        score<HD, NT, F32, 1>(sh, &kw, [&](int st, int nt, uint32_t *w) {
 #pragma unroll
                             for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
                         });
+                        const float (*s)[4] = sh[0];
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             acc[i][h][0] += ex2(fmaf(s[nt][0], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[nt][1], ks * fr[nt][1], -ls[nt][1]));
@@ -143,7 +144,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                     v += __shfl_xor_sync(FULL, v, 1);
                     v += __shfl_xor_sync(FULL, v, 2);
                     const uint32_t m = __shfl_sync(FULL, seen, i);
-                    const int tok = 16 * h + 8 * c + g;
+                    const int tok = 16 * h + row_token(g) + 2 * c;
                     if (t == 0) red[warp][i * 32 + tok] = (m >> tok) & 1 ? v : 0.f;
                 }
         __syncthreads();
