@@ -62,7 +62,8 @@ typedef enum {
     EBRL_ERR_TIMEOUT = 7        /* a bounded device-side wait gave up                           */
 } ebrl_status_t;
 
-typedef enum { EBRL_F32 = 0, EBRL_BF16 = 1 } ebrl_dtype_t;
+typedef enum { EBRL_F32 = 0, EBRL_BF16 = 1,
+               EBRL_E4M3 = 2 /* kv_dtype only: prefixes as 8-bit records (ebrl_prefix8.h) */ } ebrl_dtype_t;
 
 /* cfg.flags */
 #define EBRL_FLAG_TEST_PULL   1u  /* replace the network by v = b_out - a (integrator check)    */
@@ -105,7 +106,11 @@ typedef struct {
     int32_t max_group_envs;      /* upper bound on n_envs of one submit                         */
     int32_t max_inflight_groups; /* groups that may be submitted before a sync (>= 1)           */
     int32_t param_dtype;         /* ebrl_dtype_t of the matrices                                */
-    int32_t kv_dtype;            /* ebrl_dtype_t of the prefix planes                           */
+    int32_t kv_dtype;            /* ebrl_dtype_t of the prefix planes: param_dtype, or EBRL_E4M3 (d_ctx = 0):
+                                    prefix_kv[i] is then environment i's 8-bit record (ebrl_prefix8.h)
+                                    of the layout {kv_layers, n_heads, head_dim, max_prefix_len},
+                                    P_i its length; hidden tokens take no part in cross-attention,
+                                    and one whose tokens are all hidden gives 0                 */
     int32_t kv_layers;           /* 1: one K/V plane pair for all layers; n_layers: per layer   */
     float rms_eps;               /* 1e-6                                                        */
     float temb_scale;            /* 1000                                                        */
@@ -195,6 +200,7 @@ ebrl_status_t ebrl_actgen_create(const ebrl_actgen_cfg_t *cfg, const ebrl_actgen
  *              planes live in scratch of the handle that grows to the largest batch seen
  *              (n_layers * 2 * sum(P_i) * d elements per batch in flight; EBRL_ERR_NOMEM when
  *              the device cannot hold it).
+ *              With kv_dtype = EBRL_E4M3 it is the environment's 8-bit record; what follows does not concern those.
  *              Every value in an environment's planes must be finite.  The tensor-core attention
  *              reads keys and values in blocks of 16 rows; in the last block of a plane the rows
  *              past P_i are the first rows of what follows it INSIDE THE SAME ENVIRONMENT'S
@@ -236,13 +242,24 @@ ebrl_status_t ebrl_actgen_submit_scattered(ebrl_actgen_t h, int32_t n_envs, cons
                                            float *const *out_ptrs, int32_t sm_quota, void *stream,
                                            const ebrl_submit_ext_t *ext);
 
+/* The same as ebrl_actgen_submit for handles with kv_dtype = EBRL_E4M3, which also adds up the weight that every
+ * prefix token gets in cross-attention -- over the layers, the Euler steps of the submit, the heads and the H action
+ * tokens: what ebrl_prefix8_evict shortens a prefix by.
+ *   prefix_weight  host [n] of DEVICE pointers, env i: fp32 [max_prefix_len], 4-byte aligned; entries below P_i are added to,
+ *                  the others left alone.  NULL entries: no weights of that environment.  Environments in flight
+ *                  must not share an array (checked within the groups queued together).
+ * The weights are ready when `out` is.  Each is a sum in a fixed order, and does not depend on the batch or the quota. */
+ebrl_status_t ebrl_actgen_submit_weighed(ebrl_actgen_t h, int32_t n_envs, const int64_t *env_ids, const void *const *prefix_kv,
+                                         const float *noise, float *out, float *const *prefix_weight, int32_t sm_quota,
+                                         void *stream, const ebrl_submit_ext_t *ext);
+
 /* The same with HOST buffers: prefix_kv[i], noise and out point to host memory (pinned memory
  * makes the copies asynchronous).  The planes and the noise are copied to device staging
  * owned by the handle when the call is made -- on a copy stream of the handle, so that the
  * upload of one batch overlaps the kernels of the previous one -- the group runs with its batch
  * on `stream` once its uploads are done, and `out` is copied back after the batch on `stream`;
  * `out` is valid after ebrl_actgen_sync.  The host buffers must stay valid until then.  Needs
- * prefix_len in ext, or every P_e = max_prefix_len.
+ * prefix_len in ext, or every P_e = max_prefix_len.  (8-bit records are copied whole, whatever their length.)
  * Batches of host-staged groups ramp up: after create and after every sync the first batch
  * closes at 1 group, the next at 2, then 4, ... up to max_inflight_groups, so that only the first
  * group's upload is exposed and every later batch uploads behind the previous one's kernels. */

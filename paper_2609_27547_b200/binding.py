@@ -16,7 +16,7 @@ from . import build as _build
 
 ABI_VERSION = 3
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_NOMEM, ERR_CUDA, ERR_ENV_BUSY, ERR_QUOTA, ERR_TIMEOUT = range(8)
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 FLAG_TEST_PULL, FLAG_GREEN_CTX, FLAG_TIMING, FLAG_FORCE_SIMT, FLAG_NO_FUSED, FLAG_FORCE_FUSED = 1, 2, 4, 8, 16, 32
 FLAG_TEST_DROP_GEMM_COPIES, FLAG_TEST_DROP_ATTN_COPIES, FLAG_DEBUG_CANARY = 64, 128, 256
 KC_NAMES = ("embed", "gemm", "self_attn", "cross_attn", "head", "prefix", "fused")
@@ -109,6 +109,7 @@ def lib():
                C.c_void_p, C.c_int32, C.c_void_p, C.POINTER(SubmitExt)]
         L.ebrl_actgen_submit.argtypes = sub
         L.ebrl_actgen_submit_host.argtypes = sub
+        L.ebrl_actgen_submit_weighed.argtypes = sub[:6] + [C.c_void_p] + sub[6:]
         L.ebrl_actgen_sync.argtypes = [C.c_void_p]
         L.ebrl_actgen_flush.argtypes = [C.c_void_p]
         L.ebrl_actgen_update_weights.argtypes = [C.c_void_p, C.POINTER(Weights), C.c_void_p, C.POINTER(C.c_uint64)]
@@ -147,10 +148,11 @@ def lib():
 
 def make_cfg(*, H, A, d, n_layers, n_heads, K_steps, max_prefix_len, max_group_envs,
              max_inflight_groups=1, dtype=F32, mlp_mult=4, kv_layers=1, rms_eps=1e-6,
-             temb_scale=1000.0, temb_max_period=10000.0, flags=0, device=0, d_ctx=0) -> Cfg:
-    """``d_ctx > 0``: prefixes are hidden states [P][d_ctx] projected per layer (then kv_layers = n_layers)."""
+             temb_scale=1000.0, temb_max_period=10000.0, flags=0, device=0, d_ctx=0, kv_dtype=None) -> Cfg:
+    """``d_ctx > 0``: prefixes are hidden states [P][d_ctx] projected per layer (then kv_layers = n_layers).
+    ``kv_dtype``: default ``dtype``; E4M3: prefixes are 8-bit records (``prefix8``)."""
     return Cfg(ABI_VERSION, H, A, d, n_layers, n_heads, mlp_mult, K_steps, max_prefix_len,
-               max_group_envs, max_inflight_groups, dtype, dtype, n_layers if d_ctx > 0 else kv_layers, rms_eps,
+               max_group_envs, max_inflight_groups, dtype, dtype if kv_dtype is None else kv_dtype, n_layers if d_ctx > 0 else kv_layers, rms_eps,
                temb_scale, temb_max_period, flags, device, 0, d_ctx, 0)
 
 
@@ -183,6 +185,7 @@ class ActGen:
         matrices in the configured dtype, gains and b_out fp32)."""
         self._L = lib()
         self.cfg = cfg
+        self._record_bytes = None
         w, keep = self._marshal(weights)
         self._h = C.c_void_p()
         st = self._L.ebrl_actgen_create(C.byref(cfg), C.byref(w), C.byref(self._h))
@@ -230,6 +233,19 @@ class ActGen:
         if st != OK:
             raise EbrlError(st, (self._L.ebrl_actgen_last_error(self._h) or b"").decode())
 
+    def _check_records(self, prefix_kv, prefix_len):
+        """8-bit handles: every prefix is a record of the handle's layout, and its length is given."""
+        if self.cfg.kv_dtype != E4M3:
+            return
+        if self._record_bytes is None:
+            from . import prefix8
+            self._record_bytes = prefix8.layout_for(self.cfg).record_bytes
+        if prefix_len is None:
+            raise ValueError("8-bit records need prefix_len")
+        for t in prefix_kv:
+            if t.dtype != torch.uint8 or t.numel() != self._record_bytes or not t.is_contiguous():
+                raise ValueError("8-bit records must be contiguous uint8 tensors of %d bytes" % self._record_bytes)
+
     def _submit(self, fn, env_ids, kv_ptrs, noise_ptr, out_ptr, sm_quota, stream, prefix_len, step_index, n_steps):
         n = len(env_ids)
         ids = (C.c_int64 * max(1, n))(*[int(e) for e in env_ids])
@@ -240,9 +256,11 @@ class ActGen:
     def submit(self, env_ids: Sequence[int], prefix_kv: Optional[Sequence[torch.Tensor]], noise: torch.Tensor,
                out: torch.Tensor, sm_quota: int = 0, stream: Optional[torch.cuda.Stream] = None,
                prefix_len: Optional[Sequence[int]] = None, step_index: Optional[Sequence[int]] = None,
-               n_steps: int = 0):
+               n_steps: int = 0, prefix_weight: Optional[Sequence[Optional[torch.Tensor]]] = None):
         """``ebrl_actgen_submit``: device tensors; prefix_kv[i] is [kv_layers][2][P_i][d], or the
-        hidden states [P_i][d_ctx] when the handle was created with ``d_ctx > 0``."""
+        hidden states [P_i][d_ctx] when the handle was created with ``d_ctx > 0``, or a record (uint8, then with
+        ``prefix_len``) when it was created with ``kv_dtype = E4M3``.  ``prefix_weight`` (records only): fp32
+        [>= max_prefix_len] tensors or None, one per environment (``ebrl_actgen_submit_weighed``)."""
         if noise.device.type != "cuda" or out.device.type != "cuda":
             raise ValueError("noise and out must be CUDA tensors")
         if noise.dtype != torch.float32 or out.dtype != torch.float32 or not noise.is_contiguous() or not out.is_contiguous():
@@ -252,11 +270,21 @@ class ActGen:
             for t in prefix_kv:
                 if t.device.type != "cuda" or not t.is_contiguous():
                     raise ValueError("prefix planes must be contiguous CUDA tensors")
+            self._check_records(prefix_kv, prefix_len)
             kv_ptrs = [t.data_ptr() for t in prefix_kv]
             if prefix_len is None:
                 prefix_len = [t.shape[-2] for t in prefix_kv]
         s = stream if stream is not None else torch.cuda.current_stream(noise.device)
-        self._submit(self._L.ebrl_actgen_submit, env_ids, kv_ptrs, noise.data_ptr(), out.data_ptr(), sm_quota,
+        fn = self._L.ebrl_actgen_submit
+        if prefix_weight is not None:
+            if len(prefix_weight) != len(env_ids):
+                raise ValueError("one prefix_weight per environment")
+            for t in prefix_weight:
+                if t is not None and (t.device != noise.device or t.dtype != torch.float32 or not t.is_contiguous() or t.numel() < self.cfg.max_prefix_len):
+                    raise ValueError("prefix_weight must be contiguous CUDA fp32 tensors of at least max_prefix_len elements")
+            wp = (C.c_void_p * max(1, len(env_ids)))(*[t.data_ptr() if t is not None else None for t in prefix_weight])
+            fn = lambda h, n, ids, kv, no, ou, qu, st, ex: self._L.ebrl_actgen_submit_weighed(h, n, ids, kv, no, ou, wp, qu, st, ex)  # noqa: E731
+        self._submit(fn, env_ids, kv_ptrs, noise.data_ptr(), out.data_ptr(), sm_quota,
                      s.cuda_stream, prefix_len, step_index, n_steps)
 
     def submit_host(self, env_ids, prefix_kv: Optional[Sequence[torch.Tensor]], noise: torch.Tensor, out: torch.Tensor,
@@ -267,6 +295,7 @@ class ActGen:
             raise ValueError("noise and out must be host tensors")
         kv_ptrs = None
         if prefix_kv is not None:
+            self._check_records(prefix_kv, prefix_len)
             kv_ptrs = [t.data_ptr() for t in prefix_kv]
             if prefix_len is None:
                 prefix_len = [t.shape[-2] for t in prefix_kv]
@@ -407,9 +436,11 @@ def sim_corunner_launch(buf: torch.Tensor, n_steps: int, n_ctas: int, stream: to
         raise EbrlError(st, "corunner launch failed")
 
 
-def cfg_for(w, *, max_group_envs: Optional[int] = None, max_inflight_groups: int = 1, flags: int = 0, device: int = 0) -> Cfg:
+def cfg_for(w, *, max_group_envs: Optional[int] = None, max_inflight_groups: int = 1, flags: int = 0, device: int = 0,
+            kv_dtype: Optional[int] = None) -> Cfg:
     """The library configuration of a ``synth.Workload``."""
     return make_cfg(H=w.H, A=w.A, d=w.d, n_layers=w.L, n_heads=w.n_heads, K_steps=w.K, max_prefix_len=w.P[1],
                     max_group_envs=max_group_envs or (w.group[1] if w.group else w.B),
                     max_inflight_groups=max_inflight_groups, dtype=BF16 if w.dtype == "bf16" else F32,
-                    mlp_mult=w.mlp_mult, flags=flags, device=device, d_ctx=getattr(w, "d_ctx", 0))
+                    mlp_mult=w.mlp_mult, flags=flags, device=device, d_ctx=getattr(w, "d_ctx", 0),
+                    kv_dtype=kv_dtype)

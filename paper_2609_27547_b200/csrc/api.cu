@@ -4,6 +4,7 @@
 // table built once at create.
 #include "../../include/ebrl_actgen.h"
 #include "actgen_internal.h"
+#include "prefix8_internal.h"
 
 #include <algorithm>
 #include <cmath>
@@ -99,6 +100,9 @@ struct Slot {
     void *hid_pack = nullptr, *planes = nullptr;
     size_t proj_cap_rows = 0;
     int prefix_rows = 0, prefix_slices = 0;   // of the batch being launched
+    // 8-bit prefixes: the log-sum-exp of every row and head (of the last cross-attention), for the token weights
+    float *lse = nullptr;
+    int weigh_len = 0;                        // of the batch being launched: its longest prefix if any environment wants weights, else 0
     TensorMap128 t_hid;
 };
 
@@ -123,6 +127,8 @@ struct ebrl_actgen {
     bool use_attn_mma = false;    // tensor-core attention (bf16, H <= 16, head_dim 64/128)
     int attn_hpc = 8;             // heads per slab of the tensor-core attention kernel and its descriptors
     bool use_attn_f32 = false;    // warp-per-item fp32 attention (head_dim 64, H <= 8)
+    bool kv8 = false;             // prefixes are 8-bit records of the layout `rec`
+    p8::Record rec = {};
     int *status_d = nullptr;      // device status word written by kernels whose waits ran out
     unsigned long long wait_ns = 0;
     size_t esz = 4;   // bytes per element of matrices / activations / planes
@@ -171,7 +177,7 @@ ebrl_status_t check_cfg(const ebrl_actgen_cfg_t *c, std::string *why)
     if (c->d % c->n_heads) return bad(EBRL_ERR_INVALID_ARG, "d must be a multiple of n_heads");
     if (c->max_prefix_len < 1 || c->max_group_envs < 1 || c->max_inflight_groups < 1)
         return bad(EBRL_ERR_INVALID_ARG, "max_prefix_len, max_group_envs, max_inflight_groups must be >= 1");
-    if ((c->param_dtype != EBRL_F32 && c->param_dtype != EBRL_BF16) || (c->kv_dtype != EBRL_F32 && c->kv_dtype != EBRL_BF16))
+    if ((c->param_dtype != EBRL_F32 && c->param_dtype != EBRL_BF16) || (c->kv_dtype != EBRL_F32 && c->kv_dtype != EBRL_BF16 && c->kv_dtype != EBRL_E4M3))
         return bad(EBRL_ERR_INVALID_ARG, "unknown dtype");
     if (c->kv_layers != 1 && c->kv_layers != c->n_layers) return bad(EBRL_ERR_INVALID_ARG, "kv_layers must be 1 or n_layers");
     if (!(c->rms_eps >= 0.f) || !(c->temb_max_period > 0.f)) return bad(EBRL_ERR_INVALID_ARG, "rms_eps >= 0 and temb_max_period > 0 required");
@@ -179,7 +185,11 @@ ebrl_status_t check_cfg(const ebrl_actgen_cfg_t *c, std::string *why)
     if (c->d % SSQ_W) return bad(EBRL_ERR_UNSUPPORTED, "d must be a multiple of 128");
     const int hd = c->d / c->n_heads;
     if (hd != 32 && hd != 64 && hd != 128) return bad(EBRL_ERR_UNSUPPORTED, "head_dim must be 32, 64 or 128");
-    if (c->param_dtype != c->kv_dtype) return bad(EBRL_ERR_UNSUPPORTED, "param_dtype and kv_dtype must match");
+    if (c->kv_dtype == EBRL_E4M3) {
+        if (c->d_ctx > 0) return bad(EBRL_ERR_UNSUPPORTED, "8-bit prefixes are keys and values, not hidden states (d_ctx = 0)");
+        const ebrl_prefix8_layout_t l = {std::max(c->kv_layers, 1), c->n_heads, hd, c->max_prefix_len};
+        if (!ebrl_prefix8_record_bytes(&l)) return bad(EBRL_ERR_UNSUPPORTED, ebrl_prefix8_last_error());
+    } else if (c->param_dtype != c->kv_dtype) return bad(EBRL_ERR_UNSUPPORTED, "kv_dtype must be param_dtype or 8 bits");
     if ((int64_t)c->d * c->A * 4 > 200 * 1024) return bad(EBRL_ERR_UNSUPPORTED, "d * A is limited to 51200 (the input embedding is staged in shared memory)");
     if (c->d_ctx < 0) return bad(EBRL_ERR_INVALID_ARG, "d_ctx < 0");
     if (c->d_ctx > 0) {
@@ -514,6 +524,29 @@ cudaError_t launch_attn(ebrl_actgen *h, const AttnArgs &a, int grid, cudaStream_
     return launch_attn_simt(a, h->bf16, grid, st);
 }
 
+// Cross-attention over 8-bit records, and the token weights where a submit asked for them.  Prefixes are never cut: an
+// environment's result involves nothing but the environment.
+void cross_attend8(ebrl_actgen *h, Slot &s, Launcher &ln, const AttnArgs &x, double sum_P)
+{
+    static const p8::Envs none = {};
+    const int d = x.d, M = x.n_envs * x.H;
+    p8::AttendArgs a{};
+    a.r.rec = h->rec; a.r.layer = x.kv_plane; a.r.q = x.q; a.r.q_env = (long long)x.H * x.q_stride; a.r.q_tok = x.q_stride;
+    a.r.H = x.H; a.r.heads = x.n_heads; a.r.G = 1; a.r.scale = 1.0f / sqrtf((float)x.hd); a.r.meta = x.meta; a.r.n_envs = x.n_envs;
+    a.out = x.out; a.o_env = (long long)x.H * x.o_stride; a.o_tok = x.o_stride;
+    a.out_t1 = x.out_t1; a.out_t2 = x.out_t2; a.split_out = x.split_out;
+    a.n_split = 1; a.lse = s.weigh_len > 0 ? s.lse : nullptr;
+    const int quota = ln.grid < h->n_sms ? ln.grid : 0;   // the whole chip: the launch that evens out ragged prefixes
+    ln.run(EBRL_KC_CROSS_ATTN, 4.0 * x.H * sum_P * d, 2.0 * sum_P * d + 2.0 * M * d * (double)h->esz,
+           [&] { return p8::launch_attend(a, none, !h->bf16, quota, ln.st); });
+    if (s.weigh_len > 0) {
+        p8::WeighArgs w{};
+        w.r = a.r; w.lse = s.lse; w.l_env = (long long)x.H * x.n_heads; w.l_tok = x.n_heads; w.l_head = 1; w.accumulate = 1;
+        ln.run(EBRL_KC_CROSS_ATTN, 2.0 * x.H * sum_P * d, sum_P * d + (double)M * d * h->esz,
+               [&] { return p8::launch_weigh(w, none, !h->bf16, s.weigh_len, quota, ln.st); });
+    }
+}
+
 // Tile shape of a tensor-core GEMM by estimated time = waves x tile area / relative efficiency:
 // 2 = CTA pairs (256 x 256), 256 = one CTA 128 x 256, 128 = one CTA 128 x 128.  The accumulation
 // order per output element is the same for every shape, so the choice does not change a single
@@ -666,7 +699,8 @@ cudaError_t enqueue_batch(ebrl_actgen *h, Slot &s, int S, const int32_t *n_activ
                     a.plane_rows = c.d_ctx > 0 ? s.prefix_rows : 0;
                     a.self_map = s.maps_d; a.kv_maps = s.maps_d + 1;
                     if (h->use_tc3) { a.out = s.att3[0]; a.out_t1 = s.att3[1]; a.out_t2 = s.att3[2]; a.split_out = 1; }
-                    ln.run(EBRL_KC_CROSS_ATTN, 4.0 * H * sum_P_active[step] * d,
+                    if (h->kv8) cross_attend8(h, s, ln, a, sum_P_active[step]);
+                    else ln.run(EBRL_KC_CROSS_ATTN, 4.0 * H * sum_P_active[step] * d,
                            2.0 * sum_P_active[step] * d * esz + 2.0 * M * d * esz, [&] { return launch_attn(h, a, grid, st); });
                 }
                 gemm(s.att, s.t_att, w.w_oc, w.t_oc, d, d, EPI_RESID, nullptr, w.g3, w.t3[3]);
@@ -698,7 +732,7 @@ ebrl_status_t flush_slot(ebrl_actgen *h, Slot &s)
     std::vector<double> sum_P(c.K_steps, 0.0);
     int S = 0;
     std::vector<TensorMap128> maps_packed;
-    const bool with_maps = h->use_attn_mma && !(c.flags & EBRL_FLAG_TEST_PULL);
+    const bool with_maps = h->use_attn_mma && !h->kv8 && !(c.flags & EBRL_FLAG_TEST_PULL);
     const bool hidden = c.d_ctx > 0 && !(c.flags & EBRL_FLAG_TEST_PULL) && c.n_layers > 0;
     if (with_maps) maps_packed.resize(n);
     long prefix_rows = 0;
@@ -711,6 +745,9 @@ ebrl_status_t flush_slot(ebrl_actgen *h, Slot &s)
         S = std::max(S, (int)m.nsteps);
         for (int t = 0; t < m.nsteps; ++t) { n_active[t] += 1; sum_P[t] += m.P; }
     }
+    s.weigh_len = 0;
+    for (const EnvMeta &m : s.pending)
+        if (m.weight) s.weigh_len = std::max(s.weigh_len, (int)m.P);
     s.pending.clear();
     s.pending_maps.clear();
     if (hidden) {
@@ -766,7 +803,7 @@ ebrl_status_t flush_slot(ebrl_actgen *h, Slot &s)
         h->host_depth = std::min(2 * h->host_depth, c.max_inflight_groups);
     }
     CK(cudaMemcpyAsync(s.meta_d, s.meta_h, sizeof(EnvMeta) * (size_t)n, cudaMemcpyHostToDevice, cs));
-    if (h->use_attn_mma && !(c.flags & EBRL_FLAG_TEST_PULL)) {
+    if (with_maps) {
         // one TMA descriptor per environment: its planes as a [kv_layers * 2 * P][d] matrix
         // (encoded when the group was submitted, so that the host work overlaps the previous batch)
         for (int j = 0; j < n; ++j) s.maps_h[j] = maps_packed[j];
@@ -798,7 +835,8 @@ ebrl_status_t flush_slot(ebrl_actgen *h, Slot &s)
 ebrl_status_t submit_impl(ebrl_actgen *h, int32_t n, const int64_t *env_ids, const void *const *prefix_kv,
                           const float *noise, float *out, int32_t sm_quota, void *stream,
                           const ebrl_submit_ext_t *ext, bool host_buffers,
-                          const float *const *noise_ptrs = nullptr, float *const *out_ptrs = nullptr)
+                          const float *const *noise_ptrs = nullptr, float *const *out_ptrs = nullptr,
+                          float *const *prefix_weight = nullptr)
 {
     if (noise_ptrs || out_ptrs) {   // per-environment state and result pointers instead of two [n][H][A] arrays
         if (!noise_ptrs || !out_ptrs || host_buffers || n < 1) return fail(h, EBRL_ERR_INVALID_ARG, "per-environment pointers: both arrays, device buffers, n >= 1");
@@ -816,6 +854,16 @@ ebrl_status_t submit_impl(ebrl_actgen *h, int32_t n, const int64_t *env_ids, con
         if (h->busy_ids.count(env_ids[i]))
             return fail(h, EBRL_ERR_ENV_BUSY, "env id %lld is in a group that has not been synced", (long long)env_ids[i]);
     if (h->sticky != EBRL_OK) return fail(h, h->sticky, "handle is in a failed state: %s", h->err.c_str());
+    if (prefix_weight) {
+        std::unordered_set<const void *> seen;
+        for (const EnvMeta &m : h->slots[h->fill].pending)
+            if (m.weight) seen.insert(m.weight);
+        for (int i = 0; i < n; ++i) {
+            if (!prefix_weight[i]) continue;
+            if ((uintptr_t)prefix_weight[i] & 3) return fail(h, EBRL_ERR_INVALID_ARG, "prefix_weight[%d] is not 4-byte aligned", i);
+            if (!seen.insert(prefix_weight[i]).second) return fail(h, EBRL_ERR_INVALID_ARG, "prefix_weight[%d] is another environment's, too", i);
+        }
+    }
     CK(cudaSetDevice(h->cfg.device));
 
     const ebrl_actgen_cfg_t &c = h->cfg;
@@ -836,7 +884,7 @@ ebrl_status_t submit_impl(ebrl_actgen *h, int32_t n, const int64_t *env_ids, con
 
     // bytes of one environment's prefix as the caller hands it over: its planes, or its hidden states
     auto prefix_bytes = [&](int P) {
-        return c.d_ctx > 0 ? (size_t)P * c.d_ctx * h->esz : (size_t)c.kv_layers * 2 * P * c.d * h->esz;
+        return h->kv8 ? h->rec.bytes : (c.d_ctx > 0 ? (size_t)P * c.d_ctx * h->esz : (size_t)c.kv_layers * 2 * P * c.d * h->esz);
     };
     const float *noise_d = noise;
     float *out_d = out;
@@ -856,7 +904,7 @@ ebrl_status_t submit_impl(ebrl_actgen *h, int32_t n, const int64_t *env_ids, con
             const size_t whole = need / (size_t)(s.groups_pending + 1) * (size_t)c.max_inflight_groups;
             h->stage_hint = std::max(h->stage_hint, std::max(need, whole));
             if ((st = flush_slot(h, s)) != EBRL_OK) return st;
-            return submit_impl(h, n, env_ids, prefix_kv, noise, out, sm_quota, stream, ext, host_buffers);
+            return submit_impl(h, n, env_ids, prefix_kv, noise, out, sm_quota, stream, ext, host_buffers, noise_ptrs, out_ptrs, prefix_weight);
         }
         if (!pull && (s.kv_stage_bytes < need || (s.stage_used == 0 && s.kv_stage_bytes < h->stage_hint))) {   // nothing staged in the slot: grow it
             if (s.kv_stage) cudaFree(s.kv_stage);
@@ -900,7 +948,7 @@ ebrl_status_t submit_impl(ebrl_actgen *h, int32_t n, const int64_t *env_ids, con
 
     // descriptors of the group's planes first: a failure must leave nothing of the group queued
     std::vector<TensorMap128> group_maps;
-    if (h->use_attn_mma && !pull && c.d_ctx == 0) {   // (projected planes get theirs when the batch is launched)
+    if (h->use_attn_mma && !h->kv8 && !pull && c.d_ctx == 0) {   // (projected planes get theirs when the batch is launched)
         group_maps.resize(n);
         for (int i = 0; i < n; ++i) {
             const int P = (ext && ext->prefix_len) ? ext->prefix_len[i] : c.max_prefix_len;
@@ -919,6 +967,7 @@ ebrl_status_t submit_impl(ebrl_actgen *h, int32_t n, const int64_t *env_ids, con
         m.nsteps = ns;
         m.noise = noise_ptrs ? noise_ptrs[i] : noise_d + (size_t)i * chunk;
         m.out = out_ptrs ? out_ptrs[i] : out_d + (size_t)i * chunk;
+        m.weight = prefix_weight ? prefix_weight[i] : nullptr;
         s.pending.push_back(m);
         if (!group_maps.empty()) s.pending_maps.push_back(group_maps[i]);
         env_steps += (uint64_t)ns;
@@ -1039,6 +1088,8 @@ ebrl_status_t ebrl_actgen_create(const ebrl_actgen_cfg_t *cfg, const ebrl_actgen
     h->esz = h->bf16 ? 2 : 4;
     h->hd = cfg->d / cfg->n_heads;
     h->md = cfg->mlp_mult * cfg->d;
+    h->kv8 = cfg->kv_dtype == EBRL_E4M3;
+    if (h->kv8) h->rec = p8::record_of(ebrl_prefix8_layout_t{std::max(cfg->kv_layers, 1), cfg->n_heads, h->hd, cfg->max_prefix_len});
 
     auto bail = [&](ebrl_status_t s) {
         g_create_error = h->err;
@@ -1065,7 +1116,7 @@ ebrl_status_t ebrl_actgen_create(const ebrl_actgen_cfg_t *cfg, const ebrl_actgen
     h->use_attn_f32 = !h->bf16 && !(cfg->flags & EBRL_FLAG_FORCE_SIMT) && attn_f32_supported(cfg->H, h->hd);
     h->use_tc3 = !h->bf16 && !(cfg->flags & EBRL_FLAG_FORCE_SIMT) && gemm_tc3_supported(d, d) && gemm_tc3_supported(md, d) &&
                  gemm_tc3_supported(d, md) && gemm_tc3_supported(3 * d, d);
-    h->fused_ok = h->use_tc && h->use_attn_mma && fused_supported(cfg->H, cfg->A, d, md, cfg->n_heads, h->hd);
+    h->fused_ok = h->use_tc && h->use_attn_mma && !h->kv8 && fused_supported(cfg->H, cfg->A, d, md, cfg->n_heads, h->hd);
     if (const char *e6 = getenv("EBRL_FUSED_MAX_ROWS")) h->fused_max_rows = atol(e6);
     if (const char *e7 = getenv("EBRL_TRACE")) h->trace = atoi(e7) != 0;
     {   // the attention descriptors are shared with the persistent step kernel, whose slabs are at most 8 heads: wide slabs
@@ -1121,6 +1172,10 @@ ebrl_status_t ebrl_actgen_create(const ebrl_actgen_cfg_t *cfg, const ebrl_actgen
             cudaGetLastError();
             fail(h, EBRL_ERR_NOMEM, "pinned staging allocation failed");
             return bail(EBRL_ERR_NOMEM);
+        }
+        if (h->kv8) {
+            if ((st = dev_alloc(h, &p, rows * cfg->n_heads * 4, "the log-sum-exp workspace")) != EBRL_OK) return bail(st);
+            s.lse = (float *)p;
         }
         // stale workspace rows are read (never stored) as padding of tiles and boxes: keep them finite
         if (cudaMemset(s.x, 0, rows * d * 4) != cudaSuccess || cudaMemset(s.xg, 0, rows * d * esz) != cudaSuccess ||
@@ -1218,6 +1273,17 @@ ebrl_status_t ebrl_actgen_submit_scattered(ebrl_actgen_t h, int32_t n, const int
     if (n == 0) return EBRL_OK;
     if (n < 0 || !state_ptrs || !out_ptrs) return fail(h, EBRL_ERR_INVALID_ARG, "n_envs < 0, or state_ptrs / out_ptrs is NULL");
     return submit_impl(h, n, env_ids, prefix_kv, nullptr, nullptr, sm_quota, stream, ext, false, state_ptrs, out_ptrs);
+}
+
+ebrl_status_t ebrl_actgen_submit_weighed(ebrl_actgen_t h, int32_t n, const int64_t *env_ids, const void *const *prefix_kv,
+                                         const float *noise, float *out, float *const *prefix_weight, int32_t sm_quota,
+                                         void *stream, const ebrl_submit_ext_t *ext)
+{
+    if (!h) return EBRL_ERR_INVALID_ARG;
+    std::lock_guard<std::mutex> lk(h->mu);
+    if (!h->kv8) return fail(h, EBRL_ERR_UNSUPPORTED, "token weights need 8-bit prefixes (kv_dtype = EBRL_E4M3)");
+    if (n > 0 && !prefix_weight) return fail(h, EBRL_ERR_INVALID_ARG, "prefix_weight is NULL");
+    return submit_impl(h, n, env_ids, prefix_kv, noise, out, sm_quota, stream, ext, false, nullptr, nullptr, prefix_weight);
 }
 
 ebrl_status_t ebrl_actgen_submit_host(ebrl_actgen_t h, int32_t n, const int64_t *env_ids, const void *const *prefix_kv_host,

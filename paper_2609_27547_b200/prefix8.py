@@ -147,6 +147,11 @@ def _n_slots(lens: torch.Tensor, slots, pool: torch.Tensor):
     return s, (None if s is None else s.data_ptr())
 
 
+def layout_for(cfg) -> Layout:
+    """The layout of the records that a handle created with ``cfg`` (kv_dtype E4M3) takes."""
+    return Layout(max(cfg.kv_layers, 1), cfg.n_heads, cfg.d // cfg.n_heads, cfg.max_prefix_len)
+
+
 def new_pool(layout: Layout, n_slots: int, device="cuda") -> torch.Tensor:
     """A zeroed pool of ``n_slots`` records."""
     if layout.record_bytes == 0:
