@@ -538,7 +538,7 @@ void cross_attend8(ebrl_actgen *h, Slot &s, Launcher &ln, const AttnArgs &x, dou
     a.n_split = 1; a.lse = s.weigh_len > 0 ? s.lse : nullptr;
     const int quota = ln.grid < h->n_sms ? ln.grid : 0;   // the whole chip: the launch that evens out ragged prefixes
     ln.run(EBRL_KC_CROSS_ATTN, 4.0 * x.H * sum_P * d, 2.0 * sum_P * d + 2.0 * M * d * (double)h->esz,
-           [&] { return p8::launch_attend(a, none, !h->bf16, quota, ln.st); });
+           [&] { return p8::launch_attend(a, none, !h->bf16, quota, h->n_sms, ln.st); });
     if (s.weigh_len > 0) {
         p8::WeighArgs w{};
         w.r = a.r; w.lse = s.lse; w.l_env = (long long)x.H * x.n_heads; w.l_tok = x.n_heads; w.l_head = 1; w.accumulate = 1;

@@ -156,9 +156,9 @@ void cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int h
     }
     long long items = 0;
     for (int i = 0; i < n; ++i) items += len[i] > 0;
-    const int rows = H * (heads / l.n_kv_heads), tile = row_tile(rows);
-    items *= (long long)l.n_kv_heads * ((rows + tile - 1) / tile);
-    const long long warps = (long long)sms * attend_warps(rows, f32);
+    const int rows = H * (heads / l.n_kv_heads);
+    items *= (long long)l.n_kv_heads * ((rows + 7) / 8);   // few items are taken in tiles of 8 rows
+    const long long warps = (long long)sms * attend_warps(8, f32);
     if (items == 0 || items * 2 > warps) return;
     const long long parts = warps / items;
     const long long piece = std::max(256LL, ((most + parts - 1) / parts + 127) / 128 * 128);
@@ -278,8 +278,8 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
         if ((st = device_sms(sm_quota, &sms)) != EBRL_OK) return st;
         const bool f32 = q_dtype == EBRL_F32;
         cut(*layout, n, len, H, n_heads, split_tokens, sm_quota ? sm_quota : sms, f32, &split, &n_split);
-        const int rows = H * (n_heads / layout->n_kv_heads), tile = row_tile(rows);
-        if ((int64_t)std::min(n, CHUNK_ENVS) * layout->n_kv_heads * n_split * ((rows + tile - 1) / tile) > INT32_MAX)
+        const int rows = H * (n_heads / layout->n_kv_heads);
+        if ((int64_t)std::min(n, CHUNK_ENVS) * layout->n_kv_heads * n_split * ((rows + 7) / 8) > INT32_MAX)
             return fail(EBRL_ERR_UNSUPPORTED, "too many pieces in one call");
         const uint64_t pr = part_rows(n, n_split, H, n_heads), need = pr * (layout->head_dim + 2) * 4;
         if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need))
@@ -299,7 +299,7 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
                 a.part_o = (float *)workspace + at * layout->head_dim;
                 a.part_ml = (float *)workspace + pr * layout->head_dim + at * 2;
             }
-            if ((st = launched(launch_attend(a, e, f32, sm_quota, (cudaStream_t)stream))) != EBRL_OK) return st;
+            if ((st = launched(launch_attend(a, e, f32, sm_quota, sms, (cudaStream_t)stream))) != EBRL_OK) return st;
             if (n_split > 1 && (st = launched(launch_attend_join(a, e, f32, sm_quota, sms, (cudaStream_t)stream))) != EBRL_OK) return st;
         }
         return EBRL_OK;

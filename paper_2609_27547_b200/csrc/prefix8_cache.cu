@@ -329,9 +329,8 @@ cudaError_t launch_evict(const EvictArgs &a, const EvictEnvs &e, int max_keep, i
     if (err != cudaSuccess) return err;
     const int chunks = (max_keep + 8 * BLOCK - 1) / (8 * BLOCK);
     const long long heads = (long long)e.n * a.rec.kv_layers * 2 * a.rec.kvh;
-    // in place the chunks of a head are one CTA's, in order; otherwise enough parts to fill the chip
-    long long part = a.src == a.dst ? 1 : (4LL * n_sms + heads - 1) / heads;
-    if (part > chunks) part = chunks;
+    // in place the chunks of a head are one CTA's, in order; otherwise each is a CTA's
+    const long long part = a.src == a.dst ? 1 : chunks;
     const long long items = heads * part, cap = grid ? grid : 1 << 20;
     const int g2 = (int)(items < cap ? items : cap);
     switch (a.rec.hd) {

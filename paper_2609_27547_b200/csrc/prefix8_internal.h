@@ -59,11 +59,11 @@ struct WeighArgs {
     int accumulate;
 };
 
-// Query rows (H * G) per tile: 8, 16 or 32.
+// Query rows (H * G) per tile: 8, 16 or 32 (attend may take smaller ones).
 inline int row_tile(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32); }
 int attend_warps(int rows, bool f32);     // items (one warp each) that an SM holds
 // grid = CTAs of a persistent grid (an SM quota), 0: as many small CTAs as there are items
-cudaError_t launch_attend(const AttendArgs &a, const Envs &e, bool f32, int grid, cudaStream_t st);
+cudaError_t launch_attend(const AttendArgs &a, const Envs &e, bool f32, int grid, int sms, cudaStream_t st);
 cudaError_t launch_attend_join(const AttendArgs &a, const Envs &e, bool f32, int grid, int n_sms, cudaStream_t st);
 cudaError_t launch_weigh(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st);
 

@@ -116,7 +116,7 @@ _HERE = contextlib.nullcontext()
 
 def _on(device: torch.device):
     """Makes a device current for the call (nothing when it already is)."""
-    now = torch.cuda.current_device()
+    now = torch._C._cuda_getDevice()      # (there is a CUDA tensor: the runtime is up)
     return _HERE if now == device.index else _moved(device.index, now)
 
 
@@ -152,6 +152,13 @@ def layout_for(cfg) -> Layout:
     return Layout(max(cfg.kv_layers, 1), cfg.n_heads, cfg.d // cfg.n_heads, cfg.max_prefix_len)
 
 
+def _addresses(base: int, step: int, n: int):
+    """n addresses, `step` bytes apart, as a C array."""
+    if n <= 16:
+        return (C.c_void_p * n)(*[base + i * step for i in range(n)])
+    return (C.c_void_p * n).from_buffer(np.arange(n, dtype=np.int64) * step + base)
+
+
 def new_pool(layout: Layout, n_slots: int, device="cuda") -> torch.Tensor:
     """A zeroed pool of ``n_slots`` records."""
     if layout.record_bytes == 0:
@@ -184,7 +191,8 @@ def quantize(layout: Layout, pool: torch.Tensor, planes: Planes, lens=None, *, s
     if n == 0:
         return
     d = layout.n_kv_heads * layout.head_dim
-    dt, rs, rows = views_[0].dtype, None, []
+    dt, rows = views_[0].dtype, []
+    rs = next((x.stride(-2) for x in views_ if x.dim() >= 2 and x.shape[-2] > 1), d)   # (one row has no distance to the next)
     if dt not in _DTYPES:
         raise TypeError("planes must be bf16 or fp32, not %s" % dt)
     for x in views_:
@@ -196,46 +204,45 @@ def quantize(layout: Layout, pool: torch.Tensor, planes: Planes, lens=None, *, s
         P = sh[2]
         if d > 1 and sd[3] != 1:
             raise ValueError("columns must be contiguous")
-        r = sd[2] if P > 1 else (rs or d)
-        if rs is None:
-            rs = r
+        r = sd[2] if P > 1 else rs
         plane = sd[1]     # the distance of the planes, in whole rows
         if r != rs or r < d or plane % rs or plane < P * rs or (layout.kv_layers > 1 and sd[0] != 2 * plane):
             raise ValueError("planes must share one row stride and lie a whole number of rows apart")
         rows.append(plane // rs)
     if whole:
-        ptrs = np.arange(n, dtype=np.int64) * (planes.stride(0) * planes.element_size()) + planes.data_ptr()
-        rows = np.full(n, rows[0], dtype=np.int32)
+        limit = [P] * n
+        ptrs = _addresses(planes.data_ptr(), planes.stride(0) * planes.element_size(), n)
+        rows = (C.c_int32 * n)(*rows * n)
     else:
-        ptrs = np.array([x.data_ptr() for x in views_], dtype=np.int64)
-        rows = np.array(rows, dtype=np.int32)
+        limit = [x.shape[2] for x in views_]
+        ptrs = (C.c_void_p * n)(*[x.data_ptr() for x in views_])
+        rows = (C.c_int32 * n)(*rows)
     _same_device(pool, *views_)
-    limit = np.full(n, planes.shape[3], dtype=np.int32) if whole else np.array([x.shape[2] for x in views_], dtype=np.int32)
-    L = _host(torch.from_numpy(limit) if lens is None else lens, "lens")
+    L = _host(limit if lens is None else lens, "lens")
     if L.numel() != n:
         raise ValueError("%d lengths for %d environments" % (L.numel(), n))
-    if (L.numpy() > limit).any():
+    given = L.tolist()
+    if max(given) > limit[0] if whole else any(a > b for a, b in zip(given, limit)):
         raise ValueError("a length exceeds its planes")
     mp, masks = None, []
     if mask is not None:
         masks = list(mask) if not torch.is_tensor(mask) else [mask]
         if torch.is_tensor(mask):
-            if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < int(L.max()) or (mask.shape[1] > 1 and mask.stride(1) != 1):
+            if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < max(given) or (mask.shape[1] > 1 and mask.stride(1) != 1):
                 raise ValueError("mask must be [n, >= P] with contiguous rows")
-            addr = np.arange(n, dtype=np.int64) * mask.stride(0) + mask.data_ptr()
+            mp = _addresses(mask.data_ptr(), mask.stride(0), n)
         else:
-            if len(masks) != n or any(m is not None and (m.dim() != 1 or m.numel() < k or (m.numel() > 1 and m.stride(0) != 1)) for m, k in zip(masks, L.tolist())):
+            if len(masks) != n or any(m is not None and (m.dim() != 1 or m.numel() < k or (m.numel() > 1 and m.stride(0) != 1)) for m, k in zip(masks, given)):
                 raise ValueError("masks must be n contiguous tensors [>= P_i] or None")
-            addr = np.array([m.data_ptr() if m is not None else 0 for m in masks], dtype=np.int64)
+            mp = (C.c_void_p * n)(*[m.data_ptr() if m is not None else None for m in masks])
         if any(m is not None and m.dtype not in (torch.uint8, torch.bool) for m in masks):
             raise TypeError("masks must be uint8 or bool")
         _same_device(pool, *masks)
-        mp = addr.ctypes.data
     s, sp = _n_slots(L, slots, pool)
     with _on(pool.device):
         st = _stream(pool.device, stream, pool, *views_, *masks)
-        _check(_load().ebrl_prefix8_quantize(cl, pool.data_ptr(), pool.shape[0], n, sp, ptrs.ctypes.data, L.data_ptr(),
-                                             rows.ctypes.data, rs, _DTYPES[dt], mp, int(sm_quota), st))
+        _check(_load().ebrl_prefix8_quantize(cl, pool.data_ptr(), pool.shape[0], n, sp, ptrs, L.data_ptr(),
+                                             rows, rs, _DTYPES[dt], mp, int(sm_quota), st))
 
 
 def _queries(layout: Layout, pool: torch.Tensor, q: torch.Tensor, lens, what: str = "q"):
@@ -328,7 +335,7 @@ def evict(layout: Layout, src: torch.Tensor, dst: torch.Tensor, weight: torch.Te
     if K.numel() != n:
         raise ValueError("%d numbers to keep for %d environments" % (K.numel(), n))
     new = torch.minimum(L, K)
-    most = int(new.max()) if n else 0
+    most = max(new.tolist(), default=0)
     ws = _weights(layout, src, weight, "weight")
     wo = 0 if weight_out is None else _weights(layout, src, weight_out, "weight_out")
     if kept is None:
