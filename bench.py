@@ -84,6 +84,7 @@ def parse_args(argv=None):
                          "group-level batching and under step-level continuous batching")
     ap.add_argument("--min-warmup", type=int, default=3, help="lower bound on warm-up steps (profiling captures use 1)")
     ap.add_argument("--d-ctx", type=int, default=0, help="variant: prefixes are hidden states [P][d_ctx], projected to K/V per layer")
+    ap.add_argument("--kv8", action="store_true", help="variant: prefixes are 8-bit records (e4m3 codes, a scale per 32 tokens and head)")
     ap.add_argument("--inflight", type=int, default=16, help="groups queued before a batch is launched")
     ap.add_argument("--fused", action="store_true",
                     help="run every batch through the persistent step kernel (one resident grid for all Euler steps)")
@@ -356,15 +357,26 @@ def run_ours(args, emit=True):
     inflight = args.inflight
     flags = (B.FLAG_FORCE_SIMT if args.simt else 0) | (B.FLAG_GREEN_CTX if args.green_ctx else 0) | \
         (B.FLAG_FORCE_FUSED if args.fused else 0)
-    cfg = B.cfg_for(w, max_group_envs=max(len(g) for g in groups), max_inflight_groups=inflight, flags=flags, device=local)
+    cfg = B.cfg_for(w, max_group_envs=max(len(g) for g in groups), max_inflight_groups=inflight, flags=flags, device=local,
+                    kv_dtype=B.E4M3 if args.kv8 else None)
     gen = B.ActGen(cfg, wt)
     stream = torch.cuda.Stream(dev)
+    prefix = {e: envs[e].kv for e in ids}
+    if args.kv8:
+        from paper_2609_27547_b200 import prefix8
+        lay = prefix8.layout_for(cfg)
+        pool = prefix8.new_pool(lay, len(ids), dev)
+        prefix8.quantize(lay, pool, [envs[e].kv for e in ids])
+        prefix = {e: pool[i] for i, e in enumerate(ids)}
+        kv_bytes = pool.numel()
+        for e in ids:
+            envs[e].kv = None
 
     def step():
         for g in groups:
             lo = pos[g[0]]
-            gen.submit(g, [envs[e].kv for e in g], noise[lo:lo + len(g)], out[lo:lo + len(g)], sm_quota=quota,
-                       stream=stream, step_index=[envs[e].step for e in g])
+            gen.submit(g, [prefix[e] for e in g], noise[lo:lo + len(g)], out[lo:lo + len(g)], sm_quota=quota,
+                       stream=stream, prefix_len=[envs[e].P for e in g] if args.kv8 else None, step_index=[envs[e].step for e in g])
         gen.sync()
 
     n_warm = max(args.min_warmup, args.warmup)
@@ -494,13 +506,14 @@ def run_ours(args, emit=True):
     if not args.no_e2e:
         h_noise = noise.cpu().pin_memory()
         h_out = torch.empty_like(h_noise).pin_memory()
-        h_kv = {e: envs[e].kv.cpu().pin_memory() for e in ids}
+        h_kv = {e: prefix[e].cpu().pin_memory() for e in ids}
 
         def step_host():
             for g in groups:
                 lo = pos[g[0]]
                 gen.submit_host(g, [h_kv[e] for e in g], h_noise[lo:lo + len(g)], h_out[lo:lo + len(g)], sm_quota=quota,
-                                stream=stream, step_index=[envs[e].step for e in g])
+                                stream=stream, prefix_len=[envs[e].P for e in g] if args.kv8 else None,
+                                step_index=[envs[e].step for e in g])
             gen.sync()
 
         n_e2e = max(1, min(args.steps, 3))
@@ -533,7 +546,7 @@ def run_ours(args, emit=True):
             "ms_per_step": ms_step, "higher_is_better": True, "scaling": "weak", "vs_baseline": None,
             "dtype": "bf16" if bf16 else "f32", "data": "synthetic",
             "config": {"workload": synth.workload_label(args.config), "envs_per_gpu": w.B, "H": w.H, "A": w.A, "d": w.d,
-                       "L": w.L, "heads": w.n_heads, "P": list(w.P), "K": w.K, "d_ctx": w.d_ctx, "groups": len(groups),
+                       "L": w.L, "heads": w.n_heads, "P": list(w.P), "K": w.K, "d_ctx": w.d_ctx, "prefix": "8-bit records" if args.kv8 else w.dtype, "groups": len(groups),
                        "group_sizes": [min(map(len, groups)), max(map(len, groups))], "sm_quota": q_eff,
                        "inflight_groups": inflight, "corunner": co_report if co_report is not None else False,
                        "kernels": "persistent step kernel" if args.fused else ("plain ALU" if args.simt else "one kernel per operation"),

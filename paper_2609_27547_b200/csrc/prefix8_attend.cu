@@ -34,7 +34,7 @@ namespace p8 {
 
 template <int HD, int NT, bool F32> struct AttendCfg {
     // per SM: as many as their registers allow (168 a thread at 12, 255 at 8)
-    static constexpr int WARPS = NT == 4 ? (F32 && HD == 128 ? 6 : 8) : (NT == 2 ? (HD == 128 || F32 ? 8 : 12) : (HD == 128 || F32 ? 12 : 16));
+    static constexpr int WARPS = NT == 4 ? (F32 && HD == 128 ? 6 : 8) : (NT == 2 ? (HD == 128 || F32 ? 8 : 12) : (HD == 128 ? 12 : 16));
     static constexpr int TILE = BLOCK * HD;
     // queries in shared memory where registers hold the outputs of 32 rows, or of 16 beside two f16 terms: per warp
     static constexpr bool QS = NT == 4 || (NT == 2 && F32);
@@ -349,13 +349,13 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
     }
 }
 
-// Joins the pieces of long prefixes: one CTA per query row, the pieces divided over its eight warps, sums in warp order.
+// Joins the pieces of long prefixes: one CTA per query row, the pieces divided over its sixteen warps, sums in warp order.
 // Traffic is the pieces' results only (1 / 64 of the cache at 896-token pieces and 4 rows).
 template <int HD, bool F32>
-__global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs ev)
+__global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs ev)
 {
     constexpr int V = HD / 32;
-    __shared__ float so[8][HD], sl[8];
+    __shared__ float so[16][HD], sl[16];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, RH = a.r.H * a.r.heads;
     const long long rows = (long long)ev.n * RH;
     pdl_launch_dependents();
@@ -371,8 +371,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
         float acc[V], L = 0.f;
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = 0.f;
-#pragma unroll 4
-        for (int p = warp; p < np; p += 8) {
+#pragma unroll 8
+        for (int p = warp; p < np; p += 16) {
             const float2 u = ml[(size_t)p * RH];
             const float f = ex2(u.x - M);
             L = fmaf(f, u.y, L);
@@ -386,7 +386,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
         if (threadIdx.x < HD) {
             float s = 0.f, z = 0.f;
 #pragma unroll
-            for (int w = 0; w < 8; ++w) { s += so[w][threadIdx.x]; z += sl[w]; }
+            for (int w = 0; w < 16; ++w) { s += so[w][threadIdx.x]; z += sl[w]; }
             const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + threadIdx.x;
             const float v = z == 0.f ? 0.f : s / z;
             if constexpr (F32) ((float *)a.out)[off] = v;
@@ -457,10 +457,14 @@ cudaError_t launch_attend_join(const AttendArgs &a, const Envs &e, bool f32, int
     const long long cap = grid ? grid : (long long)n_sms * 8;
     const int g = (int)(rows < cap ? rows : cap);
     if (g == 0) return cudaSuccess;
+    struct Early {   // the join may be set up while the last pieces are being worked on; it waits for them itself
+        Early() { pdl_set(true); }
+        ~Early() { pdl_set(false); }
+    } early;
     switch (a.r.rec.hd) {
-    case 128: return f32 ? launch_kernel(attend_join_kernel<128, true>, g, 256, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<128, false>, g, 256, 0, st, 1, a, e);
-    case 64: return f32 ? launch_kernel(attend_join_kernel<64, true>, g, 256, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<64, false>, g, 256, 0, st, 1, a, e);
-    default: return f32 ? launch_kernel(attend_join_kernel<32, true>, g, 256, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<32, false>, g, 256, 0, st, 1, a, e);
+    case 128: return f32 ? launch_kernel(attend_join_kernel<128, true>, g, 512, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<128, false>, g, 512, 0, st, 1, a, e);
+    case 64: return f32 ? launch_kernel(attend_join_kernel<64, true>, g, 512, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<64, false>, g, 512, 0, st, 1, a, e);
+    default: return f32 ? launch_kernel(attend_join_kernel<32, true>, g, 512, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<32, false>, g, 512, 0, st, 1, a, e);
     }
 }
 

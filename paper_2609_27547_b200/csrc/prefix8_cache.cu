@@ -2,6 +2,7 @@
 #include "prefix8_internal.h"
 #include "rowops.cuh"
 
+#include <cuda_fp16.h>
 #include <math.h>
 
 namespace ebrl {
@@ -25,6 +26,28 @@ __device__ __forceinline__ uint32_t narrow2(float a, float b)
     uint16_t r;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(b), "f"(a));
     return r;
+}
+// Two e4m3 codes as f16, one code's value, two codes' values.
+__device__ __forceinline__ uint32_t code_half2(uint32_t two)
+{
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((uint16_t)two));
+    return r;
+}
+__device__ __forceinline__ float2 code_pair(uint32_t two)
+{
+    const uint32_t r = code_half2(two);
+    return __half22float2(*reinterpret_cast<const __half2 *>(&r));
+}
+__device__ __forceinline__ float code_value(uint32_t c) { return code_pair(c).x; }
+// Two codes times a power of two, as codes; NaN stays NaN.
+__device__ __forceinline__ uint32_t times2(uint32_t two, __half2 f)
+{
+    const uint32_t r = code_half2(two);
+    const __half2 p = __hmul2(*reinterpret_cast<const __half2 *>(&r), f);
+    uint16_t o;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(o) : "r"(*reinterpret_cast<const uint32_t *>(&p)));
+    return o;
 }
 __device__ __forceinline__ float finite_abs(float x)
 {
@@ -235,7 +258,7 @@ __global__ void __launch_bounds__(1024) select_kernel(const __grid_constant__ Ev
 // the rows being written.  Otherwise the chunks are spread over n_part CTAs.
 // Bound: HBM, 2 bytes per kept code.
 template <int HD>
-__global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ EvictEnvs ev, int n_part)
+__global__ void __launch_bounds__(256, 4) gather_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ EvictEnvs ev, int n_part)
 {
     constexpr int LPR = HD / 16, RPI = 32 / LPR, N = 32 / RPI;   // lanes per row, rows per load, loads per lane
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -267,29 +290,40 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Evi
                 }
             }
             float amax = 0.f;
-            uint32_t nan = 0;
+            bool nan = false;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                // codes without their sign are ordered like their values; 0x7f is NaN and does not count
+                // codes without their sign are ordered like their values, 0x7f (NaN) above all; two codes are compared in one instruction
                 const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-                uint32_t m = 0;
+                uint32_t even = 0, odd = 0;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t c = w[j] & 0x7f7f7f7fu, n = __vcmpeq4(c, 0x7f7f7f7fu);
-                    nan |= n;
-                    m = __vmaxu4(m, c & ~n);
+                for (int j = 0; j < 4; ++j) { even = __vmaxu2(even, w[j] & 0x007f007fu); odd = __vmaxu2(odd, w[j] & 0x7f007f00u); }
+                const uint32_t m = __vmaxu2(even, odd >> 8), top = max(m & 0xffffu, m >> 16);
+                nan |= top == 0x7fu;
+                amax = fmaxf(amax, finite_abs(code_value(top) * sc[i]));
+            }
+            const bool any_nan = __any_sync(0xffffffffu, nan);
+            if (any_nan) {   // the largest of the others
+                amax = 0.f;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+                    for (int j = 0; j < 16; ++j) {
+                        const uint32_t c = (w[j >> 2] >> (8 * (j & 3))) & 0x7fu;
+                        if (c != 0x7fu) amax = fmaxf(amax, finite_abs(code_value(c) * sc[i]));
+                    }
                 }
-                m = __vmaxu4(m, m >> 16);
-                const uint32_t top = max(m & 0xffu, (m >> 8) & 0xffu);
-                uint32_t f2;
-                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f2) : "h"((uint16_t)top));
-                float f;
-                asm("{.reg .f16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.f32.f16 %0, l;}" : "=f"(f) : "r"(f2));
-                amax = fmaxf(amax, finite_abs(f * sc[i]));
             }
             amax = warp_max(amax);
             const float s = block_scale(amax), inv = 1.f / s;
-            const bool any_nan = __any_sync(0xffffffffu, nan != 0);
+            // whether every row changes its scale by a power of two that f16 holds
+            bool fine = true;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float by = sc[i] * inv;
+                fine &= sc[i] == 0.f || ((__float_as_uint(by) & 0x007fffffu) == 0 && by >= 1.f / 16384.f && by <= 16384.f);
+            }
+            fine = __all_sync(0xffffffffu, fine);
             __syncthreads();   // every block of the chunk has been read
             if (b0 < keep) {
                 char *dst = a.dst + head_off;
@@ -300,18 +334,23 @@ __global__ void __launch_bounds__(256) gather_kernel(const __grid_constant__ Evi
                     if (row < keep) {
                         const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
                         uint32_t o[4];
+                        const float by = sc[i] * inv;
+                        if (fine) {
+                            // codes are f16 values, a power of two of one is, too (or far below the smallest code)
+                            const __half2 f = __float2half2_rn(by);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            uint32_t r = 0;
+                            for (int j = 0; j < 4; ++j) o[j] = times2(w[j], f) | times2(w[j] >> 16, f) << 16;
+                        } else {
 #pragma unroll
-                            for (int q = 0; q < 2; ++q) {
-                                uint32_t f2;
-                                asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(f2) : "h"((uint16_t)(w[j] >> (16 * q))));
-                                float lo, hi;
-                                asm("{.reg .f16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;}" : "=f"(lo), "=f"(hi) : "r"(f2));
-                                r |= narrow2(lo * sc[i] * inv, hi * sc[i] * inv) << (16 * q);
+                            for (int j = 0; j < 4; ++j) {
+                                uint32_t r = 0;
+#pragma unroll
+                                for (int q = 0; q < 2; ++q) {
+                                    const float2 f = code_pair((w[j] >> (16 * q)) & 0xffffu);
+                                    r |= narrow2(f.x * sc[i] * inv, f.y * sc[i] * inv) << (16 * q);
+                                }
+                                o[j] = r;
                             }
-                            o[j] = r;
                         }
                         *reinterpret_cast<uint4 *>(dst + (size_t)row * HD + (lane % LPR) * 16) = make_uint4(o[0], o[1], o[2], o[3]);
                     }

@@ -4,10 +4,10 @@
 // attention's own traffic; gathering the weights inside attention would need either the scores of all heads in memory
 // (16 rows x 4 B per token and head against 128 B of codes) or atomics across heads, whose order changes the last bits.
 //
-// A CTA owns 128 x TW tokens of one environment and walks every (key/value head, row tile): its eight warps are HW
+// A CTA owns 256 x TW tokens of one environment and walks every (key/value head, row tile): its eight warps are HW
 // parallel heads x TW token groups (HW = 8 with eight heads or more).  A warp keeps its head's queries in registers for
-// four tiles -- the query rows then cost a quarter of the keys' L2 traffic at 16 rows -- and the weights of its 128 tokens
-// in 16 registers per lane over all of its heads.  Only at the end are they summed over the lanes of a quad and, in
+// eight tiles -- the query rows then cost an eighth of the keys' L2 traffic at 16 rows -- and the weights of its 256 tokens
+// in 32 registers per lane over all of its heads.  Only at the end are they summed over the lanes of a quad and, in
 // warp order, over the parallel heads: a fixed order, no atomics.  The key tiles of a warp's heads are one stream through a
 // ring of cp.async slots, so the ring stays full across heads.
 #include "prefix8_tile.cuh"
@@ -16,8 +16,9 @@ namespace ebrl {
 namespace p8 {
 
 template <int HD, int NT, bool F32> struct WeighCfg {
-    static constexpr int TILE = BLOCK * HD, RING = HD == 32 ? 8192 : 12288, SLOTS = RING / TILE;
-    static constexpr int CTAS = (NT == 4 || F32) ? 1 : 2;
+    // tiles per warp (8 against 4: 107 -> 95 us on 256 x 734 tokens x 16 heads x 16 rows; 16 spill), CTAs per SM
+    static constexpr int TT = 8, CTAS = (NT == 4 || F32) ? 1 : 2;
+    static constexpr int TILE = BLOCK * HD, RING = HD == 32 ? 8192 : (CTAS == 2 ? 12288 : 24576), SLOTS = RING / TILE < 8 ? RING / TILE : 8;
     static constexpr int SMEM = 8 * RING;
 };
 
@@ -26,8 +27,9 @@ __global__ void __launch_bounds__(256, WeighCfg<HD, NT, F32>::CTAS)
 weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs ev, int hw_log2, int n_chunk)
 {
     using C = WeighCfg<HD, NT, F32>;
+    constexpr int TOK = C::TT * BLOCK;   // tokens per warp
     extern __shared__ __align__(128) char smem[];
-    __shared__ float red[8][128];
+    __shared__ float red[8][C::TT * BLOCK];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t ring_u = ptx::smem_u32(smem + (size_t)warp * C::RING);
     const int G = a.r.G, R = a.r.H * G, RT = (R + NT * 8 - 1) / (NT * 8), kvh = a.r.rec.kvh, units = kvh * RT;
@@ -50,10 +52,10 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
             len = ev.len[env];
             wp = a.weight + (size_t)ev.slot[env] * a.stride;
         }
-        const int c0 = chunk * TW * 128;                     // first token of the CTA
+        const int c0 = chunk * TW * TOK;                     // first token of the CTA
         if (c0 >= len || !wp) continue;                      // (the same for the whole CTA)
-        const int b0 = c0 + tw * 128;                        // ... and of the warp
-        const int live = b0 >= len ? 0 : min(4, (len - b0 + BLOCK - 1) / BLOCK);
+        const int b0 = c0 + tw * TOK;                        // ... and of the warp
+        const int live = b0 >= len ? 0 : min(C::TT, (len - b0 + BLOCK - 1) / BLOCK);
         const int mine = hw < units ? (units - hw + HW - 1) >> hw_log2 : 0;   // this warp's (head, row tile) units: hw, hw + HW, ...
         const int loads = mine * live;
         // load j of the warp's stream: tile j % live of its unit j / live
@@ -75,9 +77,9 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
             const int v = len - b0 - lane * BLOCK;
             if (v < BLOCK) seen &= (1u << v) - 1u;
         }
-        float acc[4][2][2];
+        float acc[C::TT][2][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < C::TT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) acc[i][h][0] = acc[i][h][1] = 0.f;
 
@@ -87,6 +89,16 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
             const int unit = hw + u * HW, kh = unit / RT, rt = unit - kh * RT;
             uint32_t q[NT][HD / 16][QW<F32>];
             float fr[NT][2], ls[NT][2];
+            if (u + 1 < mine) {   // the next unit's queries on their way into L1
+                constexpr int LINES = HD * (F32 ? 4 : 2) / 128 > 0 ? HD * (F32 ? 4 : 2) / 128 : 1;   // 128-byte lines of a row
+                const int un = unit + HW, kn = un / RT, rn = un - kn * RT;
+#pragma unroll
+                for (int i = lane; i < NT * 8 * LINES; i += 32) {
+                    const int r = rn * NT * 8 + i / LINES, tok = r / G;
+                    const size_t off = (size_t)env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)(kn * G + r - tok * G) * HD;
+                    if (r < R) prefetch_l1((const char *)a.r.q + off * (F32 ? 4 : 2) + (i % LINES) * 128);
+                }
+            }
             const float ks_l = lane < live ? read_scale(reinterpret_cast<const float *>(rec + a.r.rec.head_scales(a.r.layer, 0, kh))[b0 / BLOCK + lane]) : 0.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
@@ -104,7 +116,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < C::TT; ++i) {
                 if (i < live) {
                     const float ks = __shfl_sync(FULL, ks_l, i);
                     cp_wait<C::SLOTS - 2>();
@@ -135,7 +147,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
         cp_wait<0>();
         // over the quad's row pairs, then over the parallel heads
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < C::TT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -148,11 +160,11 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                     if (t == 0) red[warp][i * 32 + tok] = (m >> tok) & 1 ? v : 0.f;
                 }
         __syncthreads();
-        for (int k = threadIdx.x; k < TW * 128; k += 256) {
-            const int tok = c0 + k, first = (k >> 7) << hw_log2;
+        for (int k = threadIdx.x; k < TW * TOK; k += 256) {
+            const int tok = c0 + k, first = k / TOK << hw_log2;
             if (tok < len) {
                 float v = 0.f;
-                for (int h = 0; h < HW; ++h) v += red[first + h][k & 127];
+                for (int h = 0; h < HW; ++h) v += red[first + h][k % TOK];
                 wp[tok] = a.accumulate ? wp[tok] + v : v;
             }
         }
@@ -175,7 +187,7 @@ template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Env
     }
     const int units = a.r.rec.kvh * ((a.r.H * a.r.G + NT * 8 - 1) / (NT * 8));
     const int hw = units >= 8 ? 3 : (units >= 4 ? 2 : (units >= 2 ? 1 : 0));
-    const int n_chunk = (max_len + (128 << (3 - hw)) - 1) / (128 << (3 - hw));
+    const int n_chunk = (max_len + (C::TT * BLOCK << (3 - hw)) - 1) / (C::TT * BLOCK << (3 - hw));
     const long long items = (long long)(a.r.meta ? a.r.n_envs : e.n) * n_chunk, cap = grid ? grid : 1 << 20;
     if (items == 0) return cudaSuccess;
     return launch_kernel(weigh_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), 256, (size_t)C::SMEM, st, 1, a, e, hw, n_chunk);
