@@ -143,7 +143,8 @@ int longest(const int32_t *len, int n)
 // How prefixes are cut: tokens per piece and pieces of the longest prefix.  Left to itself, a call is cut only when its
 // (environment, head, row tile) items are at most half of the warps that the SMs hold, into as many pieces as there
 // are warps for (never more: a second wave would double the time) and not below 256 tokens.
-// Measured on two 65 k-token prefixes with 4 heads: whole 2.4 ms, pieces of 2048 36 us, this rule (896) 29 us.
+// Measured on two 65 k-token prefixes with 4 heads: whole 1394 us, pieces of 8192 tokens 193 us, 2048 58 us, 512 35 us,
+// 384 (this rule) 33 us, 256 41 us, 128 48 us.
 void cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int heads, int asked, int sms, bool f32, int *split, int *n_split)
 {
     const int most = longest(len, n);
@@ -157,12 +158,13 @@ void cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int h
     long long items = 0;
     for (int i = 0; i < n; ++i) items += len[i] > 0;
     const int rows = H * (heads / l.n_kv_heads);
-    items *= (long long)l.n_kv_heads * ((rows + 7) / 8);   // few items are taken in tiles of 8 rows
-    const long long warps = (long long)sms * attend_warps(8, f32);
+    const int tile = attend_tile(l.head_dim, rows, f32, most);
+    items *= (long long)l.n_kv_heads * ((rows + tile - 1) / tile);
+    const long long warps = (long long)sms * attend_warps(l.head_dim, tile);
     if (items == 0 || items * 2 > warps) return;
-    const long long parts = warps / items;
-    const long long piece = std::max(256LL, ((most + parts - 1) / parts + 127) / 128 * 128);
-    if (piece >= most) return;
+    const long long parts = std::min<long long>(warps / items, most / 256);
+    if (parts < 2) return;
+    const long long piece = ((most + parts - 1) / parts + 127) / 128 * 128;
     *split = (int)piece;
     *n_split = (int)((most + piece - 1) / piece);
 }
@@ -251,9 +253,12 @@ uint64_t ebrl_prefix8_attend_workspace(const ebrl_prefix8_layout_t *layout, int3
     if (check_layout(layout) != EBRL_OK || n <= 0 || !len || H < 1 || n_heads < 1 || n_heads % layout->n_kv_heads) return 0;
     int sms = 0, split, n_split;
     if (device_sms(0, &sms) != EBRL_OK) return 0;
-    // fp32 queries cut into at most as many pieces as bf16 ones
-    cut(*layout, n, len, H, n_heads, split_tokens, sm_quota > 0 ? std::min<int>(sm_quota, sms) : sms, false, &split, &n_split);
-    return part_rows(n, n_split, H, n_heads) * (layout->head_dim + 2) * 4;
+    uint64_t most = 0;   // of either query type
+    for (int f32 = 0; f32 < 2; ++f32) {
+        cut(*layout, n, len, H, n_heads, split_tokens, sm_quota > 0 ? std::min<int>(sm_quota, sms) : sms, f32 != 0, &split, &n_split);
+        most = std::max(most, part_rows(n, n_split, H, n_heads) * (layout->head_dim + 2) * 4);
+    }
+    return most;
 }
 
 ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const void *pool, int32_t n_slots, int32_t n, const int32_t *slots,
@@ -291,6 +296,7 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
         a.split = split; a.n_split = n_split;
         for (int first = 0; first < n; first += CHUNK_ENVS) {
             const Envs &e = some_envs(first, std::min(CHUNK_ENVS, n - first), slots, len);
+            a.max_len = longest(e.len, e.n);
             a.r.q = (const char *)q + first * q_env_stride * es;
             a.out = (char *)out + first * o_env_stride * es;
             a.lse = lse ? lse + (size_t)first * H * n_heads : nullptr;

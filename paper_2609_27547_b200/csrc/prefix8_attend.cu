@@ -1,20 +1,21 @@
 // Softmax attention over 8-bit prefix records (include/ebrl_prefix8.h): out = softmax(scale q k^T) v, k = code * scale.
 //
-// Bound: HBM.  Each code is read once and used by the 1 .. 32 query rows of a row tile, far left of the ridge even on mma.sync, so
+// Bound: HBM.  Each code is read once and used by the 1 .. 16 query rows of a row tile, far left of the ridge even on mma.sync, so
 // what counts is that bytes are always in flight and that a code costs few instructions.
 //
 //   Item = (environment, piece of its prefix, key/value head, row tile), worked on by ONE WARP: its own running softmax, its
 //   own ring of stages (a key and a value tile each) filled by cp.async, no barrier, no partial results to join unless a prefix is
 //   cut.  A record's head is contiguous, so a tile is one straight 4 KB run at head_dim 128.
-//   SMs hold 16 warps at 8 rows, 12 at 16, 8 at 32 (what registers allow); 130 - 190 KB of tiles are in flight per SM, three
-//   times what HBM latency asks for.  With all SMs to itself the launch is one CTA per item, which lets the hardware even out
-//   ragged prefixes; under an SM quota it is a persistent grid of `quota` CTAs that hold all of an SM's warps.
+//   At head_dim 128 SMs hold 12 warps at 8 rows and 8 at 16, at 64 they hold 16 and 12 (what registers allow); 96 - 130 KB of
+//   tiles are in flight per SM, twice what HBM latency asks for.  With all SMs to itself the launch is one CTA per item,
+//   which lets the hardware even out ragged prefixes; under an SM quota it is a persistent grid of `quota` CTAs that hold all of an SM's warps.
 //   (Four warps per item, joined in shared memory, were 1.6 times slower on 512 x 768 tokens x 16 heads: an item was
 //   over before its set-up and join were paid for.)
 //
-//   With the cache in L2 (arithmetic alone) 512 x 768 tokens x 16 heads of 128 take 143 us at 8 rows, 240 at 16, 460 at 32; from
-//   HBM 241 us (6.7 TB/s of codes), 296 (5.4) and 492.  Half of the cycles of the 16-row kernel are dependent-instruction waits
-//   at two warps per scheduler; removing any one kind of work (products, exponentials, conversions, transposes) saves 1 - 5 %.
+//   With the cache in L2 (arithmetic alone) 512 x 768 tokens x 16 heads of 128 take 143 us at 8 rows and 240 at 16; from HBM
+//   241 us (6.7 TB/s of codes) and 296 (5.4).  At 16 rows the legacy tensor path is what it waits for: a product occupies a
+//   quarter-SM for 9 cycles (64 a tile), fp32 instructions do not run beside it (conversions and exponentials do), and the
+//   sum of both is 740 of the 1300 cycles a tile takes.
 //
 //   Running maximum, lazily: a row's reference is raised only when a score exceeds it by 2^14 / 2^6; until then the weights
 //   2^(s - ref) stay below 2^14, which f16 holds with the same 11 bits.  The common tile needs one vote and no
@@ -23,7 +24,8 @@
 //   powers of two), and where they differ by more than 2^20 the block's product is scaled by itself.  Any finite scales work.
 //   fp32 queries always take the latter way: summed up in the tensor core over 16 tiles, outputs were 1.1e-6 off instead of 3.5e-7.
 //
-//   bf16 queries are exact (prefix8_tile.cuh), weights are rounded to f16: 11 bits, an eighth of the output's own rounding.  fp32 queries: queries and weights in two f16 terms each (22 bits).  Sums are fp32.
+//   bf16 queries are exact (prefix8_tile.cuh), weights are rounded to f16: 11 bits, an eighth of the output's own rounding.
+//   fp32 queries: queries and weights in two f16 terms each (22 bits).  Sums are fp32.
 #include "prefix8_tile.cuh"
 #include "rowops.cuh"
 
@@ -33,15 +35,12 @@ namespace ebrl {
 namespace p8 {
 
 template <int HD, int NT, bool F32> struct AttendCfg {
-    // per SM: as many as their registers allow (168 a thread at 12, 255 at 8)
-    static constexpr int WARPS = NT == 4 ? (F32 && HD == 128 ? 6 : 8) : (NT == 2 ? (HD == 128 || F32 ? 8 : 12) : (HD == 128 ? 12 : 16));
+    // per SM: as many as their registers allow (128 a thread at 16, 168 at 12, 255 at 8)
+    static constexpr int WARPS = HD == 128 ? (NT == 1 ? 12 : 8) : (NT == 1 ? 16 : 12);
     static constexpr int TILE = BLOCK * HD;
-    // queries in shared memory where registers hold the outputs of 32 rows, or of 16 beside two f16 terms: per warp
-    static constexpr bool QS = NT == 4 || (NT == 2 && F32);
-    static constexpr int QBYTES = QS ? HD / 16 * NT * 32 * 4 * QW<F32> : 0;
-    static constexpr int ROOM = (224 * 1024 / WARPS - QBYTES) / (2 * TILE);
+    static constexpr int ROOM = 224 * 1024 / WARPS / (2 * TILE);
     static constexpr int STAGES = ROOM < 4 ? ROOM : 4;                // 2 .. 4 pairs of a key and a value tile per warp
-    static constexpr int WARP_BYTES = STAGES * 2 * TILE + QBYTES;     // ring, queries
+    static constexpr int WARP_BYTES = STAGES * 2 * TILE;              // its ring
     static constexpr int PSTRIDE = HD + 4;                            // floats per staged output row
     static_assert(STAGES >= 2 && 8 * PSTRIDE * 4 <= STAGES * 2 * TILE, "ring");
 };
@@ -56,7 +55,6 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int g = lane >> 2, t = lane & 3;
     const uint32_t ring_u = ptx::smem_u32(smem + (size_t)warp * C::WARP_BYTES);
-    const uint32_t q_u = ring_u + C::STAGES * 2 * C::TILE;
     const int G = a.r.G, R = a.r.H * G, RT = (R + NT * 8 - 1) / (NT * 8), kvh = a.r.rec.kvh;
     const int n_envs = a.r.meta ? a.r.n_envs : ev.n;
     const long long items = (long long)n_envs * kvh * a.n_split * RT;
@@ -98,39 +96,20 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         for (int j = 0; j < C::STAGES - 1; ++j) issue(j);
 
         // queries
-        uint32_t q[C::QS ? 1 : NT][ST][QW<F32>];
+        uint32_t q[NT][ST][QW<F32>];
         float fr[NT][2];   // what takes a raw product of row 2t (+ 1) of column tile nt to a score in units of log 2 (times the key scale)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             const int r = rt * NT * 8 + nt * 8 + g, tok = r / G;
             const size_t off = (size_t)env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)(kh * G + r - tok * G) * HD;
             const void *p = F32 ? (const void *)((const float *)a.r.q + off) : (const void *)((const __nv_bfloat16 *)a.r.q + off);
-            uint32_t b[ST][QW<F32>];
-            const float f = load_q<HD, F32>(p, r < R, a.r.scale < 0.f, t, b) * (fabsf(a.r.scale) * LOG2E);
+            const float f = load_q<HD, F32>(p, r < R, a.r.scale < 0.f, t, q[nt]) * (fabsf(a.r.scale) * LOG2E);
             fr[nt][0] = __shfl_sync(FULL, f, 8 * t);
             fr[nt][1] = __shfl_sync(FULL, f, 8 * t + 4);
-#pragma unroll
-            for (int st = 0; st < ST; ++st) {
-                if constexpr (C::QS) {
-                    const uint32_t at = q_u + (uint32_t)(((st * NT + nt) * 32 + lane) * 4 * QW<F32>);
-                    if constexpr (F32) sts128(at, b[st][0], b[st][1], b[st][2], b[st][3]);
-                    else sts64(at, b[st][0], b[st][1]);
-                } else {
-#pragma unroll
-                    for (int c = 0; c < QW<F32>; ++c) q[nt][st][c] = b[st][c];
-                }
-            }
         }
-        // (a lane reads back from shared memory what it wrote itself)
         auto query = [&](int st, int nt, uint32_t *w) {
-            if constexpr (C::QS) {
-                const uint32_t at = q_u + (uint32_t)(((st * NT + nt) * 32 + lane) * 4 * QW<F32>);
-                if constexpr (F32) { const uint4 u = lds128(at); w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w; }
-                else { const uint2 u = lds64(at); w[0] = u.x; w[1] = u.y; }
-            } else {
 #pragma unroll
-                for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
-            }
+            for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
         };
 
         float o[MT][NT][4];   // column m * 16 + g of rows 2t, 2t + 1, column + 8 of the same; in units of `unit`
@@ -171,19 +150,10 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
             if (mk) {
                 uint32_t pb[2][NT][2], pl[F32 ? 2 : 1][NT][2];
                 float s[2][NT][4];
-                if constexpr (NT <= 2) {
-                    KeyWords<HD> kw[2];
-                    kw[0].load(kslot, koff, 0);
-                    kw[1].load(kslot, koff, 1);
-                    score<HD, NT, F32, 2>(s, kw, query);
-                } else {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        KeyWords<HD> kw;
-                        kw.load(kslot, koff, h);
-                        score<HD, NT, F32, 1>(s + h, &kw, query);
-                    }
-                }
+                KeyWords<HD> kw[2];
+                kw[0].load(kslot, koff, 0);
+                kw[1].load(kslot, koff, 1);
+                score<HD, NT, F32, 2>(s, kw, query);
                 const bool hides = mk != FULL;
                 if (hides) {
 #pragma unroll
@@ -349,20 +319,23 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
     }
 }
 
-// Joins the pieces of long prefixes: one CTA per query row, the pieces divided over its sixteen warps, sums in warp order.
-// Traffic is the pieces' results only (1 / 64 of the cache at 896-token pieces and 4 rows).
-template <int HD, bool F32>
+// Joins the pieces of long prefixes: WPR warps per query row (16 where there are many pieces: latency; 1 where there are few: rows),
+// the pieces divided over them, sums in warp order.  Traffic is the pieces' results only (1 / 32 of the cache at 384-token pieces and
+// 4 rows).
+template <int HD, bool F32, int WPR>
 __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs ev)
 {
-    constexpr int V = HD / 32;
+    constexpr int V = HD / 32, RPC = 16 / WPR;
     __shared__ float so[16][HD], sl[16];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, RH = a.r.H * a.r.heads;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, RH = a.r.H * a.r.heads, sub = warp % WPR;
     const long long rows = (long long)ev.n * RH;
     pdl_launch_dependents();
     pdl_wait();
-    for (long long row = blockIdx.x; row < rows; row += gridDim.x) {
-        const int env = (int)(row / RH), rr = (int)(row - (long long)env * RH), tok = rr / a.r.heads, head = rr - tok * a.r.heads;
-        const int np = max(1, (ev.len[env] + a.split - 1) / a.split);
+    for (long long row0 = (long long)blockIdx.x * RPC; row0 < rows; row0 += (long long)gridDim.x * RPC) {
+        const long long row = row0 + warp / WPR;
+        const bool there = row < rows;
+        const int env = there ? (int)(row / RH) : 0, rr = there ? (int)(row - (long long)env * RH) : 0, tok = rr / a.r.heads, head = rr - tok * a.r.heads;
+        const int np = there ? max(1, (ev.len[env] + a.split - 1) / a.split) : 0;
         const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (size_t)env * a.n_split * RH + rr;
         const float *po = a.part_o + ((size_t)env * a.n_split * RH + rr) * HD + lane * V;
         float M = -FLT_MAX;
@@ -372,50 +345,66 @@ __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant_
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = 0.f;
 #pragma unroll 8
-        for (int p = warp; p < np; p += 16) {
+        for (int p = sub; p < np; p += WPR) {
             const float2 u = ml[(size_t)p * RH];
             const float f = ex2(u.x - M);
             L = fmaf(f, u.y, L);
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[i] = fmaf(f, po[(size_t)p * RH * HD + i], acc[i]);
         }
-#pragma unroll
-        for (int i = 0; i < V; ++i) so[warp][lane * V + i] = acc[i];
-        if (lane == 0) sl[warp] = L;
-        __syncthreads();
-        if (threadIdx.x < HD) {
-            float s = 0.f, z = 0.f;
-#pragma unroll
-            for (int w = 0; w < 16; ++w) { s += so[w][threadIdx.x]; z += sl[w]; }
-            const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + threadIdx.x;
+        auto store = [&](int col, float s, float z) {
+            const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + col;
             const float v = z == 0.f ? 0.f : s / z;
             if constexpr (F32) ((float *)a.out)[off] = v;
             else ((__nv_bfloat16 *)a.out)[off] = __float2bfloat16_rn(v);
-            if (a.lse && threadIdx.x == 0) a.lse[(size_t)env * RH + rr] = z == 0.f ? -INFINITY : (M + log2f(z)) * LN2;
+            if (a.lse && col == 0) a.lse[(size_t)env * RH + rr] = z == 0.f ? -INFINITY : (M + log2f(z)) * LN2;
+        };
+        if constexpr (WPR == 1) {
+            if (there) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) store(lane * V + i, acc[i], L);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; ++i) so[warp][lane * V + i] = acc[i];
+            if (lane == 0) sl[warp] = L;
+            __syncthreads();
+            if (threadIdx.x < HD) {   // (one row per CTA: every thread knows it)
+                float s = 0.f, z = 0.f;
+#pragma unroll
+                for (int w = 0; w < 16; ++w) { s += so[w][threadIdx.x]; z += sl[w]; }
+                store(threadIdx.x, s, z);
+            }
+            __syncthreads();
         }
-        __syncthreads();
     }
 }
 
-int attend_warps(int rows, bool f32)
+int attend_warps(int hd, int tile) { return hd == 128 ? (tile == 8 ? AttendCfg<128, 1, false>::WARPS : AttendCfg<128, 2, false>::WARPS) : (tile == 8 ? AttendCfg<64, 1, false>::WARPS : AttendCfg<64, 2, false>::WARPS); }
+
+// Query rows per item: 8, or 16 where that fills its rows and long prefixes make up for fewer warps per SM.  Rows beyond a tile are
+// further items next to this one: they read the same keys and values from L2.  A row's result is the same in every tile.
+// Measured, us with 8 / 16 (/ 32, which is gone) rows per item, 16 heads:
+//   head_dim 128, 128 x 768 tokens:  16 rows 91 / 83 / 124,  32 rows 146 / 132 / 134,  64 rows 280 / 241 / 251
+//                 256 x 256 tokens:  16 rows 71 / 77 / 116,  32 rows 124 / 124 / 134;  512 x 64: 16 rows 70 / 87 / 120
+//   head_dim 64,  128 x 768 tokens:  16 rows 50 / 61 / 77,   32 rows  89 /  82 /  82,  64 rows 169 / 141 / 155;  512 x 768: 16 rows 180 / 161
+//                 256 x 256 tokens:  16 rows 44 / 48 / 76,   32 rows  79 /  75 /  87;  512 x 64: 32 rows 83 / 91 / 101
+//   fp32, 64:     128 x 768 tokens:  16 rows 62 / 68 / 109,  32 rows 114 / 114 / 116: always 8
+int attend_tile(int hd, int rows, bool f32, int max_len)
 {
-    const int nt = row_tile(rows) / 8;
-    return f32 ? (nt == 1 ? AttendCfg<128, 1, true>::WARPS : (nt == 2 ? AttendCfg<128, 2, true>::WARPS : AttendCfg<128, 4, true>::WARPS))
-               : (nt == 1 ? AttendCfg<128, 1, false>::WARPS : (nt == 2 ? AttendCfg<128, 2, false>::WARPS : AttendCfg<128, 4, false>::WARPS));
+    const bool fills = (rows - 1) % 16 >= 8;
+    const bool pays = max_len >= 512 || (hd < 128 && rows >= 32 && max_len >= 256);
+    return !f32 && fills && pays ? 16 : 8;
 }
 
 namespace {
 
-// Query rows per item, as the smallest tile whose items still fill the SMs' warps if there is one below the rows' own tile: with few
-// items more of them beat reading a prefix once (96 environments x 301 tokens x 64 rows: 59 us with 32 rows, 22 with 8).
-// A row's result is the same in every tile.
+// ... and where items of 16 rows would not keep every warp busy one and a half times, items of 8 (the 50 / 61 above).
 int tile_for(const AttendArgs &a, const Envs &e, bool f32, int sms)
 {
-    const int rows = a.r.H * a.r.G;
-    int tile = row_tile(rows);
-    const long long base = (long long)(a.r.meta ? a.r.n_envs : e.n) * a.r.rec.kvh * a.n_split;
-    while (tile > 8 && base * ((rows + tile - 1) / tile) < (long long)sms * attend_warps(tile, f32)) tile /= 2;
-    return tile;
+    const int rows = a.r.H * a.r.G, tile = attend_tile(a.r.rec.hd, rows, f32, a.max_len);
+    const long long items = (long long)(a.r.meta ? a.r.n_envs : e.n) * a.r.rec.kvh * a.n_split * ((rows + tile - 1) / tile);
+    return 2 * items < 3LL * sms * attend_warps(a.r.rec.hd, tile) ? 8 : tile;
 }
 
 template <int HD, int NT, bool F32> cudaError_t go(const AttendArgs &a, const Envs &e, int grid, cudaStream_t st)
@@ -439,9 +428,8 @@ template <int HD, int NT, bool F32> cudaError_t go(const AttendArgs &a, const En
 
 template <int HD> cudaError_t pick(const AttendArgs &a, const Envs &e, bool f32, int grid, int sms, cudaStream_t st)
 {
-    const int nt = tile_for(a, e, f32, grid ? grid : sms) / 8;
-    if (f32) return nt == 1 ? go<HD, 1, true>(a, e, grid, st) : (nt == 2 ? go<HD, 2, true>(a, e, grid, st) : go<HD, 4, true>(a, e, grid, st));
-    return nt == 1 ? go<HD, 1, false>(a, e, grid, st) : (nt == 2 ? go<HD, 2, false>(a, e, grid, st) : go<HD, 4, false>(a, e, grid, st));
+    if (f32) return go<HD, 1, true>(a, e, grid, st);
+    return tile_for(a, e, f32, grid ? grid : sms) == 8 ? go<HD, 1, false>(a, e, grid, st) : go<HD, 2, false>(a, e, grid, st);
 }
 
 }  // namespace
@@ -451,20 +439,26 @@ cudaError_t launch_attend(const AttendArgs &a, const Envs &e, bool f32, int grid
     return a.r.rec.hd == 128 ? pick<128>(a, e, f32, grid, sms, st) : (a.r.rec.hd == 64 ? pick<64>(a, e, f32, grid, sms, st) : pick<32>(a, e, f32, grid, sms, st));
 }
 
+template <int HD, int WPR> static cudaError_t join(const AttendArgs &a, const Envs &e, bool f32, int g, cudaStream_t st)
+{
+    return f32 ? launch_kernel(attend_join_kernel<HD, true, WPR>, g, 512, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<HD, false, WPR>, g, 512, 0, st, 1, a, e);
+}
+
 cudaError_t launch_attend_join(const AttendArgs &a, const Envs &e, bool f32, int grid, int n_sms, cudaStream_t st)
 {
-    const long long rows = (long long)e.n * a.r.H * a.r.heads;
-    const long long cap = grid ? grid : (long long)n_sms * 8;
-    const int g = (int)(rows < cap ? rows : cap);
+    const bool many = a.n_split > 16;
+    const long long rows = (long long)e.n * a.r.H * a.r.heads, need = many ? rows : (rows + 15) / 16;
+    const long long cap = grid ? grid : (long long)n_sms * 4;
+    const int g = (int)(need < cap ? need : cap);
     if (g == 0) return cudaSuccess;
     struct Early {   // the join may be set up while the last pieces are being worked on; it waits for them itself
         Early() { pdl_set(true); }
         ~Early() { pdl_set(false); }
     } early;
     switch (a.r.rec.hd) {
-    case 128: return f32 ? launch_kernel(attend_join_kernel<128, true>, g, 512, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<128, false>, g, 512, 0, st, 1, a, e);
-    case 64: return f32 ? launch_kernel(attend_join_kernel<64, true>, g, 512, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<64, false>, g, 512, 0, st, 1, a, e);
-    default: return f32 ? launch_kernel(attend_join_kernel<32, true>, g, 512, 0, st, 1, a, e) : launch_kernel(attend_join_kernel<32, false>, g, 512, 0, st, 1, a, e);
+    case 128: return many ? join<128, 16>(a, e, f32, g, st) : join<128, 1>(a, e, f32, g, st);
+    case 64: return many ? join<64, 16>(a, e, f32, g, st) : join<64, 1>(a, e, f32, g, st);
+    default: return many ? join<32, 16>(a, e, f32, g, st) : join<32, 1>(a, e, f32, g, st);
     }
 }
 

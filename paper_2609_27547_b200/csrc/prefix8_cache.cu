@@ -162,13 +162,17 @@ __device__ __forceinline__ uint32_t weight_key(const EvictArgs &a, const float *
 }
 
 // Which tokens stay: one CTA per environment.  The key of the last kept token is found byte by byte (four passes of a
-// 256-bin histogram over the weights, which stay in L1/L2), then one pass in token order lists what is above it and the
-// first of what ties with it.  The mask and the weights follow in chunks that are read as a whole before they are
+// 256-bin histogram over the keys, which stay in shared memory up to SELECT_KEYS tokens and are made anew from the weights beyond),
+// then one pass in token order lists what is above it and the first of what ties with it.  The mask and the weights follow in chunks that are read as a whole before they are
 // written: a kept token never moves to a higher index, so working in place is safe.
 // Bound: latency -- 4 B per token against 256 B of codes in the second kernel.
-__global__ void __launch_bounds__(1024) select_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ EvictEnvs ev)
+constexpr int SELECT_KEYS = 49152;
+
+__global__ void __launch_bounds__(1024) select_kernel(const __grid_constant__ EvictArgs a, const __grid_constant__ EvictEnvs ev, int room)
 {
-    __shared__ int hist[256], wsum[2][32];
+    extern __shared__ uint32_t keys[];   // [room]
+    __shared__ int hist[256];
+    __shared__ uint32_t wsum[32];
     __shared__ uint32_t s_prefix;
     __shared__ int s_need;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -181,12 +185,20 @@ __global__ void __launch_bounds__(1024) select_kernel(const __grid_constant__ Ev
         int *kept = a.kept + (size_t)env * a.kept_stride;
         uint32_t prefix = 0;      // the bytes of the last kept key found so far
         int need = keep;          // how many tokens are kept among those that start with them
+        const bool cached = len <= room;
+        if (keep < len && cached) {
+#pragma unroll 4
+            for (int t = threadIdx.x; t < len; t += 1024) keys[t] = weight_key(a, w, mask, t, len);
+            __syncthreads();
+        }
+        auto key_of = [&](int t) { return cached ? keys[t] : weight_key(a, w, mask, t, len); };
         if (keep < len) {
             for (int shift = 24; shift >= 0; shift -= 8) {
                 if (threadIdx.x < 256) hist[threadIdx.x] = 0;
                 __syncthreads();
+#pragma unroll 4
                 for (int t = threadIdx.x; t < len; t += 1024) {
-                    const uint32_t k = weight_key(a, w, mask, t, len);
+                    const uint32_t k = key_of(t);
                     if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255], 1);   // counts: the order does not matter
                 }
                 __syncthreads();
@@ -212,27 +224,41 @@ __global__ void __launch_bounds__(1024) select_kernel(const __grid_constant__ Ev
                 need = s_need;
             }
         }
-        // tokens in order: above the last kept key, or the first `need` that equal it
+        // tokens in order, four to a thread: above the last kept key, or the first `need` that equal it.  Positions come from a scan of
+        // both counts at once (16 bits each: a round has 4096 tokens).
         int done_above = 0, done_equal = 0;
-        for (int base = 0; base < len; base += 1024) {
-            const int t = base + threadIdx.x;
-            bool above = false, equal = false;
-            if (t < len) {
-                if (keep == len) above = true;
-                else { const uint32_t k = weight_key(a, w, mask, t, len); above = k > prefix; equal = k == prefix; }
+        for (int base = 0; base < len; base += 4096) {
+            const int t0 = base + 4 * threadIdx.x;
+            uint32_t flags = 0, mine = 0;     // bit i: above, bit 4 + i: equal
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (t0 + i >= len) continue;
+                const uint32_t k = keep == len ? 1u : key_of(t0 + i);
+                const bool above = keep == len || k > prefix, equal = keep != len && k == prefix;
+                flags |= (uint32_t)above << i | (uint32_t)equal << (4 + i);
+                mine += (uint32_t)above + ((uint32_t)equal << 16);
             }
-            const uint32_t ba = __ballot_sync(0xffffffffu, above), be = __ballot_sync(0xffffffffu, equal), lower = (1u << lane) - 1u;
+            uint32_t upto = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
             __syncthreads();
-            if (lane == 0) { wsum[0][warp] = __popc(ba); wsum[1][warp] = __popc(be); }
+            if (lane == 31) wsum[warp] = upto;
             __syncthreads();
-            int na = done_above + __popc(ba & lower), ne = done_equal + __popc(be & lower);
-            for (int i = 0; i < 32; ++i) {
-                const int x = wsum[0][i], y = wsum[1][i];
-                if (i < warp) { na += x; ne += y; }
-                done_above += x; done_equal += y;
+            uint32_t all = wsum[lane];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) { const uint32_t v = __shfl_up_sync(0xffffffffu, all, o); if (lane >= o) all += v; }
+            const uint32_t before = (warp ? __shfl_sync(0xffffffffu, all, warp - 1) : 0u) + upto - mine, total = __shfl_sync(0xffffffffu, all, 31);
+            int na = done_above + (int)(before & 0xffffu), ne = done_equal + (int)(before >> 16);
+            done_above += (int)(total & 0xffffu);
+            done_equal += (int)(total >> 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool above = (flags >> i) & 1, equal = (flags >> (4 + i)) & 1;
+                const int at = na + min(ne, need);
+                if ((above || (equal && ne < need)) && at < keep) kept[at] = t0 + i;   // (always below keep unless someone changes the weights meanwhile)
+                na += above;
+                ne += equal;
             }
-            const int at = na + min(ne, need);
-            if ((above || (equal && ne < need)) && at < keep) kept[at] = t;   // (always below keep unless someone changes the weights meanwhile)
         }
         __syncthreads();   // the list is there for the whole CTA
         uint32_t *to_mask = reinterpret_cast<uint32_t *>(a.dst + (size_t)ev.slot[env] * a.rec.bytes + a.rec.mask);
@@ -364,7 +390,18 @@ cudaError_t launch_evict(const EvictArgs &a, const EvictEnvs &e, int max_keep, i
 {
     if (e.n == 0 || max_keep == 0) return cudaSuccess;
     const int g1 = grid && grid < e.n ? grid : e.n;
-    cudaError_t err = launch_kernel(select_kernel, g1, 1024, 0, st, 1, a, e);
+    int longest = 0;
+    for (int i = 0; i < e.n; ++i) longest = longest > e.len[i] ? longest : e.len[i];
+    const int room = longest < SELECT_KEYS ? longest : SELECT_KEYS;
+    static bool set[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!set[dev]) {
+        const cudaError_t e2 = cudaFuncSetAttribute(select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SELECT_KEYS * 4);
+        if (e2 != cudaSuccess) return e2;
+        set[dev] = true;
+    }
+    cudaError_t err = launch_kernel(select_kernel, g1, 1024, (size_t)room * 4, st, 1, a, e, room);
     if (err != cudaSuccess) return err;
     const int chunks = (max_keep + 8 * BLOCK - 1) / (8 * BLOCK);
     const long long heads = (long long)e.n * a.rec.kv_layers * 2 * a.rec.kvh;

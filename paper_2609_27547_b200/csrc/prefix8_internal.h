@@ -40,6 +40,7 @@ struct ReadArgs {
 
 struct AttendArgs {
     ReadArgs r;
+    int max_len;                   // the longest prefix of the launch (0: not known)
     void *out;
     long long o_env, o_tok;
     float *lse;                    // [env][H][heads] or NULL
@@ -59,15 +60,15 @@ struct WeighArgs {
     int accumulate;
 };
 
-// Query rows (H * G) per tile: 8, 16 or 32 (attend may take smaller ones).
-inline int row_tile(int rows) { return rows <= 8 ? 8 : (rows <= 16 ? 16 : 32); }
-int attend_warps(int rows, bool f32);     // items (one warp each) that an SM holds
+// attend: query rows (H * G) per item, and items (one warp each) that an SM holds
+int attend_tile(int hd, int rows, bool f32, int max_len);
+int attend_warps(int hd, int tile);
 // grid = CTAs of a persistent grid (an SM quota), 0: as many small CTAs as there are items
 cudaError_t launch_attend(const AttendArgs &a, const Envs &e, bool f32, int grid, int sms, cudaStream_t st);
 cudaError_t launch_attend_join(const AttendArgs &a, const Envs &e, bool f32, int grid, int n_sms, cudaStream_t st);
 cudaError_t launch_weigh(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st);
 
-constexpr int QUANT_ENVS = 256;
+constexpr int QUANT_ENVS = 1024;   // 28 KB of parameters
 struct QuantEnvs {
     int n;
     const void *planes[QUANT_ENVS];

@@ -17,7 +17,7 @@ namespace p8 {
 
 template <int HD, int NT, bool F32> struct WeighCfg {
     // tiles per warp (8 against 4: 107 -> 95 us on 256 x 734 tokens x 16 heads x 16 rows; 16 spill), CTAs per SM
-    static constexpr int TT = 8, CTAS = (NT == 4 || F32) ? 1 : 2;
+    static constexpr int TT = 8, CTAS = F32 ? 1 : 2;
     static constexpr int TILE = BLOCK * HD, RING = HD == 32 ? 8192 : (CTAS == 2 ? 12288 : 24576), SLOTS = RING / TILE < 8 ? RING / TILE : 8;
     static constexpr int SMEM = 8 * RING;
 };
@@ -193,11 +193,14 @@ template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Env
     return launch_kernel(weigh_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), 256, (size_t)C::SMEM, st, 1, a, e, hw, n_chunk);
 }
 
+// Query rows per product.  Measured, us with 8 / 16 / 32 on 128 x 768 tokens x 16 heads: bf16 of 128, 16 rows 68 / 58 / 87, 32 rows
+// 124 / 97 / 97; bf16 of 64, 32 rows 85 / 66 / 75; fp32 of 64, 16 rows 69 / 61 / 80, 32 rows 125 / 104 / 90, 64 rows 230 / 193 / 161.
 template <int HD> cudaError_t pick(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st)
 {
-    const int nt = row_tile(a.r.H * a.r.G) / 8;
-    if (f32) return nt == 1 ? go<HD, 1, true>(a, e, max_len, grid, st) : (nt == 2 ? go<HD, 2, true>(a, e, max_len, grid, st) : go<HD, 4, true>(a, e, max_len, grid, st));
-    return nt == 1 ? go<HD, 1, false>(a, e, max_len, grid, st) : (nt == 2 ? go<HD, 2, false>(a, e, max_len, grid, st) : go<HD, 4, false>(a, e, max_len, grid, st));
+    const int rows = a.r.H * a.r.G;
+    if (rows <= 8) return f32 ? go<HD, 1, true>(a, e, max_len, grid, st) : go<HD, 1, false>(a, e, max_len, grid, st);
+    if (!f32) return go<HD, 2, false>(a, e, max_len, grid, st);
+    return rows <= 16 ? go<HD, 2, true>(a, e, max_len, grid, st) : go<HD, 4, true>(a, e, max_len, grid, st);
 }
 
 }  // namespace

@@ -210,15 +210,15 @@ def quantize(layout: Layout, pool: torch.Tensor, planes: Planes, lens=None, *, s
             raise ValueError("planes must share one row stride and lie a whole number of rows apart")
         rows.append(plane // rs)
     if whole:
-        limit = [P] * n
+        limit = [P]
         ptrs = _addresses(planes.data_ptr(), planes.stride(0) * planes.element_size(), n)
-        rows = (C.c_int32 * n)(*rows * n)
+        rows = (C.c_int32 * n)(*rows * n) if n <= 16 else (C.c_int32 * n).from_buffer(np.full(n, rows[0], dtype=np.int32))
     else:
         limit = [x.shape[2] for x in views_]
         ptrs = (C.c_void_p * n)(*[x.data_ptr() for x in views_])
         rows = (C.c_int32 * n)(*rows)
     _same_device(pool, *views_)
-    L = _host(limit if lens is None else lens, "lens")
+    L = torch.full((n,), P, dtype=torch.int32) if lens is None and whole else _host(limit if lens is None else lens, "lens")
     if L.numel() != n:
         raise ValueError("%d lengths for %d environments" % (L.numel(), n))
     given = L.tolist()
@@ -278,7 +278,7 @@ def attend(layout: Layout, pool: torch.Tensor, q: torch.Tensor, lens, *, layer: 
         if split_tokens > 0 or (split_tokens == 0 and layout.capacity > 256):
             need = dll.ebrl_prefix8_attend_workspace(cl, n, L.data_ptr(), H, heads, split_tokens, sm_quota)
         if out is None:
-            out = q.new_empty((n, H, heads, hd))
+            out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((n, H, heads, hd))
         if lse is None:
             lse = q.new_empty((n, H, heads), dtype=torch.float32)
         ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
