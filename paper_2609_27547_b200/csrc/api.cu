@@ -102,7 +102,7 @@ struct Slot {
     int prefix_rows = 0, prefix_slices = 0;   // of the batch being launched
     // 8-bit prefixes: the log-sum-exp of every row and head (of the last cross-attention), for the token weights
     float *lse = nullptr;
-    int longest = 0;                          // prefix of the batch being launched
+    int longest = 0, alike = 0;               // prefix of the batch being launched, whether all are that long
     int weigh_len = 0;                        // of the batch being launched: its longest prefix if any environment wants weights, else 0
     TensorMap128 t_hid;
 };
@@ -536,7 +536,7 @@ void cross_attend8(ebrl_actgen *h, Slot &s, Launcher &ln, const AttnArgs &x, dou
     a.r.H = x.H; a.r.heads = x.n_heads; a.r.G = 1; a.r.scale = 1.0f / sqrtf((float)x.hd); a.r.meta = x.meta; a.r.n_envs = x.n_envs;
     a.out = x.out; a.o_env = (long long)x.H * x.o_stride; a.o_tok = x.o_stride;
     a.out_t1 = x.out_t1; a.out_t2 = x.out_t2; a.split_out = x.split_out;
-    a.n_split = 1; a.max_len = s.longest; a.lse = s.weigh_len > 0 ? s.lse : nullptr;
+    a.n_split = 1; a.max_len = s.longest; a.alike = s.alike; a.lse = s.weigh_len > 0 ? s.lse : nullptr;
     const int quota = ln.grid < h->n_sms ? ln.grid : 0;   // the whole chip: the launch that evens out ragged prefixes
     ln.run(EBRL_KC_CROSS_ATTN, 4.0 * x.H * sum_P * d, 2.0 * sum_P * d + 2.0 * M * d * (double)h->esz,
            [&] { return p8::launch_attend(a, none, !h->bf16, quota, h->n_sms, ln.st); });
@@ -748,6 +748,7 @@ ebrl_status_t flush_slot(ebrl_actgen *h, Slot &s)
     }
     s.longest = s.weigh_len = 0;
     for (const EnvMeta &m : s.pending) s.longest = std::max(s.longest, (int)m.P);
+    s.alike = std::all_of(s.pending.begin(), s.pending.end(), [&](const EnvMeta &m) { return m.P == s.longest; });
     for (const EnvMeta &m : s.pending)
         if (m.weight) s.weigh_len = std::max(s.weigh_len, (int)m.P);
     s.pending.clear();

@@ -297,6 +297,7 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
         for (int first = 0; first < n; first += CHUNK_ENVS) {
             const Envs &e = some_envs(first, std::min(CHUNK_ENVS, n - first), slots, len);
             a.max_len = longest(e.len, e.n);
+            a.alike = std::all_of(e.len, e.len + e.n, [&](int v) { return v == a.max_len; });
             a.r.q = (const char *)q + first * q_env_stride * es;
             a.out = (char *)out + first * o_env_stride * es;
             a.lse = lse ? lse + (size_t)first * H * n_heads : nullptr;

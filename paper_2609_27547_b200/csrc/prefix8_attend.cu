@@ -7,15 +7,15 @@
 //   own ring of stages (a key and a value tile each) filled by cp.async, no barrier, no partial results to join unless a prefix is
 //   cut.  A record's head is contiguous, so a tile is one straight 4 KB run at head_dim 128.
 //   At head_dim 128 SMs hold 12 warps at 8 rows and 8 at 16, at 64 they hold 16 and 12 (what registers allow); 96 - 130 KB of
-//   tiles are in flight per SM, twice what HBM latency asks for.  With all SMs to itself the launch is one CTA per item,
-//   which lets the hardware even out ragged prefixes; under an SM quota it is a persistent grid of `quota` CTAs that hold all of an SM's warps.
-//   (Four warps per item, joined in shared memory, were 1.6 times slower on 512 x 768 tokens x 16 heads: an item was
-//   over before its set-up and join were paid for.)
+//   tiles are in flight per SM, twice what HBM latency asks for, and a warp's requests run on from one item into the next
+//   (512 x 768 tokens x 16 heads x 16 rows: 314 -> 294 us).  Where prefixes are alike, or under an SM quota, warps are persistent;
+//   where they differ the launch is one CTA per item, which lets the hardware even them out.
+//   (Four warps per item, joined in shared memory, were 1.6 times slower: an item was over before its set-up and join were paid for.)
 //
-//   With the cache in L2 (arithmetic alone) 512 x 768 tokens x 16 heads of 128 take 143 us at 8 rows and 240 at 16; from HBM
-//   241 us (6.7 TB/s of codes) and 296 (5.4).  At 16 rows the legacy tensor path is what it waits for: a product occupies a
-//   quarter-SM for 9 cycles (64 a tile), fp32 instructions do not run beside it (conversions and exponentials do), and the
-//   sum of both is 740 of the 1300 cycles a tile takes.
+//   With the cache in L2 (arithmetic alone) 512 x 768 tokens x 16 heads of 128 take 150 us at 8 rows and 228 at 16; from HBM
+//   240 us (6.7 TB/s of codes) and 286 (5.6; 294 at the power cap).  At 16 rows the legacy tensor path is what it waits for: a product
+//   occupies a quarter-SM for 9 cycles (64 a tile), fp32 instructions do not run beside it (conversions and exponentials do),
+//   and the sum of both is 740 of the 1250 cycles a tile takes.
 //
 //   Running maximum, lazily: a row's reference is raised only when a score exceeds it by 2^14 / 2^6; until then the weights
 //   2^(s - ref) stay below 2^14, which f16 holds with the same 11 bits.  The common tile needs one vote and no
@@ -41,8 +41,7 @@ template <int HD, int NT, bool F32> struct AttendCfg {
     static constexpr int ROOM = 224 * 1024 / WARPS / (2 * TILE);
     static constexpr int STAGES = ROOM < 4 ? ROOM : 4;                // 2 .. 4 pairs of a key and a value tile per warp
     static constexpr int WARP_BYTES = STAGES * 2 * TILE;              // its ring
-    static constexpr int PSTRIDE = HD + 4;                            // floats per staged output row
-    static_assert(STAGES >= 2 && 8 * PSTRIDE * 4 <= STAGES * 2 * TILE, "ring");
+    static_assert(STAGES >= 2, "ring");
 };
 
 template <int HD, int NT, bool F32>
@@ -64,44 +63,82 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
     pdl_launch_dependents();
     pdl_wait();
 
+    // what item `i` is: its row tile, head, piece, environment, record and tokens t0 .. t1 (none past the prefix's end)
+    struct Item { int rt, kh, sp, env, len, t0, t1; const char *rec; };
+    auto item_of = [&](unsigned x) {
+        Item it;
+        it.rt = (int)(x % (unsigned)RT); x /= (unsigned)RT;
+        it.kh = (int)(x % (unsigned)kvh); x /= (unsigned)kvh;
+        it.sp = (int)(x % (unsigned)a.n_split); it.env = (int)(x / (unsigned)a.n_split);
+        if (a.r.meta) { it.rec = (const char *)a.r.meta[it.env].kv; it.len = a.r.meta[it.env].P; }
+        else { it.rec = a.r.pool + (size_t)ev.slot[it.env] * a.r.rec.bytes; it.len = ev.len[it.env]; }
+        it.t0 = it.sp * a.split;
+        it.t1 = a.n_split == 1 ? it.len : min(it.len, it.t0 + a.split);
+        return it;
+    };
+    auto q_at = [&](const Item &it, int row) {   // offset of query row `row` of the item's kv head, in elements
+        const int tok = row / G;
+        return (size_t)it.env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)(it.kh * G + row - tok * G) * HD;
+    };
     // items go round the CTAs first, so that the last round spreads over all SMs
-    for (long long item = (long long)warp * gridDim.x + blockIdx.x; item < items; item += (long long)gridDim.x * warps) {
-        unsigned x = (unsigned)item;
-        const int rt = (int)(x % (unsigned)RT); x /= (unsigned)RT;
-        const int kh = (int)(x % (unsigned)kvh); x /= (unsigned)kvh;
-        const int sp = (int)(x % (unsigned)a.n_split), env = (int)(x / (unsigned)a.n_split);
-        const char *rec;
-        int len;
-        if (a.r.meta) { rec = (const char *)a.r.meta[env].kv; len = a.r.meta[env].P; }
-        else { rec = a.r.pool + (size_t)ev.slot[env] * a.r.rec.bytes; len = ev.len[env]; }
-        const int t0 = sp * a.split, t1 = a.n_split == 1 ? len : min(len, t0 + a.split);
-        if (sp > 0 && t0 >= len) continue;
-        const int ntile = (t1 - t0 + BLOCK - 1) / BLOCK;
-        const char *kp = rec + a.r.rec.head(a.r.layer, 0, kh) + (size_t)t0 * HD, *vp = rec + a.r.rec.head(a.r.layer, 1, kh) + (size_t)t0 * HD;
+    const unsigned first = (unsigned)warp * gridDim.x + blockIdx.x, stride = gridDim.x * (unsigned)warps;
 
-        // requests the item's next tile (keys and values) into a stage of the ring; one commit group, empty past the end
-        int left = t1 - t0;
-        auto issue = [&](int stage) {
+    // The requests run STAGES - 1 tiles ahead of the arithmetic, from one item into the next: while an item's last tiles are worked on the next
+    // one's first tiles (and its queries, scales and mask, into L1) are on their way.
+    unsigned asked = first;     // the item being requested; its next tile, and the tokens that are left from there on
+    const char *kp = nullptr, *vp = nullptr;
+    int left = 0;
+    auto seek = [&]() {
+        while (asked < (unsigned)items) {
+            const Item it = item_of(asked);
+            left = it.t1 - it.t0;
             if (left > 0) {
-                const uint32_t dst = ring_u + (uint32_t)(stage * 2 * C::TILE);
-                request_tile<HD>(dst, kp, left, lane);
-                request_tile<HD>(dst + C::TILE, vp, left, lane);
-                kp += C::TILE;
-                vp += C::TILE;
-                left -= BLOCK;
-            }
-            cp_commit();
-        };
+                kp = it.rec + a.r.rec.head(a.r.layer, 0, it.kh) + (size_t)it.t0 * HD;
+                vp = it.rec + a.r.rec.head(a.r.layer, 1, it.kh) + (size_t)it.t0 * HD;
+                constexpr int LINES = HD * (F32 ? 4 : 2) > 128 ? HD * (F32 ? 4 : 2) / 128 : 1;   // 128-byte lines of a query row
 #pragma unroll
-        for (int j = 0; j < C::STAGES - 1; ++j) issue(j);
+                for (int i = 0; i < (NT * 8 * LINES + 31) / 32; ++i) {
+                    const int row = it.rt * NT * 8 + (i * 32 + lane) / LINES;
+                    if (i * 32 + lane < NT * 8 * LINES && row < R) prefetch_l1((const char *)a.r.q + q_at(it, row) * (F32 ? 4 : 2) + (lane % LINES) * 128);
+                }
+                if (lane < 3) prefetch_l1((lane < 2 ? it.rec + a.r.rec.head_scales(a.r.layer, lane, it.kh) : it.rec + a.r.rec.mask) + it.t0 / BLOCK * 4);
+                return;
+            }
+            asked += stride;
+        }
+        left = 0;
+    };
+    seek();
+    auto issue = [&](int stage) {   // one commit group, empty when nothing is left
+        if (left > 0) {
+            const uint32_t dst = ring_u + (uint32_t)(stage * 2 * C::TILE);
+            request_tile<HD>(dst, kp, left, lane);
+            request_tile<HD>(dst + C::TILE, vp, left, lane);
+            kp += C::TILE;
+            vp += C::TILE;
+            left -= BLOCK;
+            if (left <= 0) { asked += stride; seek(); }
+        }
+        cp_commit();
+    };
+#pragma unroll
+    for (int j = 0; j < C::STAGES - 1; ++j) issue(j);
+    int stage = 0;
+
+    for (unsigned item = first; item < (unsigned)items; item += stride) {
+        const Item it = item_of(item);
+        const int rt = it.rt, kh = it.kh, sp = it.sp, env = it.env, t0 = it.t0, t1 = it.t1;
+        const char *rec = it.rec;
+        if (sp > 0 && t0 >= it.len) continue;
+        const int ntile = (t1 - t0 + BLOCK - 1) / BLOCK;
 
         // queries
         uint32_t q[NT][ST][QW<F32>];
         float fr[NT][2];   // what takes a raw product of row 2t (+ 1) of column tile nt to a score in units of log 2 (times the key scale)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = rt * NT * 8 + nt * 8 + g, tok = r / G;
-            const size_t off = (size_t)env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)(kh * G + r - tok * G) * HD;
+            const int r = rt * NT * 8 + nt * 8 + g;
+            const size_t off = q_at(it, r < R ? r : 0);
             const void *p = F32 ? (const void *)((const float *)a.r.q + off) : (const void *)((const __nv_bfloat16 *)a.r.q + off);
             const float f = load_q<HD, F32>(p, r < R, a.r.scale < 0.f, t, q[nt]) * (fabsf(a.r.scale) * LOG2E);
             fr[nt][0] = __shfl_sync(FULL, f, 8 * t);
@@ -126,7 +163,6 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         }
         float ks_l = 0.f, vs_l = 0.f;      // scales and visible tokens of tile (i & ~31) + lane
         uint32_t mk_l = 0;
-        int stage = 0;
         for (int i = 0; i < ntile; ++i) {
             if ((i & 31) == 0) {
                 const int tile = t0 / BLOCK + i + lane;
@@ -272,11 +308,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                     });
             }
         }
-        cp_wait<0>();      // only empty groups are left; the ring is free
-        __syncwarp();
-
-        // one column tile of rows at a time through the ring, so that rows leave in whole 128-byte runs
-        float *rows = reinterpret_cast<float *>(smem + (size_t)warp * C::WARP_BYTES);
+        // Outputs: lane (g, t) has columns g of rows 2t, 2t + 1 of 8 x 8 matrices; transposed it has columns 2t, 2t + 1 of row g.
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             float L[2], inv[2];
@@ -293,30 +325,33 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                     else if (a.lse) a.lse[(size_t)env * a.r.H * a.r.heads + row] = L[j] == 0.f ? -INFINITY : (mr[nt][j] + log2f(L[j])) * LN2;
                 }
             }
+            const int r = rt * NT * 8 + nt * 8 + g, tok = r / G, head = kh * G + r - tok * G;
+            const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + 2 * t;
+            float *part = a.part_o + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + (size_t)tok * a.r.heads + head) * HD + 2 * t;
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    rows[(2 * t) * C::PSTRIDE + m * 16 + 8 * k + g] = o[m][nt][2 * k] * inv[0];
-                    rows[(2 * t + 1) * C::PSTRIDE + m * 16 + 8 * k + g] = o[m][nt][2 * k + 1] * inv[1];
+                    const int col = m * 16 + 8 * k;
+                    const float x = o[m][nt][2 * k] * inv[0], y = o[m][nt][2 * k + 1] * inv[1];
+                    if (F32 || a.n_split > 1) {   // upper and lower halves apart
+                        const uint32_t xu = __float_as_uint(x), yu = __float_as_uint(y);
+                        const uint32_t hi = transpose8(__byte_perm(xu, yu, 0x7632)), lo = transpose8(__byte_perm(xu, yu, 0x5410));
+                        const float2 v = make_float2(__uint_as_float(__byte_perm(lo, hi, 0x5410)), __uint_as_float(__byte_perm(lo, hi, 0x7632)));
+                        if (r < R) {
+                            if (a.n_split > 1) *reinterpret_cast<float2 *>(part + col) = v;
+                            else if (a.split_out) store_split2(a.out, a.out_t1, a.out_t2, off + col, v.x, v.y);
+                            else *reinterpret_cast<float2 *>((float *)a.out + off + col) = v;
+                        }
+                    } else {
+                        const __nv_bfloat162 u = __floats2bfloat162_rn(x, y);
+                        const uint32_t w = transpose8(*reinterpret_cast<const uint32_t *>(&u));
+                        if (r < R) *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + off + col) = w;
+                    }
                 }
-            __syncwarp();
-#pragma unroll
-            for (int v = 0; v < HD / 16; ++v) {
-                const int row = (v * 32 + lane) / (HD / 4), col = (v * 32 + lane) % (HD / 4) * 4, r = rt * NT * 8 + nt * 8 + row, tok = r / G, head = kh * G + r - tok * G;
-                if (r < R) {
-                    const float4 u = *reinterpret_cast<const float4 *>(rows + row * C::PSTRIDE + col);
-                    const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + col;
-                    if (a.n_split > 1)
-                        *reinterpret_cast<float4 *>(a.part_o + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + (size_t)tok * a.r.heads + head) * HD + col) = u;
-                    else if constexpr (!F32) store4<__nv_bfloat16>((__nv_bfloat16 *)a.out + off, u.x, u.y, u.z, u.w);
-                    else if (a.split_out) store_split4(a.out, a.out_t1, a.out_t2, off, u.x, u.y, u.z, u.w);
-                    else store4<float>((float *)a.out + off, u.x, u.y, u.z, u.w);
-                }
-            }
-            __syncwarp();
         }
     }
+    cp_wait<0>();      // only empty groups are left
 }
 
 // Joins the pieces of long prefixes: WPR warps per query row (16 where there are many pieces: latency; 1 where there are few: rows),
@@ -407,7 +442,7 @@ int tile_for(const AttendArgs &a, const Envs &e, bool f32, int sms)
     return 2 * items < 3LL * sms * attend_warps(a.r.rec.hd, tile) ? 8 : tile;
 }
 
-template <int HD, int NT, bool F32> cudaError_t go(const AttendArgs &a, const Envs &e, int grid, cudaStream_t st)
+template <int HD, int NT, bool F32> cudaError_t go(const AttendArgs &a, const Envs &e, int grid, int sms, cudaStream_t st)
 {
     using C = AttendCfg<HD, NT, F32>;
     static bool set[64] = {};
@@ -421,15 +456,17 @@ template <int HD, int NT, bool F32> cudaError_t go(const AttendArgs &a, const En
     const long long n = a.r.meta ? a.r.n_envs : e.n;
     const long long items = n * a.r.rec.kvh * a.n_split * ((a.r.H * a.r.G + NT * 8 - 1) / (NT * 8));
     if (items == 0) return cudaSuccess;
+    // Under a quota: persistent CTAs with all of an SM's warps.  Else one-warp CTAs: as many as the SMs hold where prefixes are alike (the
+    // ring then runs on from item to item), one per item where they are not (the hardware hands out the next as one ends).
     const int warps = grid ? C::WARPS : 1;
-    const long long cap = grid ? grid : 1 << 20;   // items go round the CTAs first: a grid of `quota` CTAs uses as many SMs as it has items
+    const long long cap = grid ? grid : (a.alike ? (long long)sms * C::WARPS : 1 << 20);
     return launch_kernel(attend_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), warps * 32, (size_t)(warps * C::WARP_BYTES), st, 1, a, e);
 }
 
 template <int HD> cudaError_t pick(const AttendArgs &a, const Envs &e, bool f32, int grid, int sms, cudaStream_t st)
 {
-    if (f32) return go<HD, 1, true>(a, e, grid, st);
-    return tile_for(a, e, f32, grid ? grid : sms) == 8 ? go<HD, 1, false>(a, e, grid, st) : go<HD, 2, false>(a, e, grid, st);
+    if (f32) return go<HD, 1, true>(a, e, grid, sms, st);
+    return tile_for(a, e, f32, grid ? grid : sms) == 8 ? go<HD, 1, false>(a, e, grid, sms, st) : go<HD, 2, false>(a, e, grid, sms, st);
 }
 
 }  // namespace

@@ -40,7 +40,8 @@ struct ReadArgs {
 
 struct AttendArgs {
     ReadArgs r;
-    int max_len;                   // the longest prefix of the launch (0: not known)
+    int max_len;                   // the longest prefix of the launch
+    int alike;                     // whether all are that long
     void *out;
     long long o_env, o_tok;
     float *lse;                    // [env][H][heads] or NULL

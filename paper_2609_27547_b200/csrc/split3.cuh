@@ -29,4 +29,15 @@ __device__ __forceinline__ void store_split4(void *p0, void *p1, void *p2, size_
     *reinterpret_cast<uint2 *>((__nv_bfloat16 *)p2 + off) = *reinterpret_cast<const uint2 *>(t2);
 }
 
+// Two consecutive values (4 bytes each).
+__device__ __forceinline__ void store_split2(void *p0, void *p1, void *p2, size_t off, float a, float b)
+{
+    __nv_bfloat16 t0[2], t1[2], t2[2];
+    split3(a, t0[0], t1[0], t2[0]);
+    split3(b, t0[1], t1[1], t2[1]);
+    *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)p0 + off) = *reinterpret_cast<const uint32_t *>(t0);
+    *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)p1 + off) = *reinterpret_cast<const uint32_t *>(t1);
+    *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)p2 + off) = *reinterpret_cast<const uint32_t *>(t2);
+}
+
 }  // namespace ebrl
