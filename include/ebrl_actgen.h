@@ -79,8 +79,8 @@ typedef enum { EBRL_F32 = 0, EBRL_BF16 = 1,
                                      walks all Euler steps of a small batch); always launch one
                                      kernel per operation                                        */
 #define EBRL_FLAG_FORCE_FUSED 32u /* use the persistent step kernel for every batch the kernel
-                                     covers (bf16 tensor-core models with H a divisor of 128 and
-                                     A <= 16), whatever its size.  Without the flag no batch takes
+                                     covers (bf16 tensor-core models on bf16 planes with H a divisor
+                                     of 128 and A <= 16), whatever its size.  Without the flag no batch takes
                                      it: it delivers the same bits as the per-operation kernels
                                      but has measured slower on B200 at every batch size tried;
                                      EBRL_FUSED_MAX_ROWS=<rows> in the environment at create makes

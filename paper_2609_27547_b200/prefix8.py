@@ -134,10 +134,17 @@ def _stream(device: torch.device, stream: Optional[torch.cuda.Stream], *tensors)
         return now
     if stream.device != device:
         raise ValueError("the stream belongs to another device")
+    here = torch.cuda.current_stream(device)
     for t in tensors:
         if t is not None:
             t.record_stream(stream)
+            t.record_stream(here)
     return stream.cuda_stream
+
+
+def _elsewhere(device: torch.device, stream: Optional[torch.cuda.Stream]) -> bool:
+    """Whether the call runs on another stream than the current one."""
+    return stream is not None and stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _n_slots(lens: torch.Tensor, slots, pool: torch.Tensor):
@@ -277,12 +284,14 @@ def attend(layout: Layout, pool: torch.Tensor, q: torch.Tensor, lens, *, layer: 
         need = 0
         if split_tokens > 0 or (split_tokens == 0 and layout.capacity > 256):
             need = dll.ebrl_prefix8_attend_workspace(cl, n, L.data_ptr(), H, heads, split_tokens, sm_quota)
-        if out is None:
-            out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((n, H, heads, hd))
-        if lse is None:
-            lse = q.new_empty((n, H, heads), dtype=torch.float32)
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        st = _stream(pool.device, stream, pool, q, out, lse, ws)
+        # what is allocated here belongs to the stream that writes it; results are used on the current one, too
+        with torch.cuda.stream(stream) if _elsewhere(pool.device, stream) else _HERE:
+            if out is None:
+                out = torch.empty_like(q) if q.is_contiguous() else q.new_empty((n, H, heads, hd))
+            if lse is None:
+                lse = q.new_empty((n, H, heads), dtype=torch.float32)
+            ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        st = _stream(pool.device, stream, pool, q, out, lse)
         if n and H and heads:
             _check(dll.ebrl_prefix8_attend(cl, pool.data_ptr(), pool.shape[0], n, sp, L.data_ptr(), int(layer), q.data_ptr(), _DTYPES[q.dtype],
                                            H, heads, q.stride(0), q.stride(1), out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr(),
@@ -339,7 +348,8 @@ def evict(layout: Layout, src: torch.Tensor, dst: torch.Tensor, weight: torch.Te
     ws = _weights(layout, src, weight, "weight")
     wo = 0 if weight_out is None else _weights(layout, src, weight_out, "weight_out")
     if kept is None:
-        kept = torch.empty((n, max(1, most)), dtype=torch.int32, device=src.device)
+        with torch.cuda.stream(stream) if _elsewhere(src.device, stream) else _HERE:
+            kept = torch.empty((n, max(1, most)), dtype=torch.int32, device=src.device)
     elif kept.dtype != torch.int32 or kept.dim() != 2 or kept.shape[0] != n or (kept.shape[1] > 1 and kept.stride(1) != 1) or \
             kept.shape[1] < most or (n > 1 and kept.stride(0) < kept.shape[1]):
         raise ValueError("kept must be int32 [n, >= the largest new length] with contiguous rows")
