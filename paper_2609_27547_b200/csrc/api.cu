@@ -544,7 +544,7 @@ void cross_attend8(ebrl_actgen *h, Slot &s, Launcher &ln, const AttnArgs &x, dou
         p8::WeighArgs w{};
         w.r = a.r; w.lse = s.lse; w.l_env = (long long)x.H * x.n_heads; w.l_tok = x.n_heads; w.l_head = 1; w.accumulate = 1;
         ln.run(EBRL_KC_CROSS_ATTN, 2.0 * x.H * sum_P * d, sum_P * d + (double)M * d * h->esz,
-               [&] { return p8::launch_weigh(w, none, !h->bf16, s.weigh_len, quota, ln.st); });
+               [&] { return p8::launch_weigh(w, none, !h->bf16, s.weigh_len, quota, h->n_sms, ln.st); });
     }
 }
 

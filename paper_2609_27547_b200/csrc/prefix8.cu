@@ -336,7 +336,7 @@ ebrl_status_t ebrl_prefix8_weigh(const ebrl_prefix8_layout_t *layout, const void
             const Envs &e = some_envs(first, std::min(CHUNK_ENVS, n - first), slots, len);
             a.r.q = (const char *)q + first * q_env_stride * (int64_t)esize(q_dtype);
             a.lse = lse + first * lse_env_stride;
-            if ((st = launched(launch_weigh(a, e, q_dtype == EBRL_F32, longest(e.len, e.n), sm_quota, (cudaStream_t)stream))) != EBRL_OK) return st;
+            if ((st = launched(launch_weigh(a, e, q_dtype == EBRL_F32, longest(e.len, e.n), sm_quota, sms, (cudaStream_t)stream))) != EBRL_OK) return st;
         }
         return EBRL_OK;
     });

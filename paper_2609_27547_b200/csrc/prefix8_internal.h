@@ -67,7 +67,7 @@ int attend_warps(int hd, int tile);
 // grid = CTAs of a persistent grid (an SM quota), 0: as many small CTAs as there are items
 cudaError_t launch_attend(const AttendArgs &a, const Envs &e, bool f32, int grid, int sms, cudaStream_t st);
 cudaError_t launch_attend_join(const AttendArgs &a, const Envs &e, bool f32, int grid, int n_sms, cudaStream_t st);
-cudaError_t launch_weigh(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st);
+cudaError_t launch_weigh(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, int sms, cudaStream_t st);
 
 constexpr int QUANT_ENVS = 1024;   // 28 KB of parameters
 struct QuantEnvs {

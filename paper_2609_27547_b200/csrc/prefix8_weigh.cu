@@ -4,35 +4,35 @@
 // attention's own traffic; gathering the weights inside attention would need either the scores of all heads in memory
 // (16 rows x 4 B per token and head against 128 B of codes) or atomics across heads, whose order changes the last bits.
 //
-// A CTA owns 256 x TW tokens of one environment and walks every (key/value head, row tile): its eight warps are HW
-// parallel heads x TW token groups (HW = 8 with eight heads or more).  A warp keeps its head's queries in registers for
-// eight tiles -- the query rows then cost an eighth of the keys' L2 traffic at 16 rows -- and the weights of its 256 tokens
-// in 32 registers per lane over all of its heads.  Only at the end are they summed over the lanes of a quad and, in
-// warp order, over the parallel heads: a fixed order, no atomics.  The key tiles of a warp's heads are one stream through a
-// ring of cp.async slots, so the ring stays full across heads.
+// A CTA owns some tiles x TW of one environment and walks every (key/value head, row tile): its eight warps are HW parallel
+// heads x TW token groups (HW = 8 with eight heads or more).  A warp keeps its head's queries in registers for up to twelve
+// tiles, adds a token's weights up over the quad's rows by three exchanges, and over its heads in shared memory, in
+// words of its own.  At the end the parallel heads are added in warp order: a fixed order whatever the tiles per warp, no atomics.
+// The key tiles of a warp's heads are one stream through a ring of cp.async slots, so the ring stays full across heads.
 #include "prefix8_tile.cuh"
 
 namespace ebrl {
 namespace p8 {
 
+constexpr int MAX_TILES = 12;   // per warp
+
 template <int HD, int NT, bool F32> struct WeighCfg {
-    // tiles per warp (8 against 4: 107 -> 95 us on 256 x 734 tokens x 16 heads x 16 rows; 16 spill), CTAs per SM
-    static constexpr int TT = 8, CTAS = F32 ? 1 : 2;
+    static constexpr int CTAS = F32 && (NT > 1 || HD == 128) ? 1 : 2;   // per SM
     static constexpr int TILE = BLOCK * HD, RING = HD == 32 ? 8192 : (CTAS == 2 ? 12288 : 24576), SLOTS = RING / TILE < 8 ? RING / TILE : 8;
     static constexpr int SMEM = 8 * RING;
 };
 
 template <int HD, int NT, bool F32>
 __global__ void __launch_bounds__(256, WeighCfg<HD, NT, F32>::CTAS)
-weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs ev, int hw_log2, int n_chunk)
+weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs ev, int hw_log2, int n_chunk, int tiles)
 {
     using C = WeighCfg<HD, NT, F32>;
-    constexpr int TOK = C::TT * BLOCK;   // tokens per warp
     extern __shared__ __align__(128) char smem[];
-    __shared__ float red[8][C::TT * BLOCK];
+    __shared__ float red[8][MAX_TILES * BLOCK];   // per warp: the sums of its tokens over its heads
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t ring_u = ptx::smem_u32(smem + (size_t)warp * C::RING);
     const int G = a.r.G, R = a.r.H * G, RT = (R + NT * 8 - 1) / (NT * 8), kvh = a.r.rec.kvh, units = kvh * RT;
+    const int tok_w = tiles * BLOCK;   // tokens per warp
     const int HW = 1 << hw_log2, TW = 8 >> hw_log2, hw = warp & (HW - 1), tw = warp >> hw_log2;
     const int n_envs = a.r.meta ? a.r.n_envs : ev.n;
     const long long items = (long long)n_envs * n_chunk;
@@ -52,10 +52,10 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
             len = ev.len[env];
             wp = a.weight + (size_t)ev.slot[env] * a.stride;
         }
-        const int c0 = chunk * TW * TOK;                     // first token of the CTA
+        const int c0 = chunk * TW * tok_w;                     // first token of the CTA
         if (c0 >= len || !wp) continue;                      // (the same for the whole CTA)
-        const int b0 = c0 + tw * TOK;                        // ... and of the warp
-        const int live = b0 >= len ? 0 : min(C::TT, (len - b0 + BLOCK - 1) / BLOCK);
+        const int b0 = c0 + tw * tok_w;                        // ... and of the warp
+        const int live = b0 >= len ? 0 : min(tiles, (len - b0 + BLOCK - 1) / BLOCK);
         const int mine = hw < units ? (units - hw + HW - 1) >> hw_log2 : 0;   // this warp's (head, row tile) units: hw, hw + HW, ...
         const int loads = mine * live;
         // load j of the warp's stream: tile j % live of its unit j / live
@@ -77,11 +77,8 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
             const int v = len - b0 - lane * BLOCK;
             if (v < BLOCK) seen &= (1u << v) - 1u;
         }
-        float acc[C::TT][2][2];
-#pragma unroll
-        for (int i = 0; i < C::TT; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) acc[i][h][0] = acc[i][h][1] = 0.f;
+        for (int k = lane; k < tok_w; k += 32) red[warp][k] = 0.f;
+        __syncwarp();
 
         int slot = 0, j = 0;
         for (int u = 0; u < mine; ++u) {
@@ -115,56 +112,49 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                     ls[nt][c] = __shfl_sync(FULL, l, 8 * t + 4 * c);
                 }
             }
+            for (int i = 0; i < live; ++i) {
+                const float ks = __shfl_sync(FULL, ks_l, i);
+                cp_wait<C::SLOTS - 2>();
+                __syncwarp();
+                issue(j + C::SLOTS - 1, slot == 0 ? C::SLOTS - 1 : slot - 1);
+                const uint32_t at = ring_u + (uint32_t)(slot * C::TILE);
+                slot = slot + 1 == C::SLOTS ? 0 : slot + 1;
+                ++j;
+                KeyWords<HD> kw[2];
+                kw[0].load(at, koff, 0);
+                kw[1].load(at, koff, 1);
+                float s[2][NT][4];
+                score<HD, NT, F32, 2>(s, kw, [&](int st, int nt, uint32_t *w) {
 #pragma unroll
-            for (int i = 0; i < C::TT; ++i) {
-                if (i < live) {
-                    const float ks = __shfl_sync(FULL, ks_l, i);
-                    cp_wait<C::SLOTS - 2>();
-                    __syncwarp();
-                    issue(j + C::SLOTS - 1, slot == 0 ? C::SLOTS - 1 : slot - 1);
-                    const uint32_t at = ring_u + (uint32_t)(slot * C::TILE);
-                    slot = slot + 1 == C::SLOTS ? 0 : slot + 1;
-                    ++j;
+                    for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
+                });
+                float v[4] = {0.f, 0.f, 0.f, 0.f};   // token 16 h + row_token(g) + 2 c at v[2 h + c], over this lane's rows
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        KeyWords<HD> kw;
-                        kw.load(at, koff, h);
-                        float sh[1][NT][4];
-                        score<HD, NT, F32, 1>(sh, &kw, [&](int st, int nt, uint32_t *w) {
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-                            for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
-                        });
-                        const float (*s)[4] = sh[0];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            acc[i][h][0] += ex2(fmaf(s[nt][0], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[nt][1], ks * fr[nt][1], -ls[nt][1]));
-                            acc[i][h][1] += ex2(fmaf(s[nt][2], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[nt][3], ks * fr[nt][1], -ls[nt][1]));
-                        }
+                    for (int nt = 0; nt < NT; ++nt) {
+                        v[2 * h] += ex2(fmaf(s[h][nt][0], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[h][nt][1], ks * fr[nt][1], -ls[nt][1]));
+                        v[2 * h + 1] += ex2(fmaf(s[h][nt][2], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[h][nt][3], ks * fr[nt][1], -ls[nt][1]));
                     }
-                }
+                // over the quad by halving exchanges: lane t ends with the total of v[t]
+                const float a0 = (t & 2 ? v[2] : v[0]) + __shfl_xor_sync(FULL, t & 2 ? v[0] : v[2], 2);
+                const float a1 = (t & 2 ? v[3] : v[1]) + __shfl_xor_sync(FULL, t & 2 ? v[1] : v[3], 2);
+                const float sum = (t & 1 ? a1 : a0) + __shfl_xor_sync(FULL, t & 1 ? a0 : a1, 1);
+                red[warp][i * 32 + 16 * (t >> 1) + row_token(g) + 2 * (t & 1)] += sum;   // (a word of its own for every lane)
             }
         }
         cp_wait<0>();
-        // over the quad's row pairs, then over the parallel heads
-#pragma unroll
-        for (int i = 0; i < C::TT; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float v = acc[i][h][c];
-                    v += __shfl_xor_sync(FULL, v, 1);
-                    v += __shfl_xor_sync(FULL, v, 2);
-                    const uint32_t m = __shfl_sync(FULL, seen, i);
-                    const int tok = 16 * h + row_token(g) + 2 * c;
-                    if (t == 0) red[warp][i * 32 + tok] = (m >> tok) & 1 ? v : 0.f;
-                }
+        __syncwarp();
+        for (int k = lane; k < live * 32; k += 32) {   // hidden tokens got nothing
+            const uint32_t m = __shfl_sync(FULL, seen, k >> 5);
+            if (!((m >> lane) & 1)) red[warp][k] = 0.f;
+        }
         __syncthreads();
-        for (int k = threadIdx.x; k < TW * TOK; k += 256) {
-            const int tok = c0 + k, first = k / TOK << hw_log2;
+        for (int k = threadIdx.x; k < TW * tok_w; k += 256) {
+            const int tok = c0 + k, group = k / tok_w, first = group << hw_log2;
             if (tok < len) {
                 float v = 0.f;
-                for (int h = 0; h < HW; ++h) v += red[first + h][k % TOK];
+                for (int h = 0; h < HW; ++h) v += red[first + h][k - group * tok_w];
                 wp[tok] = a.accumulate ? wp[tok] + v : v;
             }
         }
@@ -174,7 +164,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
 
 namespace {
 
-template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Envs &e, int max_len, int grid, cudaStream_t st)
+template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Envs &e, int max_len, int grid, int sms, cudaStream_t st)
 {
     using C = WeighCfg<HD, NT, F32>;
     static bool set[64] = {};
@@ -187,27 +177,34 @@ template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Env
     }
     const int units = a.r.rec.kvh * ((a.r.H * a.r.G + NT * 8 - 1) / (NT * 8));
     const int hw = units >= 8 ? 3 : (units >= 4 ? 2 : (units >= 2 ? 1 : 0));
-    const int n_chunk = (max_len + (C::TT * BLOCK << (3 - hw)) - 1) / (C::TT * BLOCK << (3 - hw));
-    const long long items = (long long)(a.r.meta ? a.r.n_envs : e.n) * n_chunk, cap = grid ? grid : 1 << 20;
-    if (items == 0) return cudaSuccess;
-    return launch_kernel(weigh_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), 256, (size_t)C::SMEM, st, 1, a, e, hw, n_chunk);
+    // Tiles per warp: up to 12, evenly (a head's queries are brought in once for all of them: 4, 8, 12 tiles took 107, 90, 84 us on
+    // 256 x 734 tokens x 16 heads x 16 rows), but fewer where that gives the SMs less than two CTAs each.
+    const int n = a.r.meta ? a.r.n_envs : e.n, TW = 8 >> hw, all = (max_len + BLOCK - 1) / BLOCK, most = (all + TW - 1) / TW;
+    if (n == 0 || all == 0) return cudaSuccess;
+    int n_chunk = (most + MAX_TILES - 1) / MAX_TILES;
+    const int wanted = (2 * (grid ? grid : sms) + n - 1) / n;
+    if (n_chunk < wanted) n_chunk = wanted < most ? wanted : most;
+    const int tiles = (most + n_chunk - 1) / n_chunk;
+    n_chunk = (most + tiles - 1) / tiles;
+    const long long items = (long long)n * n_chunk, cap = grid ? grid : 1 << 20;
+    return launch_kernel(weigh_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), 256, (size_t)C::SMEM, st, 1, a, e, hw, n_chunk, tiles);
 }
 
 // Query rows per product.  Measured, us with 8 / 16 / 32 on 128 x 768 tokens x 16 heads: bf16 of 128, 16 rows 68 / 58 / 87, 32 rows
 // 124 / 97 / 97; bf16 of 64, 32 rows 85 / 66 / 75; fp32 of 64, 16 rows 69 / 61 / 80, 32 rows 125 / 104 / 90, 64 rows 230 / 193 / 161.
-template <int HD> cudaError_t pick(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st)
+template <int HD> cudaError_t pick(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, int sms, cudaStream_t st)
 {
     const int rows = a.r.H * a.r.G;
-    if (rows <= 8) return f32 ? go<HD, 1, true>(a, e, max_len, grid, st) : go<HD, 1, false>(a, e, max_len, grid, st);
-    if (!f32) return go<HD, 2, false>(a, e, max_len, grid, st);
-    return rows <= 16 ? go<HD, 2, true>(a, e, max_len, grid, st) : go<HD, 4, true>(a, e, max_len, grid, st);
+    if (rows <= 8) return f32 ? go<HD, 1, true>(a, e, max_len, grid, sms, st) : go<HD, 1, false>(a, e, max_len, grid, sms, st);
+    if (!f32) return go<HD, 2, false>(a, e, max_len, grid, sms, st);
+    return rows <= 16 ? go<HD, 2, true>(a, e, max_len, grid, sms, st) : go<HD, 4, true>(a, e, max_len, grid, sms, st);
 }
 
 }  // namespace
 
-cudaError_t launch_weigh(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, cudaStream_t st)
+cudaError_t launch_weigh(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, int sms, cudaStream_t st)
 {
-    return a.r.rec.hd == 128 ? pick<128>(a, e, f32, max_len, grid, st) : (a.r.rec.hd == 64 ? pick<64>(a, e, f32, max_len, grid, st) : pick<32>(a, e, f32, max_len, grid, st));
+    return a.r.rec.hd == 128 ? pick<128>(a, e, f32, max_len, grid, sms, st) : (a.r.rec.hd == 64 ? pick<64>(a, e, f32, max_len, grid, sms, st) : pick<32>(a, e, f32, max_len, grid, sms, st));
 }
 
 }  // namespace p8
