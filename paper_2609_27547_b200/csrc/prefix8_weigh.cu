@@ -190,14 +190,17 @@ template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Env
     return launch_kernel(weigh_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), 256, (size_t)C::SMEM, st, 1, a, e, hw, n_chunk, tiles);
 }
 
-// Query rows per product.  Measured, us with 8 / 16 / 32 on 128 x 768 tokens x 16 heads: bf16 of 128, 16 rows 68 / 58 / 87, 32 rows
-// 124 / 97 / 97; bf16 of 64, 32 rows 85 / 66 / 75; fp32 of 64, 16 rows 69 / 61 / 80, 32 rows 125 / 104 / 90, 64 rows 230 / 193 / 161.
+// Query rows per product, from the call's rows, head and type alone, so that a batch's other lengths change no bits.  Measured,
+// us with 8 / 16 / 32 on 128 x 768 tokens x 16 heads (two CTAs per SM but for 32 rows and the fp32 forms that hold no more than
+// one): bf16 of 128, 8 rows 48 / 52 / 81, 16 rows 62 / 56 / 87, 32 rows 112 / 89 / 96; bf16 of 64, 8 rows 30 / 36 / 61, 32 rows
+// 90 / 66 / 77.  fp32 of 128, 8 rows 60 / 73 / 118, 32 rows 183 / 135 / 138.  fp32 of 64 (and of 32 alike), 8 rows 34 / 54 / 76, 32
+// rows 101 / 104 / 91 (512 x 64 tokens: 54 / 73 / 70), 64 rows 189 / 194 / 164 (97 / 129 / 122): one size for them all.
 template <int HD> cudaError_t pick(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, int sms, cudaStream_t st)
 {
     const int rows = a.r.H * a.r.G;
-    if (rows <= 8) return f32 ? go<HD, 1, true>(a, e, max_len, grid, sms, st) : go<HD, 1, false>(a, e, max_len, grid, sms, st);
-    if (!f32) return go<HD, 2, false>(a, e, max_len, grid, sms, st);
-    return rows <= 16 ? go<HD, 2, true>(a, e, max_len, grid, sms, st) : go<HD, 4, true>(a, e, max_len, grid, sms, st);
+    if (f32 && (HD < 128 || rows <= 8)) return go<HD, 1, true>(a, e, max_len, grid, sms, st);
+    if (f32) return go<HD, HD < 128 ? 1 : 2, true>(a, e, max_len, grid, sms, st);
+    return rows <= 8 ? go<HD, 1, false>(a, e, max_len, grid, sms, st) : go<HD, 2, false>(a, e, max_len, grid, sms, st);
 }
 
 }  // namespace
