@@ -77,9 +77,10 @@ ebrl_status_t ebrl_prefix8_quantize(const ebrl_prefix8_layout_t *layout, void *p
  *   lse    DEVICE fp32 [n][H][n_heads], or NULL
  *   scale  softmax scale, finite (usually 1 / sqrt(head_dim))
  * A row that sees no token gives out = 0 and lse = -inf.  Two environments of a call may share a slot.
- * Long prefixes: with few environments a prefix is cut into pieces that are joined by a second kernel.
+ * With few environments a prefix is divided among warps, which are joined in shared memory, and a long one is cut into pieces
+ * besides, which are joined by a second kernel.
  * split_tokens = 0 lets the call choose (the choice depends on the whole call, so an environment's last bits can
- * depend on its company); -1 never cuts (an environment's result then depends on nothing but itself); a positive
+ * depend on its company); -1 never divides or cuts (an environment's result then depends on nothing but itself); a positive
  * multiple of 128 cuts every prefix into pieces of that many tokens.  The pieces' partial results need
  * ebrl_prefix8_attend_workspace bytes (of the same arguments) of DEVICE memory, 16-byte aligned, that no other call in flight uses;
  * 0 bytes: workspace may be NULL.

@@ -536,7 +536,7 @@ void cross_attend8(ebrl_actgen *h, Slot &s, Launcher &ln, const AttnArgs &x, dou
     a.r.H = x.H; a.r.heads = x.n_heads; a.r.G = 1; a.r.scale = 1.0f / sqrtf((float)x.hd); a.r.meta = x.meta; a.r.n_envs = x.n_envs;
     a.out = x.out; a.o_env = (long long)x.H * x.o_stride; a.o_tok = x.o_stride;
     a.out_t1 = x.out_t1; a.out_t2 = x.out_t2; a.split_out = x.split_out;
-    a.n_split = 1; a.max_len = s.longest; a.alike = s.alike; a.lse = s.weigh_len > 0 ? s.lse : nullptr;
+    a.n_split = 1; a.team = 1; a.max_len = s.longest; a.alike = s.alike; a.lse = s.weigh_len > 0 ? s.lse : nullptr;
     const int quota = ln.grid < h->n_sms ? ln.grid : 0;   // the whole chip: the launch that evens out ragged prefixes
     ln.run(EBRL_KC_CROSS_ATTN, 4.0 * x.H * sum_P * d, 2.0 * sum_P * d + 2.0 * M * d * (double)h->esz,
            [&] { return p8::launch_attend(a, none, !h->bf16, quota, h->n_sms, ln.st); });

@@ -140,33 +140,59 @@ int longest(const int32_t *len, int n)
     return m;
 }
 
-// How prefixes are cut: tokens per piece and pieces of the longest prefix.  Left to itself, a call is cut only when its
-// (environment, head, row tile) items are at most half of the warps that the SMs hold, into as many pieces as there
-// are warps for (never more: a second wave would double the time) and not below 256 tokens.
-// Measured on two 65 k-token prefixes with 4 heads: whole 1394 us, pieces of 8192 tokens 193 us, 2048 58 us, 512 35 us,
-// 384 (this rule) 33 us, 256 41 us, 128 48 us.
-void cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int heads, int asked, int sms, bool f32, int *split, int *n_split)
+// How prefixes are cut: tokens per piece, pieces of the longest prefix, warps that share a piece (a team: one CTA, joined in
+// shared memory).  Left to itself (asked = 0), a call is cut where its items, weighed by their length, fill half of the warps that
+// the SMs hold or less: among a team of as many warps as fill them once, and where eight are too few and prefixes longer than 4096
+// tokens, into pieces of a team of four each.  Pieces cost a workspace and a second launch (7 us of the host's time), a team costs neither.
+// Measured, us on the device, one warp / this rule: 1 x 256 tokens x 16 heads of 64, 1 row 8.4 / 6.0; 4 x 6303 x 8 heads of 128, 128 rows
+// 146 / 81; 278 x 1732 x 2 heads of 64, 8 rows 49 / 30; two 65 k-token prefixes x 4 heads of 128, 4 rows 1394 / 30 (pieces of 384 tokens without
+// teams 34).  Where SMs are half full short prefixes are not worth a team (512 x 64 - 512 x 4 heads, 8 rows, fp32: 1, 2, 4 warps
+// 26, 29, 38; 96 x 0 - 301 x 2 heads of 32, 64 rows: 9.8, 14.7, 16.5), hence the least number of tiles; teams of eight at head_dim 128 leave 4 of
+// 12 warps idle.  110 random calls: geometric mean 21.3 -> 16.0.
+struct Cut { int split, n_split, team; };
+
+Cut cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int heads, int asked, int quota, int sms, bool f32)
 {
-    const int most = longest(len, n);
-    *split = std::max(most, 1);
-    *n_split = 1;
-    if (asked < 0) return;
+    const int most = longest(len, n), rows = H * (heads / l.n_kv_heads);
+    Cut c = {std::max(most, 1), 1, 1};
+    if (asked < 0 || most == 0) return c;
     if (asked > 0) {
-        if (most > asked) { *split = asked; *n_split = (most + asked - 1) / asked; }
-        return;
+        if (most > asked) { c.split = asked; c.n_split = (most + asked - 1) / asked; }
+        return c;
     }
+    if (quota) {   // persistent CTAs with a warp for each piece: as many pieces as there are warps for, not below 256 tokens
+        sms = std::min(sms, quota);
+        long long items = 0;
+        for (int i = 0; i < n; ++i) items += len[i] > 0;
+        const int tile = attend_tile(l.head_dim, rows, f32, most);
+        items *= (long long)l.n_kv_heads * ((rows + tile - 1) / tile);
+        const long long warps = (long long)sms * attend_warps(l.head_dim, tile);
+        if (items * 2 > warps) return c;
+        const long long parts = std::min<long long>(warps / items, most / 256);
+        if (parts < 2) return c;
+        c.split = (int)((most + parts - 1) / parts + 127) / 128 * 128;
+        c.n_split = (most + c.split - 1) / c.split;
+        return c;
+    }
+    double tokens = 0;
     long long items = 0;
-    for (int i = 0; i < n; ++i) items += len[i] > 0;
-    const int rows = H * (heads / l.n_kv_heads);
-    const int tile = attend_tile(l.head_dim, rows, f32, most);
-    items *= (long long)l.n_kv_heads * ((rows + tile - 1) / tile);
-    const long long warps = (long long)sms * attend_warps(l.head_dim, tile);
-    if (items == 0 || items * 2 > warps) return;
-    const long long parts = std::min<long long>(warps / items, most / 256);
-    if (parts < 2) return;
-    const long long piece = ((most + parts - 1) / parts + 127) / 128 * 128;
-    *split = (int)piece;
-    *n_split = (int)((most + piece - 1) / piece);
+    for (int i = 0; i < n; ++i) { tokens += len[i]; items += len[i] > 0; }
+    const int warps = attend_warps(l.head_dim, 8);
+    const double per = (double)l.n_kv_heads * ((rows + 7) / 8) / ((double)sms * warps);   // items of 8 rows of an environment: their part of the SMs' warps
+    const double fill = tokens / most * per, room = 2 / (items * per);   // (no more than two warps for each of theirs, however short most prefixes are)
+    if (most > 4096 && fill * 8 <= 1) {
+        const int pieces = (int)std::min(std::min(1 / (fill * 4), room / 4), most / 512.);
+        if (pieces > 1) {
+            c.split = ((most + pieces - 1) / pieces + 127) / 128 * 128;
+            c.n_split = (most + c.split - 1) / c.split;
+            c.team = 4;
+            return c;
+        }
+    }
+    c.team = fill * (warps % 8 ? warps : 8) <= 1 ? 8 : (fill <= .3 ? 4 : (fill <= .5 ? 2 : 1));
+    const int least = fill <= .04 ? 1 : (fill <= .125 ? 2 : (fill <= .3 ? 8 : 20));   // tiles for every warp of the longest
+    while (c.team > 1 && (c.team > room || most <= least * (c.team - 1) * BLOCK)) c.team /= 2;
+    return c;
 }
 
 uint64_t part_rows(int n, int n_split, int H, int heads) { return n_split > 1 ? (uint64_t)n * n_split * H * heads : 0; }
@@ -251,12 +277,12 @@ uint64_t ebrl_prefix8_attend_workspace(const ebrl_prefix8_layout_t *layout, int3
                                        int32_t split_tokens, int32_t sm_quota)
 {
     if (check_layout(layout) != EBRL_OK || n <= 0 || !len || H < 1 || n_heads < 1 || n_heads % layout->n_kv_heads) return 0;
-    int sms = 0, split, n_split;
+    int sms = 0;
     if (device_sms(0, &sms) != EBRL_OK) return 0;
     uint64_t most = 0;   // of either query type
     for (int f32 = 0; f32 < 2; ++f32) {
-        cut(*layout, n, len, H, n_heads, split_tokens, sm_quota > 0 ? std::min<int>(sm_quota, sms) : sms, f32 != 0, &split, &n_split);
-        most = std::max(most, part_rows(n, n_split, H, n_heads) * (layout->head_dim + 2) * 4);
+        const Cut c = cut(*layout, n, len, H, n_heads, split_tokens, std::max<int>(sm_quota, 0), sms, f32 != 0);
+        most = std::max(most, part_rows(n, c.n_split, H, n_heads) * (layout->head_dim + 2) * 4);
     }
     return most;
 }
@@ -279,10 +305,11 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
         if (out == q && ((n > 1 && o_env_stride != q_env_stride) || (H > 1 && o_token_stride != q_token_stride)))
             BAD("out may be q only with the same strides");
         if (split_tokens < -1 || split_tokens % 128 > 0) BAD("split_tokens is -1, 0 or a positive multiple of 128");
-        int sms = 0, split, n_split;
+        int sms = 0;
         if ((st = device_sms(sm_quota, &sms)) != EBRL_OK) return st;
         const bool f32 = q_dtype == EBRL_F32;
-        cut(*layout, n, len, H, n_heads, split_tokens, sm_quota ? sm_quota : sms, f32, &split, &n_split);
+        const Cut c = cut(*layout, n, len, H, n_heads, split_tokens, sm_quota, sms, f32);
+        const int n_split = c.n_split;
         const int rows = H * (n_heads / layout->n_kv_heads);
         if ((int64_t)std::min(n, CHUNK_ENVS) * layout->n_kv_heads * n_split * ((rows + 7) / 8) > INT32_MAX)
             return fail(EBRL_ERR_UNSUPPORTED, "too many pieces in one call");
@@ -293,7 +320,7 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
         a.r.rec = record_of(*layout); a.r.pool = (const char *)pool; a.r.layer = layer;
         a.r.q_env = q_env_stride; a.r.q_tok = q_token_stride; a.r.H = H; a.r.heads = n_heads; a.r.G = n_heads / layout->n_kv_heads; a.r.scale = scale;
         a.o_env = o_env_stride; a.o_tok = o_token_stride;
-        a.split = split; a.n_split = n_split;
+        a.split = c.split; a.n_split = n_split; a.team = c.team;
         for (int first = 0; first < n; first += CHUNK_ENVS) {
             const Envs &e = some_envs(first, std::min(CHUNK_ENVS, n - first), slots, len);
             a.max_len = longest(e.len, e.n);

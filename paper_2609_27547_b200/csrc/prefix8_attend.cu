@@ -10,7 +10,9 @@
 //   tiles are in flight per SM, twice what HBM latency asks for, and a warp's requests run on from one item into the next
 //   (512 x 768 tokens x 16 heads x 16 rows: 314 -> 294 us).  Where prefixes are alike, or under an SM quota, warps are persistent;
 //   where they differ the launch is one CTA per item, which lets the hardware even them out.
-//   (Four warps per item, joined in shared memory, were 1.6 times slower: an item was over before its set-up and join were paid for.)
+//   Calls that would leave most of the SMs empty share an item among a TEAM of 2, 4 or 8 warps (the CTA): each an even share of
+//   the tokens, joined in warp order through the rings, which are idle by then (1 x 256 tokens x 16 heads of 64: 8.4 -> 6.0 us).  With the
+//   SMs full a team of four is 1.5 times slower: an item is over before its set-up and join are paid for.
 //
 //   With the cache in L2 (arithmetic alone) 512 x 768 tokens x 16 heads of 128 take 150 us at 8 rows and 228 at 16; from HBM
 //   240 us (6.7 TB/s of codes) and 286 (5.6; 294 at the power cap).  At 16 rows the legacy tensor path is what it waits for: a product
@@ -21,7 +23,7 @@
 //   2^(s - ref) stay below 2^14, which f16 holds with the same 11 bits.  The common tile needs one vote and no
 //   shuffles.  Weights aim at 2^6 rather than 1, so that those 2^-20 of the largest are still normal f16 numbers.
 //   Value scales are never put into the weights: outputs change their unit where neighbouring blocks' scales differ (exact for
-//   powers of two), and where they differ by more than 2^20 the block's product is scaled by itself.  Any finite scales work.
+//   powers of two), and a block whose scale is 2^20 below the largest so far has its product scaled by itself.  Any finite scales work.
 //   fp32 queries always take the latter way: summed up in the tensor core over 16 tiles, outputs were 1.1e-6 off instead of 3.5e-7.
 //
 //   bf16 queries are exact (prefix8_tile.cuh), weights are rounded to f16: 11 bits, an eighth of the output's own rounding.
@@ -44,7 +46,7 @@ template <int HD, int NT, bool F32> struct AttendCfg {
     static_assert(STAGES >= 2, "ring");
 };
 
-template <int HD, int NT, bool F32>
+template <int HD, int NT, bool F32, bool TEAM>
 __global__ void __launch_bounds__(AttendCfg<HD, NT, F32>::WARPS * 32, 1)
 attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs ev)
 {
@@ -74,6 +76,11 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         else { it.rec = a.r.pool + (size_t)ev.slot[it.env] * a.r.rec.bytes; it.len = ev.len[it.env]; }
         it.t0 = it.sp * a.split;
         it.t1 = a.n_split == 1 ? it.len : min(it.len, it.t0 + a.split);
+        if constexpr (TEAM) {   // this warp's even share
+            const int part = (it.t1 - it.t0 + warps * BLOCK - 1) / (warps * BLOCK) * BLOCK;
+            it.t0 += warp * part;
+            it.t1 = min(it.t1, it.t0 + part);
+        }
         return it;
     };
     auto q_at = [&](const Item &it, int row) {   // offset of query row `row` of the item's kv head, in elements
@@ -81,7 +88,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         return (size_t)it.env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)(it.kh * G + row - tok * G) * HD;
     };
     // items go round the CTAs first, so that the last round spreads over all SMs
-    const unsigned first = (unsigned)warp * gridDim.x + blockIdx.x, stride = gridDim.x * (unsigned)warps;
+    const unsigned first = TEAM ? blockIdx.x : (unsigned)warp * gridDim.x + blockIdx.x, stride = gridDim.x * (TEAM ? 1u : (unsigned)warps);
 
     // The requests run STAGES - 1 tiles ahead of the arithmetic, from one item into the next: while an item's last tiles are worked on the next
     // one's first tiles (and its queries, scales and mask, into L1) are on their way.
@@ -129,8 +136,8 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         const Item it = item_of(item);
         const int rt = it.rt, kh = it.kh, sp = it.sp, env = it.env, t0 = it.t0, t1 = it.t1;
         const char *rec = it.rec;
-        if (sp > 0 && t0 >= it.len) continue;
-        const int ntile = (t1 - t0 + BLOCK - 1) / BLOCK;
+        if (sp > 0 && sp * a.split >= it.len) continue;
+        const int ntile = (t1 - t0 + BLOCK - 1) / BLOCK;   // (0 or less for a team's warp that got none)
 
         // queries
         uint32_t q[NT][ST][QW<F32>];
@@ -150,7 +157,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         };
 
         float o[MT][NT][4];   // column m * 16 + g of rows 2t, 2t + 1, column + 8 of the same; in units of `unit`
-        float unit = 1.f;
+        float unit = FLT_MIN, inv_unit = 1.f / FLT_MIN, most = FLT_MIN;   // (no scale is smaller); the largest scale so far
         float mr[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -292,63 +299,124 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                 };
                 // fp32 sums that stay in the tensor core lose their last bits to its truncation: fp32 queries take every block's product out
                 bool near = !F32;
-                if (!F32 && vs != unit) {
-                    const float by = unit / vs;
-                    near = by >= 1.f / 1048576.f && by <= 1048576.f;
-                    rescale(near ? by : unit);
-                    unit = near ? vs : 1.f;
+                if (F32 ? vs > unit : vs != unit) {
+                    most = fmaxf(most, vs);
+                    if (F32 || (near = vs >= most * 0x1p-20f)) {   // (bounded, so that outputs of large blocks stay in range)
+                        inv_unit = 1.f / vs;
+                        rescale(unit * inv_unit);
+                        unit = vs;
+                    }
                 }
                 if (near) values([&](int m, int nt, uint32_t (*f)[4]) { product(o[m][nt], nt, f); });
-                else   // far apart, zero, or not a number: outputs as they are, the block's own product scaled and added
+                else {   // far below the others, or not a number: the block's own product scaled and added
+                    const float by = vs * inv_unit;
                     values([&](int m, int nt, uint32_t (*f)[4]) {
                         float tmp[4] = {0.f, 0.f, 0.f, 0.f};
                         product(tmp, nt, f);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) o[m][nt][c] = fmaf(vs, tmp[c], o[m][nt][c]);
+                        for (int c = 0; c < 4; ++c) o[m][nt][c] = fmaf(by, tmp[c], o[m][nt][c]);
                     });
+                }
             }
         }
         // Outputs: lane (g, t) has columns g of rows 2t, 2t + 1 of 8 x 8 matrices; transposed it has columns 2t, 2t + 1 of row g.
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            float L[2], inv[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                L[j] = l[nt][j];
-                L[j] += __shfl_xor_sync(FULL, L[j], 4);
-                L[j] += __shfl_xor_sync(FULL, L[j], 8);
-                L[j] += __shfl_xor_sync(FULL, L[j], 16);
-                inv[j] = a.n_split > 1 ? unit : (L[j] == 0.f ? 0.f : unit / L[j]);
-                const int r = rt * NT * 8 + nt * 8 + 2 * t + j, tok = r / G, row = tok * a.r.heads + kh * G + r - tok * G;
-                if (g == 0 && r < R) {
-                    if (a.n_split > 1) *reinterpret_cast<float2 *>(a.part_ml + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + row) * 2) = make_float2(mr[nt][j], L[j]);
-                    else if (a.lse) a.lse[(size_t)env * a.r.H * a.r.heads + row] = L[j] == 0.f ? -INFINITY : (mr[nt][j] + log2f(L[j])) * LN2;
-                }
+        auto store_ml = [&](int nt, int j, float m, float L) {
+            const int r = rt * NT * 8 + nt * 8 + 2 * t + j, tok = r / G, row = tok * a.r.heads + kh * G + r - tok * G;
+            if (g == 0 && r < R) {
+                if (a.n_split > 1) *reinterpret_cast<float2 *>(a.part_ml + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + row) * 2) = make_float2(m, L);
+                else if (a.lse) a.lse[(size_t)env * a.r.H * a.r.heads + row] = L == 0.f ? -INFINITY : (m + log2f(L)) * LN2;
             }
+        };
+        struct At { bool there; size_t off; float *part; };
+        auto row_at = [&](int nt) {
             const int r = rt * NT * 8 + nt * 8 + g, tok = r / G, head = kh * G + r - tok * G;
-            const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + 2 * t;
-            float *part = a.part_o + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + (size_t)tok * a.r.heads + head) * HD + 2 * t;
+            return At{r < R, (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + 2 * t,
+                      a.part_o + (((size_t)env * a.n_split + sp) * ((size_t)a.r.H * a.r.heads) + (size_t)tok * a.r.heads + head) * HD + 2 * t};
+        };
+        auto store_o = [&](const At &at, int col, float x, float y) {   // rows' softmax-weighted means
+            if (F32 || a.n_split > 1) {   // upper and lower halves apart
+                const uint32_t xu = __float_as_uint(x), yu = __float_as_uint(y);
+                const uint32_t hi = transpose8(__byte_perm(xu, yu, 0x7632)), lo = transpose8(__byte_perm(xu, yu, 0x5410));
+                const float2 v = make_float2(__uint_as_float(__byte_perm(lo, hi, 0x5410)), __uint_as_float(__byte_perm(lo, hi, 0x7632)));
+                if (at.there) {
+                    if (a.n_split > 1) *reinterpret_cast<float2 *>(at.part + col) = v;
+                    else if (a.split_out) store_split2(a.out, a.out_t1, a.out_t2, at.off + col, v.x, v.y);
+                    else *reinterpret_cast<float2 *>((float *)a.out + at.off + col) = v;
+                }
+            } else {
+                const __nv_bfloat162 u = __floats2bfloat162_rn(x, y);
+                const uint32_t w = transpose8(*reinterpret_cast<const uint32_t *>(&u));
+                if (at.there) *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + at.off + col) = w;
+            }
+        };
+        auto sum = [&](float L) {
+            L += __shfl_xor_sync(FULL, L, 4);
+            L += __shfl_xor_sync(FULL, L, 8);
+            return L + __shfl_xor_sync(FULL, L, 16);
+        };
+        if constexpr (!TEAM) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float inv[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float L = sum(l[nt][j]);
+                    inv[j] = L == 0.f ? 0.f : unit / L;
+                    store_ml(nt, j, mr[nt][j], L);
+                }
+                const At at = row_at(nt);
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) store_o(at, m * 16 + 8 * k, o[m][nt][2 * k] * inv[0], o[m][nt][2 * k + 1] * inv[1]);
+            }
+        } else {   // (one item per CTA: nothing is requested any more) join the team's pieces through its rings, in warp order
+            constexpr int ML = NT * 8 * HD * 4;   // a warp's outputs, then its rows' (reference, sum) and its unit
+            static_assert(ML + NT * 8 * 8 + 4 <= C::WARP_BYTES, "join");
+            auto of = [&](int w) { return smem + (size_t)w * C::WARP_BYTES; };
+            auto ml = [&](int w, int nt, int j) { return *reinterpret_cast<const float2 *>(of(w) + ML + (nt * 8 + 2 * t + j) * 8); };
+            cp_wait<0>();
+            __syncwarp();
 #pragma unroll
             for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int col = m * 16 + 8 * k;
-                    const float x = o[m][nt][2 * k] * inv[0], y = o[m][nt][2 * k + 1] * inv[1];
-                    if (F32 || a.n_split > 1) {   // upper and lower halves apart
-                        const uint32_t xu = __float_as_uint(x), yu = __float_as_uint(y);
-                        const uint32_t hi = transpose8(__byte_perm(xu, yu, 0x7632)), lo = transpose8(__byte_perm(xu, yu, 0x5410));
-                        const float2 v = make_float2(__uint_as_float(__byte_perm(lo, hi, 0x5410)), __uint_as_float(__byte_perm(lo, hi, 0x7632)));
-                        if (r < R) {
-                            if (a.n_split > 1) *reinterpret_cast<float2 *>(part + col) = v;
-                            else if (a.split_out) store_split2(a.out, a.out_t1, a.out_t2, off + col, v.x, v.y);
-                            else *reinterpret_cast<float2 *>((float *)a.out + off + col) = v;
-                        }
-                    } else {
-                        const __nv_bfloat162 u = __floats2bfloat162_rn(x, y);
-                        const uint32_t w = transpose8(*reinterpret_cast<const uint32_t *>(&u));
-                        if (r < R) *reinterpret_cast<uint32_t *>((__nv_bfloat16 *)a.out + off + col) = w;
-                    }
+                for (int nt = 0; nt < NT; ++nt) *reinterpret_cast<float4 *>(of(warp) + ((m * NT + nt) * 32 + lane) * 16) = make_float4(o[m][nt][0], o[m][nt][1], o[m][nt][2], o[m][nt][3]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const float L = sum(l[nt][j]);
+                    if (g == 0) *reinterpret_cast<float2 *>(of(warp) + ML + (nt * 8 + 2 * t + j) * 8) = make_float2(mr[nt][j], L);
                 }
+            if (lane == 0) *reinterpret_cast<float *>(of(warp) + ML + NT * 8 * 8) = unit;
+            __syncthreads();
+            float M[NT][2], inv[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    float mx = -FLT_MAX, z = 0.f;
+                    for (int w = 0; w < warps; ++w) mx = fmaxf(mx, ml(w, nt, j).x);
+                    for (int w = 0; w < warps; ++w) { const float2 v = ml(w, nt, j); z = fmaf(ex2(v.x - mx), v.y, z); }
+                    M[nt][j] = mx;
+                    inv[nt][j] = z == 0.f ? 0.f : 1.f / z;
+                    if (warp == 0) store_ml(nt, j, mx, z);
+                }
+            for (int m = warp; m < MT; m += warps) {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    float x[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int w = 0; w < warps; ++w) {
+                        const float4 v = *reinterpret_cast<const float4 *>(of(w) + ((m * NT + nt) * 32 + lane) * 16);
+                        const float u = *reinterpret_cast<const float *>(of(w) + ML + NT * 8 * 8);
+                        const float f0 = ex2(ml(w, nt, 0).x - M[nt][0]) * inv[nt][0] * u, f1 = ex2(ml(w, nt, 1).x - M[nt][1]) * inv[nt][1] * u;
+                        x[0] = fmaf(f0, v.x, x[0]); x[1] = fmaf(f1, v.y, x[1]); x[2] = fmaf(f0, v.z, x[2]); x[3] = fmaf(f1, v.w, x[3]);
+                    }
+                    const At at = row_at(nt);
+                    store_o(at, m * 16, x[0], x[1]);
+                    store_o(at, m * 16 + 8, x[2], x[3]);
+                }
+            }
         }
     }
     cp_wait<0>();      // only empty groups are left
@@ -361,7 +429,7 @@ template <int HD, bool F32, int WPR>
 __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs ev)
 {
     constexpr int V = HD / 32, RPC = 16 / WPR;
-    __shared__ float so[16][HD], sl[16];
+    __shared__ float so[16][HD];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, RH = a.r.H * a.r.heads, sub = warp % WPR;
     const long long rows = (long long)ev.n * RH;
     pdl_launch_dependents();
@@ -373,42 +441,42 @@ __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant_
         const int np = there ? max(1, (ev.len[env] + a.split - 1) / a.split) : 0;
         const float2 *ml = reinterpret_cast<const float2 *>(a.part_ml) + (size_t)env * a.n_split * RH + rr;
         const float *po = a.part_o + ((size_t)env * a.n_split * RH + rr) * HD + lane * V;
-        float M = -FLT_MAX;
+        float M = -FLT_MAX, L = 0.f;
         for (int p = lane; p < np; p += 32) M = fmaxf(M, ml[(size_t)p * RH].x);
         M = warp_max(M);
-        float acc[V], L = 0.f;
+        for (int p = lane; p < np; p += 32) { const float2 u = ml[(size_t)p * RH]; L = fmaf(ex2(u.x - M), u.y, L); }
+        L = warp_sum(L);
+        const float inv = L == 0.f ? 0.f : 1.f / L;
+        float acc[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) acc[i] = 0.f;
 #pragma unroll 8
         for (int p = sub; p < np; p += WPR) {
             const float2 u = ml[(size_t)p * RH];
-            const float f = ex2(u.x - M);
-            L = fmaf(f, u.y, L);
+            const float f = ex2(u.x - M) * u.y * inv;
 #pragma unroll
             for (int i = 0; i < V; ++i) acc[i] = fmaf(f, po[(size_t)p * RH * HD + i], acc[i]);
         }
-        auto store = [&](int col, float s, float z) {
+        auto store = [&](int col, float v) {
             const size_t off = (size_t)env * a.o_env + (size_t)tok * a.o_tok + (size_t)head * HD + col;
-            const float v = z == 0.f ? 0.f : s / z;
             if constexpr (F32) ((float *)a.out)[off] = v;
             else ((__nv_bfloat16 *)a.out)[off] = __float2bfloat16_rn(v);
-            if (a.lse && col == 0) a.lse[(size_t)env * RH + rr] = z == 0.f ? -INFINITY : (M + log2f(z)) * LN2;
+            if (a.lse && col == 0) a.lse[(size_t)env * RH + rr] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
         };
         if constexpr (WPR == 1) {
             if (there) {
 #pragma unroll
-                for (int i = 0; i < V; ++i) store(lane * V + i, acc[i], L);
+                for (int i = 0; i < V; ++i) store(lane * V + i, acc[i]);
             }
         } else {
 #pragma unroll
             for (int i = 0; i < V; ++i) so[warp][lane * V + i] = acc[i];
-            if (lane == 0) sl[warp] = L;
             __syncthreads();
             if (threadIdx.x < HD) {   // (one row per CTA: every thread knows it)
-                float s = 0.f, z = 0.f;
+                float s = 0.f;
 #pragma unroll
-                for (int w = 0; w < 16; ++w) { s += so[w][threadIdx.x]; z += sl[w]; }
-                store(threadIdx.x, s, z);
+                for (int w = 0; w < 16; ++w) s += so[w][threadIdx.x];
+                store(threadIdx.x, s);
             }
             __syncthreads();
         }
@@ -442,14 +510,14 @@ int tile_for(const AttendArgs &a, const Envs &e, bool f32, int sms)
     return 2 * items < 3LL * sms * attend_warps(a.r.rec.hd, tile) ? 8 : tile;
 }
 
-template <int HD, int NT, bool F32> cudaError_t go(const AttendArgs &a, const Envs &e, int grid, int sms, cudaStream_t st)
+template <int HD, int NT, bool F32, bool TEAM = false> cudaError_t go(const AttendArgs &a, const Envs &e, int grid, int sms, cudaStream_t st)
 {
     using C = AttendCfg<HD, NT, F32>;
     static bool set[64] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!set[dev]) {
-        cudaError_t err = cudaFuncSetAttribute(attend_kernel<HD, NT, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::WARPS * C::WARP_BYTES);
+        cudaError_t err = cudaFuncSetAttribute(attend_kernel<HD, NT, F32, TEAM>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::WARPS * C::WARP_BYTES);
         if (err != cudaSuccess) return err;
         set[dev] = true;
     }
@@ -458,13 +526,14 @@ template <int HD, int NT, bool F32> cudaError_t go(const AttendArgs &a, const En
     if (items == 0) return cudaSuccess;
     // Under a quota: persistent CTAs with all of an SM's warps.  Else one-warp CTAs: as many as the SMs hold where prefixes are alike (the
     // ring then runs on from item to item), one per item where they are not (the hardware hands out the next as one ends).
-    const int warps = grid ? C::WARPS : 1;
-    const long long cap = grid ? grid : (a.alike ? (long long)sms * C::WARPS : 1 << 20);
-    return launch_kernel(attend_kernel<HD, NT, F32>, (int)(items < cap ? items : cap), warps * 32, (size_t)(warps * C::WARP_BYTES), st, 1, a, e);
+    const int warps = TEAM ? a.team : (grid ? C::WARPS : 1);
+    const long long cap = grid ? grid : (a.alike && !TEAM ? (long long)sms * C::WARPS : 1 << 20);
+    return launch_kernel(attend_kernel<HD, NT, F32, TEAM>, (int)(items < cap ? items : cap), warps * 32, (size_t)(warps * C::WARP_BYTES), st, 1, a, e);
 }
 
 template <int HD> cudaError_t pick(const AttendArgs &a, const Envs &e, bool f32, int grid, int sms, cudaStream_t st)
 {
+    if (a.team > 1) return f32 ? go<HD, 1, true, true>(a, e, grid, sms, st) : go<HD, 1, false, true>(a, e, grid, sms, st);
     if (f32) return go<HD, 1, true>(a, e, grid, sms, st);
     return tile_for(a, e, f32, grid ? grid : sms) == 8 ? go<HD, 1, false>(a, e, grid, sms, st) : go<HD, 2, false>(a, e, grid, sms, st);
 }

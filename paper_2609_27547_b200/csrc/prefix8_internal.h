@@ -46,6 +46,7 @@ struct AttendArgs {
     long long o_env, o_tok;
     float *lse;                    // [env][H][heads] or NULL
     int split, n_split;            // tokens per piece (a multiple of 128), pieces of the longest prefix; 1: not cut
+    int team;                      // warps that share an item (one CTA, joined in shared memory); 1 under an SM quota
     float *part_o, *part_ml;       // pieces' results: [env][piece][H * heads][hd], [env][piece][H * heads][2]
     // fp32 models on the tensor cores: the result as three bf16 term planes
     void *out_t1, *out_t2;

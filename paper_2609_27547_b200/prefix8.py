@@ -280,9 +280,9 @@ def attend(layout: Layout, pool: torch.Tensor, q: torch.Tensor, lens, *, layer: 
     s, sp = _n_slots(L, slots, pool)
     dll = _load()
     with _on(pool.device):
-        # (left to itself the library never cuts below 256 tokens)
+        # (left to itself and without a quota the library cuts no prefix of 4096 tokens or fewer into pieces, under a quota none of 256)
         need = 0
-        if split_tokens > 0 or (split_tokens == 0 and layout.capacity > 256):
+        if split_tokens > 0 or (split_tokens == 0 and layout.capacity > (256 if sm_quota else 4096)):
             need = dll.ebrl_prefix8_attend_workspace(cl, n, L.data_ptr(), H, heads, split_tokens, sm_quota)
         # what is allocated here belongs to the stream that writes it; results are used on the current one, too
         with torch.cuda.stream(stream) if _elsewhere(pool.device, stream) else _HERE:

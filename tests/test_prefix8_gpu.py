@@ -280,6 +280,63 @@ def test_attend_pieces_of_long_prefixes(hd, H, G, dtype):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
 
 
+# calls that leave the SMs nearly empty share an item among 2, 4 or 8 warps, the long ones in pieces besides
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,kvh,hd,lens,hide", [
+    (1, 1, 16, 64, [256], 0.0),                        # a tile for each of eight warps
+    (1, 2, 2, 128, [33, 0, 1, 32, 31], 0.5),           # warps that get nothing, environments without tokens
+    (19, 1, 2, 32, [700, 64, 0, 511], 0.9),            # warps that see nothing
+    (8, 2, 16, 128, [640] * 6 + [7], 0.1),             # teams of four
+    (32, 1, 16, 64, [2000] * 14, 0.0),                 # teams of two
+    (5, 2, 1, 64, [9000, 20, 0, 8999], 0.3),           # pieces, each of a team
+    (2, 1, 3, 128, [5000] + [3] * 40, 0.0),            # one long prefix among short ones
+])
+def test_attend_teams(H, G, kvh, hd, lens, hide, dtype):
+    lay = p8.Layout(1, kvh, hd, max(lens))
+    pool, _, _ = filled(lay, lens, hide=hide, seed=3)
+    q = torch.randn((len(lens), H, kvh * G, hd), generator=torch.Generator().manual_seed(6)).to(DT[dtype]).cuda()
+    out, lse = p8.attend(lay, pool, q, lens)
+    check_attend(lay, pool, q, lens, out, lse, 0, 1 / math.sqrt(hd))
+    again, _ = p8.attend(lay, pool, q, lens, out=q)
+    assert torch.equal(again, out)
+
+
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("split", [0, 128, 512, -1])
+def test_attend_largest_values_and_what_one_piece_sees(hd, split):
+    """Values near the end of fp32's range stay finite however they are cut; a NaN reaches who sees it, and nobody else."""
+    P = 1500
+    lay = p8.Layout(1, 1, hd, P)
+    x = torch.randn((1, 1, 2, P, hd), generator=torch.Generator().manual_seed(2))
+    x[:, :, 1] = 1e38 * torch.sign(x[:, :, 1])
+    pool = p8.new_pool(lay, 1)
+    p8.quantize(lay, pool, x.cuda(), [P])
+    q = torch.randn((1, 4, 1, hd), generator=torch.Generator().manual_seed(6)).cuda()
+    out, lse = p8.attend(lay, pool, q, [P], split_tokens=split)
+    assert out.isfinite().all()
+    check_attend(lay, pool, q, [P], out, lse, 0, 1 / math.sqrt(hd))
+    x[0, 0, 1, 1400, 3] = float("nan")
+    p8.quantize(lay, pool, x.cuda(), [P])
+    assert p8.attend(lay, pool, q, [P], split_tokens=split)[0].isnan().all()
+    o, l = p8.attend(lay, pool, q, [1376], split_tokens=split)
+    check_attend(lay, pool, q, [1376], o, l, 0, 1 / math.sqrt(hd))
+
+
+def test_attend_needs_a_workspace_for_pieces_only():
+    dll = p8._load()
+    for kvh, hd, H, G in ((1, 32, 1, 1), (16, 64, 1, 1), (4, 128, 32, 4)):
+        for n in (1, 3, 200):
+            for most, quota, needs in ((4096, 0, False), (256, 20, False), (70000, 0, n * kvh * H * G < 16 and kvh == 1)):
+                lens = torch.full((n,), most, dtype=torch.int32)
+                cl = p8._record(p8.Layout(1, kvh, hd, most))[2]
+                need = dll.ebrl_prefix8_attend_workspace(cl, n, lens.data_ptr(), H, kvh * G, 0, quota)
+                assert need > 0 if needs else (need == 0 or most > 4096), (kvh, hd, H, G, n, most, quota)
+                assert need < 64 << 20
+        lens = torch.ones(1000, dtype=torch.int32)          # the pieces of one long prefix cost the others no room
+        lens[7] = 70000
+        assert dll.ebrl_prefix8_attend_workspace(p8._record(p8.Layout(1, kvh, hd, 70000))[2], 1000, lens.data_ptr(), H, kvh * G, 0, 0) < 64 << 20
+
+
 def test_attend_strided_queries_and_in_place():
     lay = p8.Layout(1, 2, 64, 90)
     lens = [90, 41, 7]
