@@ -527,7 +527,7 @@ template <int HD, int NT, bool F32, bool TEAM = false> cudaError_t go(const Atte
     // Under a quota: persistent CTAs with all of an SM's warps.  Else one-warp CTAs: as many as the SMs hold where prefixes are alike (the
     // ring then runs on from item to item), one per item where they are not (the hardware hands out the next as one ends).
     const int warps = TEAM ? a.team : (grid ? C::WARPS : 1);
-    const long long cap = grid ? grid : (a.alike && !TEAM ? (long long)sms * C::WARPS : 1 << 20);
+    const long long cap = TEAM ? items : (grid ? grid : (a.alike ? (long long)sms * C::WARPS : 1 << 20));   // (a team takes one item: the join uses its rings)
     return launch_kernel(attend_kernel<HD, NT, F32, TEAM>, (int)(items < cap ? items : cap), warps * 32, (size_t)(warps * C::WARP_BYTES), st, 1, a, e);
 }
 

@@ -301,6 +301,18 @@ def test_attend_teams(H, G, kvh, hd, lens, hide, dtype):
     assert torch.equal(again, out)
 
 
+def test_attend_team_among_a_million_empty_items():
+    lay = p8.Layout(1, 1, 32, 700)
+    pool, _, _ = filled(lay, [700], seed=3)
+    n, H, G = 1024, 1024, 9
+    lens = [0] * (n - 1) + [700]
+    q = torch.zeros((n, H, G, 32), dtype=torch.bfloat16, device="cuda")
+    q[-1:] = torch.randn((1, H, G, 32), generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+    out, lse = p8.attend(lay, pool, q, lens, slots=[0] * n)
+    assert (out[:-1] == 0).all() and torch.isneginf(lse[:-1]).all()
+    check_attend(lay, pool, q[-1:], [700], out[-1:], lse[-1:], 0, 1 / math.sqrt(32))
+
+
 @pytest.mark.parametrize("hd", [32, 64, 128])
 @pytest.mark.parametrize("split", [0, 128, 512, -1])
 def test_attend_largest_values_and_what_one_piece_sees(hd, split):
