@@ -92,6 +92,11 @@ def _host(v, what: str) -> torch.Tensor:
     return v.contiguous()
 
 
+def _most(v: torch.Tensor) -> int:
+    """The largest of host integers, 0 of none."""
+    return max(v.tolist(), default=0) if v.numel() <= 64 else int(v.numpy().max())
+
+
 def _pool(layout: Layout, pool: torch.Tensor, what: str = "pool"):
     rec = _record(layout)
     if rec[1] == 0:
@@ -228,18 +233,18 @@ def quantize(layout: Layout, pool: torch.Tensor, planes: Planes, lens=None, *, s
     L = torch.full((n,), P, dtype=torch.int32) if lens is None and whole else _host(limit if lens is None else lens, "lens")
     if L.numel() != n:
         raise ValueError("%d lengths for %d environments" % (L.numel(), n))
-    given = L.tolist()
-    if max(given) > limit[0] if whole else any(a > b for a, b in zip(given, limit)):
+    given, most = (None, _most(L)) if whole else (L.tolist(), 0)
+    if most > limit[0] if whole else any(a > b for a, b in zip(given, limit)):
         raise ValueError("a length exceeds its planes")
     mp, masks = None, []
     if mask is not None:
         masks = list(mask) if not torch.is_tensor(mask) else [mask]
         if torch.is_tensor(mask):
-            if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < max(given) or (mask.shape[1] > 1 and mask.stride(1) != 1):
+            if mask.dim() != 2 or mask.shape[0] != n or mask.shape[1] < (most if whole else max(given)) or (mask.shape[1] > 1 and mask.stride(1) != 1):
                 raise ValueError("mask must be [n, >= P] with contiguous rows")
             mp = _addresses(mask.data_ptr(), mask.stride(0), n)
         else:
-            if len(masks) != n or any(m is not None and (m.dim() != 1 or m.numel() < k or (m.numel() > 1 and m.stride(0) != 1)) for m, k in zip(masks, given)):
+            if len(masks) != n or any(m is not None and (m.dim() != 1 or m.numel() < k or (m.numel() > 1 and m.stride(0) != 1)) for m, k in zip(masks, given or L.tolist())):
                 raise ValueError("masks must be n contiguous tensors [>= P_i] or None")
             mp = (C.c_void_p * n)(*[m.data_ptr() if m is not None else None for m in masks])
         if any(m is not None and m.dtype not in (torch.uint8, torch.bool) for m in masks):
@@ -344,7 +349,7 @@ def evict(layout: Layout, src: torch.Tensor, dst: torch.Tensor, weight: torch.Te
     if K.numel() != n:
         raise ValueError("%d numbers to keep for %d environments" % (K.numel(), n))
     new = torch.minimum(L, K)
-    most = max(new.tolist(), default=0)
+    most = _most(new)
     ws = _weights(layout, src, weight, "weight")
     wo = 0 if weight_out is None else _weights(layout, src, weight_out, "weight_out")
     if kept is None:
