@@ -196,7 +196,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                 KeyWords<HD> kw[2];
                 kw[0].load(kslot, koff, 0);
                 kw[1].load(kslot, koff, 1);
-                score<HD, NT, F32, 2>(s, kw, query);
+                score<HD, NT, F32>(s, kw, query);
                 const bool hides = mk != FULL;
                 if (hides) {
 #pragma unroll

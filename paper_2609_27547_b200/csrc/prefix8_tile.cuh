@@ -96,8 +96,8 @@ __device__ __forceinline__ uint2 lds64(uint32_t a)
     return v;
 }
 
-// A block's scale as the readers use it: the sign marks a block that holds a NaN, which poisons what reads it as a whole (the
-// integer way of widening would take a NaN code for 480).
+// A block's scale as the readers use it: the sign marks a block that holds a NaN, which poisons what reads it as a whole, whatever
+// becomes of the codes' own NaN on the way (a maximum drops it).
 __device__ __forceinline__ float read_scale(float s) { return __float_as_uint(s) >> 31 ? __uint_as_float(0x7fffffffu) : s; }
 
 // The token (of 16) that is row g of the keys' operand; row g + 8 is the one two further on.
@@ -224,21 +224,21 @@ template <int HD> struct KeyWords {
     }
 };
 
-// Raw scores of N half tiles (16 tokens each) and NT column tiles: s = keys x queries.  q(step, nt, w) hands out the queries'
-// operands.  Half tiles side by side: N * NT independent chains of products hide one another's latency.
-template <int HD, int NT, bool F32, int N, typename Q> __device__ __forceinline__ void score(float (*s)[NT][4], const KeyWords<HD> *k, Q &&q)
+// Raw scores of a tile's two halves (16 tokens each) and NT column tiles: s = keys x queries.  q(step, nt, w) hands out the queries'
+// operands.  Halves side by side: 2 NT independent chains of products hide one another's latency.
+template <int HD, int NT, bool F32, typename Q> __device__ __forceinline__ void score(float (*s)[NT][4], const KeyWords<HD> *k, Q &&q)
 {
 #pragma unroll
-    for (int h = 0; h < N; ++h)
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 4; ++c) s[h][nt][c] = 0.f;
 #pragma unroll
     for (int st = 0; st < HD / 16; ++st) {
-        uint32_t a[N][4];
+        uint32_t a[2][4];
 #pragma unroll
-        for (int h = 0; h < N; ++h) {
+        for (int h = 0; h < 2; ++h) {
             a[h][0] = widen(k[h].a[st]); a[h][1] = widen(k[h].b[st]); a[h][2] = widen(k[h].a[st] >> 16); a[h][3] = widen(k[h].b[st] >> 16);
         }
 #pragma unroll
@@ -246,7 +246,7 @@ template <int HD, int NT, bool F32, int N, typename Q> __device__ __forceinline_
             uint32_t w[QW<F32>];
             q(st, nt, w);
 #pragma unroll
-            for (int h = 0; h < N; ++h) {
+            for (int h = 0; h < 2; ++h) {
                 if constexpr (F32) mma(s[h][nt], a[h][0], a[h][1], a[h][2], a[h][3], w[2], w[3]);
                 mma(s[h][nt], a[h][0], a[h][1], a[h][2], a[h][3], w[0], w[1]);
             }

@@ -124,7 +124,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                 kw[0].load(at, koff, 0);
                 kw[1].load(at, koff, 1);
                 float s[2][NT][4];
-                score<HD, NT, F32, 2>(s, kw, [&](int st, int nt, uint32_t *w) {
+                score<HD, NT, F32>(s, kw, [&](int st, int nt, uint32_t *w) {
 #pragma unroll
                     for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
                 });
