@@ -558,9 +558,10 @@ cudaError_t launch_attend_join(const AttendArgs &a, const Envs &e, bool f32, int
     const int g = (int)(need < cap ? need : cap);
     if (g == 0) return cudaSuccess;
     struct Early {   // the join may be set up while the last pieces are being worked on; it waits for them itself
-        Early() { pdl_set(true); }
-        ~Early() { pdl_set(false); }
-    } early;
+        const bool before = pdl_enabled();
+        Early(bool on) { pdl_set(on); }
+        ~Early() { pdl_set(before); }
+    } early(grid == 0);   // (under a quota its CTAs would wait on SMs beside the attention's)
     switch (a.r.rec.hd) {
     case 128: return many ? join<128, 16>(a, e, f32, g, st) : join<128, 1>(a, e, f32, g, st);
     case 64: return many ? join<64, 16>(a, e, f32, g, st) : join<64, 1>(a, e, f32, g, st);

@@ -1,0 +1,54 @@
+"""GPU tests of the operators on 8-bit prefix records at their limits: the smallest and the largest scales, calls without
+query rows, rows of a single environment or token, score-sized sums whose difference is small, how a call is launched."""
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import prefix8_reference as ref
+from paper_2609_27547_b200 import prefix8 as p8
+from test_prefix8_gpu import DT, check_attend, check_evict, decoded, filled, planes_of, rows_of
+
+pytestmark = pytest.mark.gpu
+
+
+class _Edge(C.Structure):
+    _fields_ = [("from_port", C.c_ubyte), ("to_port", C.c_ubyte), ("type", C.c_ubyte), ("reserved", C.c_ubyte * 5)]
+
+
+def captured(call):
+    """A captured call's graph (kept)."""
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(g):
+        call()
+    return g
+
+
+def edge_types(g):
+    """The types of a graph's edges: 0 = full, 1 = programmatic (the later kernel may be resident before the earlier one is done)."""
+    cu = C.CDLL("libcuda.so.1")
+    n = C.c_size_t(0)
+    raw = C.c_void_p(g.raw_cuda_graph())
+    assert cu.cuGraphGetEdges_v2(raw, None, None, None, C.byref(n)) == 0
+    a, b, e = (C.c_void_p * n.value)(), (C.c_void_p * n.value)(), (_Edge * n.value)()
+    assert cu.cuGraphGetEdges_v2(raw, a, b, e, C.byref(n)) == 0
+    return [x.type for x in e]
+
+
+# ---- how a call is launched -------------------------------------------------------------------------------------------
+
+def test_the_join_is_not_resident_early_under_a_quota():
+    """Under a quota the join's CTAs must not wait on SMs beside the attention's own: the launch is an ordinary one."""
+    lay = p8.Layout(1, 2, 64, 1500)
+    pool, _, _ = filled(lay, [1500, 700])
+    q = torch.randn((2, 1, 4, 64), generator=torch.Generator().manual_seed(5)).to(torch.bfloat16).cuda()
+
+    def call(quota):
+        return lambda: p8.attend(lay, pool, q, [1500, 700], split_tokens=256, sm_quota=quota)
+    call(0)(), call(8)()
+    assert edge_types(captured(call(0))) == [1]
+    assert edge_types(captured(call(8))) == [0]
+    assert edge_types(captured(call(0))) == [1]
