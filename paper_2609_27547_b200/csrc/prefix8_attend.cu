@@ -23,7 +23,8 @@
 //   2^(s - ref) stay below 2^14, which f16 holds with the same 11 bits.  The common tile needs one vote and no
 //   shuffles.  Weights aim at 2^6 rather than 1, so that those 2^-20 of the largest are still normal f16 numbers.
 //   Value scales are never put into the weights: outputs change their unit where neighbouring blocks' scales differ (exact for
-//   powers of two), and a block whose scale is 2^20 below the largest so far has its product scaled by itself.  Any finite scales work.
+//   powers of two), and a block whose scale is 2^20 below the largest so far has its product scaled by itself.  Any finite scales work, zero and
+//   subnormal ones too (such a block is scaled by itself).
 //   fp32 queries always take the latter way: summed up in the tensor core over 16 tiles, outputs were 1.1e-6 off instead of 3.5e-7.
 //
 //   bf16 queries are exact (prefix8_tile.cuh), weights are rounded to f16: 11 bits, an eighth of the output's own rounding.
@@ -157,7 +158,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
         };
 
         float o[MT][NT][4];   // column m * 16 + g of rows 2t, 2t + 1, column + 8 of the same; in units of `unit`
-        float unit = FLT_MIN, inv_unit = 1.f / FLT_MIN, most = FLT_MIN;   // (no scale is smaller); the largest scale so far
+        float unit = FLT_MIN, inv_unit = 1.f / FLT_MIN, most = FLT_MIN;   // (a smaller scale never is the unit); the largest scale so far
         float mr[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -301,7 +302,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                 bool near = !F32;
                 if (F32 ? vs > unit : vs != unit) {
                     most = fmaxf(most, vs);
-                    if (F32 || (near = vs >= most * 0x1p-20f)) {   // (bounded, so that outputs of large blocks stay in range)
+                    if (F32 || (near = vs >= fmaxf(most * 0x1p-20f, FLT_MIN))) {   // (bounded, so that outputs of large blocks stay in range, and 1 / vs)
                         inv_unit = 1.f / vs;
                         rescale(unit * inv_unit);
                         unit = vs;

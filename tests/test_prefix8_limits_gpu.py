@@ -52,3 +52,26 @@ def test_the_join_is_not_resident_early_under_a_quota():
     assert edge_types(captured(call(0))) == [1]
     assert edge_types(captured(call(8))) == [0]
     assert edge_types(captured(call(0))) == [1]
+
+
+# ---- scales -----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("split", [-1, 0, 128])
+def test_attend_subnormal_scales(dtype, split):
+    """A caller's scales may lie below the smallest normal number, in the first block that a row sees, too."""
+    lay = p8.Layout(1, 1, 64, 300)
+    pool, _, _ = filled(lay, [300], seed=4, poison=False)
+    _, scales, _ = p8.views(lay, pool)
+    kept = scales.clone()
+    q = torch.randn((1, 8, 1, 64), generator=torch.Generator().manual_seed(5)).to(DT[dtype]).cuda()
+    for at in (0, 1, 9, slice(0, 4), slice(0, 10)):
+        for small in (2.0 ** -127, 1e-39, 1e-40, 1e-45):
+            scales.copy_(kept)
+            scales[0, 0, 1, 0, at] = small
+            out, lse = p8.attend(lay, pool, q, [300], split_tokens=split)
+            check_attend(lay, pool, q, [300], out, lse, 0, 1 / 8)
+    scales.copy_(kept)
+    scales[0, 0, 0, 0, 0] = 1e-40
+    out, lse = p8.attend(lay, pool, q, [300], split_tokens=split)
+    check_attend(lay, pool, q, [300], out, lse, 0, 1 / 8)
