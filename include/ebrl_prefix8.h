@@ -110,7 +110,8 @@ ebrl_status_t ebrl_prefix8_weigh(const ebrl_prefix8_layout_t *layout, const void
  * by (protected, weight, index): the first protect_first and the last protect_last tokens of the prefix as if their weight were
  * +inf, hidden tokens and NaN weights as if it were -inf, ties to the lower index.  Kept tokens keep their order; hidden ones
  * that stay remain hidden.  A block's codes are taken to its new scale (the rule of quantize on code * scale), which
- * loses nothing but what falls below the new block's smallest code when scales are powers of two.
+ * loses nothing but what falls below the new block's smallest code when scales are powers of two.  (The largest scale written is
+ * 2^127: a caller's own scales beyond it make values that no e4m3 block holds, and those are saturated.)
  *   dst          pool of the same layout and slot numbers: src itself (in place), or memory that does not overlap it
  *   weight       DEVICE fp32, by slot, as in weigh
  *   weight_out   NULL, or like weight: the kept tokens' weights; may be weight itself

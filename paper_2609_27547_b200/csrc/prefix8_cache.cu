@@ -326,41 +326,46 @@ __global__ void __launch_bounds__(256, 4) gather_kernel(const __grid_constant__ 
                 for (int j = 0; j < 4; ++j) { even = __vmaxu2(even, w[j] & 0x007f007fu); odd = __vmaxu2(odd, w[j] & 0x7f007f00u); }
                 const uint32_t m = __vmaxu2(even, odd >> 8), top = max(m & 0xffffu, m >> 16);
                 nan |= top == 0x7fu;
-                amax = fmaxf(amax, finite_abs(code_value(top) * sc[i]));
+                amax = fmaxf(amax, code_value(top) * sc[i]);   // (a NaN is dropped)
             }
             const bool any_nan = __any_sync(0xffffffffu, nan);
-            if (any_nan) {   // the largest of the others
+            // Products may pass fp32's largest number (quantize keeps 3.4e38 as 256 x 2^120): then all are taken 2^-9 as large, and so is the scale.
+            const bool vast = __any_sync(0xffffffffu, amax == INFINITY);
+            const float pre = vast ? 0x1p-9f : 1.f;
+            if (any_nan || vast) {   // the largest that is a number
                 amax = 0.f;
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
                     for (int j = 0; j < 16; ++j) {
                         const uint32_t c = (w[j >> 2] >> (8 * (j & 3))) & 0x7fu;
-                        if (c != 0x7fu) amax = fmaxf(amax, finite_abs(code_value(c) * sc[i]));
+                        if (c != 0x7fu) amax = fmaxf(amax, finite_abs(code_value(c) * pre * sc[i]));
                     }
                 }
             }
             amax = warp_max(amax);
-            const float s = block_scale(amax), inv = 1.f / s;
+            float s = block_scale(amax);
+            if (vast) s = fminf(s, 0x1p118f);   // (2^127 is the largest scale)
+            const float inv = 1.f / s;
             // whether every row changes its scale by a power of two that f16 holds
             bool fine = true;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const float by = sc[i] * inv;
+                const float by = pre * sc[i] * inv;
                 fine &= sc[i] == 0.f || ((__float_as_uint(by) & 0x007fffffu) == 0 && by >= 1.f / 16384.f && by <= 16384.f);
             }
             fine = __all_sync(0xffffffffu, fine);
             __syncthreads();   // every block of the chunk has been read
             if (b0 < keep) {
                 char *dst = a.dst + head_off;
-                if (lane == 0) *reinterpret_cast<float *>(a.dst + sc_off + (size_t)(b0 >> 5) * 4) = any_nan ? -s : s;
+                if (lane == 0) *reinterpret_cast<float *>(a.dst + sc_off + (size_t)(b0 >> 5) * 4) = (any_nan ? -s : s) * (vast ? 0x1p9f : 1.f);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     const int row = b0 + i * RPI + lane / LPR;
                     if (row < keep) {
                         const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
                         uint32_t o[4];
-                        const float by = sc[i] * inv;
+                        const float by = pre * sc[i] * inv;
                         if (fine) {
                             // codes are f16 values, a power of two of one is, too (or far below the smallest code)
                             const __half2 f = __float2half2_rn(by);
@@ -373,7 +378,7 @@ __global__ void __launch_bounds__(256, 4) gather_kernel(const __grid_constant__ 
 #pragma unroll
                                 for (int q = 0; q < 2; ++q) {
                                     const float2 f = code_pair((w[j] >> (16 * q)) & 0xffffu);
-                                    r |= narrow2(f.x * sc[i] * inv, f.y * sc[i] * inv) << (16 * q);
+                                    r |= narrow2(f.x * pre * sc[i] * inv, f.y * pre * sc[i] * inv) << (16 * q);
                                 }
                                 o[j] = r;
                             }

@@ -75,3 +75,27 @@ def test_attend_subnormal_scales(dtype, split):
     scales[0, 0, 0, 0, 0] = 1e-40
     out, lse = p8.attend(lay, pool, q, [300], split_tokens=split)
     check_attend(lay, pool, q, [300], out, lse, 0, 1 / 8)
+
+
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_largest_values(hd, in_place):
+    """A code times its scale may pass fp32's largest number (3.35e38 is kept as 256 x 2^120): the new block's scale goes by it all the same."""
+    lay = p8.Layout(1, 2, hd, 400)
+    lens, keep = [400, 400, 64], [200, 40, 40]
+    x = [planes_of(lay, P, "f32", P) for P in lens]
+    x[0][0, :, 3, 1], x[0][0, 1, 100, 2], x[0][0, 0, 390, hd + 5] = 3.35e38, -3.4e38, 3.3e38
+    x[1][0, :, 40, 0] = -3.4e38
+    src = p8.new_pool(lay, 3)
+    p8.quantize(lay, src, [t.cuda() for t in x], lens)
+    _, scales, _ = p8.views(lay, src)
+    assert float(scales[0, 0, 0, 0, 0]) == 2.0 ** 120
+    scales[1] *= 1.25                                     # not a power of two
+    scales[2, 0, :, 0, 0] = 2.0 ** 127                    # the largest power of two, whatever the codes
+    weight = torch.rand((3, 400), generator=torch.Generator().manual_seed(3)).cuda()
+    weight[:, 3] = weight[:, 40] = weight[:, 100] = 2.0
+    weight[0, 390] = 2.0
+    src0, dst = src.clone(), src if in_place else torch.full_like(src, 0x33)
+    dst0 = dst.clone()
+    _, kept = p8.evict(lay, src, dst, weight, lens, keep)
+    check_evict(lay, src0, dst, dst0, weight, lens, keep, 0, 0, None, None, kept)
