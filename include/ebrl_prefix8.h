@@ -99,7 +99,7 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
  * nothing), of env i, token h, head a at lse + i * lse_env_stride + h * lse_token_stride + a * lse_head_stride.
  *   weight      DEVICE fp32, row of a SLOT at weight + slot * weight_stride, weight_stride >= capacity
  *   accumulate  0: written, else added to what is there
- * The sum is taken in a fixed order.  Slots of one call must differ. */
+ * Without rows (H or n_heads is 0; q and lse may be NULL) the sum is 0.  It is taken in a fixed order.  Slots of one call must differ. */
 ebrl_status_t ebrl_prefix8_weigh(const ebrl_prefix8_layout_t *layout, const void *pool, int32_t n_slots, int32_t n,
                                  const int32_t *slots, const int32_t *len, int32_t layer, const void *q, int32_t q_dtype, int32_t H,
                                  int32_t n_heads, int64_t q_env_stride, int64_t q_token_stride, const float *lse, int64_t lse_env_stride,

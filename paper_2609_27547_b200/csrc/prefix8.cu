@@ -96,12 +96,14 @@ bool rows_apart(int64_t n, int64_t H, int64_t env, int64_t tok, int64_t width)
 }
 
 ebrl_status_t check_queries(const ebrl_prefix8_layout_t *l, int32_t layer, const void *q, int32_t dtype, int32_t H, int32_t heads,
-                            int64_t q_env, int64_t q_tok, float scale)
+                            int64_t q_env, int64_t q_tok, float scale, bool none_too = false)
 {
     if (layer < 0 || layer >= l->kv_layers) BAD("layer %d is outside 0..kv_layers - 1", layer);
     if (dtype != EBRL_F32 && dtype != EBRL_BF16) BAD("unknown q_dtype");
-    if (H < 1 || heads < 1 || heads % l->n_kv_heads) BAD("H must be positive and n_heads a positive multiple of n_kv_heads");
+    const int least = none_too ? 0 : 1;
+    if (H < least || heads < least || heads % l->n_kv_heads) BAD("H must be positive and n_heads a positive multiple of n_kv_heads");
     if (H > 1024 || heads > 1 << 16) return fail(EBRL_ERR_UNSUPPORTED, "H is limited to 1024 and n_heads to 65536");
+    if (H == 0 || heads == 0) return EBRL_OK;
     if (!q || ((uintptr_t)q & 15)) BAD("q is NULL or not 16-byte aligned");
     if (q_env < 0 || q_tok < 0 || q_env * esize(dtype) % 16 || q_tok * esize(dtype) % 16)
         BAD("query strides must be multiples of 16 bytes and not negative");
@@ -348,12 +350,14 @@ ebrl_status_t ebrl_prefix8_weigh(const ebrl_prefix8_layout_t *layout, const void
     return guarded([&]() -> ebrl_status_t {
         ebrl_status_t st = check_envs(layout, pool, n_slots, n, slots, len, sm_quota, true);
         if (st != EBRL_OK || n == 0) return st;
-        if ((st = check_queries(layout, layer, q, q_dtype, H, n_heads, q_env_stride, q_token_stride, scale)) != EBRL_OK) return st;
-        if (!lse || !weight || (((uintptr_t)lse | (uintptr_t)weight) & 3)) BAD("lse or weight is NULL or not 4-byte aligned");
-        if (lse_env_stride < 0 || lse_token_stride < 0 || lse_head_stride < 0) BAD("lse strides must not be negative");
+        const bool rows = H != 0 && n_heads != 0;   // (without rows there is nothing to read, but a sum to write)
+        if ((st = check_queries(layout, layer, q, q_dtype, H, n_heads, q_env_stride, q_token_stride, scale, true)) != EBRL_OK) return st;
+        if ((rows && !lse) || !weight || (((uintptr_t)lse | (uintptr_t)weight) & 3)) BAD("lse or weight is NULL or not 4-byte aligned");
+        if (rows && (lse_env_stride < 0 || lse_token_stride < 0 || lse_head_stride < 0)) BAD("lse strides must not be negative");
         if (weight_stride < layout->capacity) BAD("weight_stride < capacity");
         int sms = 0;
         if ((st = device_sms(sm_quota, &sms)) != EBRL_OK) return st;
+        if (!rows && accumulate) return EBRL_OK;
         WeighArgs a{};
         a.r.rec = record_of(*layout); a.r.pool = (const char *)pool; a.r.layer = layer;
         a.r.q_env = q_env_stride; a.r.q_tok = q_token_stride; a.r.H = H; a.r.heads = n_heads; a.r.G = n_heads / layout->n_kv_heads; a.r.scale = scale;

@@ -327,7 +327,7 @@ def weigh(layout: Layout, pool: torch.Tensor, q: torch.Tensor, lse: torch.Tensor
     s, sp = _n_slots(L, slots, pool)
     with _on(pool.device):
         st = _stream(pool.device, stream, pool, q, lse, weight)
-        if n and H and heads:
+        if n:
             _check(_load().ebrl_prefix8_weigh(cl, pool.data_ptr(), pool.shape[0], n, sp, L.data_ptr(), int(layer), q.data_ptr(), _DTYPES[q.dtype],
                                               H, heads, q.stride(0), q.stride(1), lse.data_ptr(), *lse.stride(), 1.0 / math.sqrt(hd) if scale is None else float(scale),
                                               weight.data_ptr(), ws, 1 if accumulate else 0, int(sm_quota), st))

@@ -99,3 +99,23 @@ def test_evict_largest_values(hd, in_place):
     dst0 = dst.clone()
     _, kept = p8.evict(lay, src, dst, weight, lens, keep)
     check_evict(lay, src0, dst, dst0, weight, lens, keep, 0, 0, None, None, kept)
+
+
+# ---- weigh ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("H,heads", [(0, 2), (3, 0), (0, 0)])
+def test_weigh_without_query_rows(H, heads):
+    """The sum over no rows is 0: written where the call writes, added where it adds; the rest of the row stays."""
+    lay = p8.Layout(1, 2, 64, 90)
+    lens, slots = [90, 0, 40], [3, 0, 1]
+    pool, _, _ = filled(lay, lens, slots=slots, n_slots=4, hide=0.3)
+    q, lse = torch.empty((3, H, heads, 64), device="cuda"), torch.empty((3, H, heads), device="cuda")
+    w = torch.full((4, 95), 5.0, device="cuda")
+    assert p8.weigh(lay, pool, q, lse, lens, w, slots=slots) is w
+    assert (w == 5).all()
+    for quota in (0, 2):
+        w.fill_(5.0)
+        p8.weigh(lay, pool, q, lse, lens, w, slots=slots, accumulate=False, sm_quota=quota)
+        want = torch.full((4, 95), 5.0, device="cuda")
+        want[3, :90], want[1, :40] = 0.0, 0.0
+        assert torch.equal(w, want)

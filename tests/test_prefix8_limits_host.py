@@ -1,0 +1,36 @@
+"""CPU-only tests of the 8-bit prefix operators: calls that have to be let through (arguments are checked before anything touches a
+device, so without one a valid call ends with a CUDA error), and what the binding hands to the library."""
+import gc
+import weakref
+
+import pytest
+import torch
+
+from paper_2609_27547_b200 import binding as B
+from paper_2609_27547_b200 import prefix8 as p8
+from test_prefix8_host import LAY, P0, attend, evict, weigh
+
+no_device = pytest.mark.skipif(torch.cuda.is_available(), reason="this check is for a box without a GPU")
+
+
+class Pool:
+    """What the binding asks of a pool."""
+    device = torch.device("cuda", 0)
+    dtype = torch.uint8
+    shape = (2, LAY.record_bytes)
+
+    def dim(self):
+        return 2
+
+    def is_contiguous(self):
+        return True
+
+
+@no_device
+def test_weigh_without_query_rows():
+    assert weigh(H=0, acc=0) == B.ERR_CUDA
+    assert weigh(H=0, acc=0, q=None, lse=None) == B.ERR_CUDA
+    assert weigh(H=3, heads=0, acc=0, q=None, lse=None) == B.ERR_CUDA
+    for kw in (dict(slots=[1, 2, 1]), dict(w=None), dict(ws=99), dict(layer=2), dict(len=[1, 101, 0]), dict(dt=2), dict(H=-1), dict(heads=-4)):
+        assert weigh(**{**dict(H=0, acc=0), **kw}) == B.ERR_INVALID_ARG, kw
+    assert attend(H=0) == B.ERR_INVALID_ARG and attend(heads=0) == B.ERR_INVALID_ARG
