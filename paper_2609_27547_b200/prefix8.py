@@ -64,9 +64,11 @@ def _load():
 
 @functools.lru_cache(maxsize=256)
 def _record(layout: Layout):
-    """(the C struct, its address, ...): kept, because a layout is a plain value."""
+    """(the C struct, its record's bytes, a reference that calls take): kept, because a layout is a plain value.  The reference holds the
+    struct, so that a call in progress is not touched when other layouts push this one out."""
     c = _CLayout(*[int(v) for v in layout])
-    return c, int(_load().ebrl_prefix8_record_bytes(C.byref(c))), C.addressof(c)
+    at = C.byref(c)
+    return c, int(_load().ebrl_prefix8_record_bytes(at)), at
 
 
 def _check(st: int):

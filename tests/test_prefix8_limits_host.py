@@ -26,6 +26,19 @@ class Pool:
         return True
 
 
+def test_a_layout_in_use_outlives_the_cache():
+    """Other threads may use any number of layouts between a call's check of its pool and the call itself."""
+    held = p8._pool(LAY, Pool())
+    alive = weakref.ref(p8._record(LAY)[0])
+    for i in range(600):
+        p8._record(LAY._replace(capacity=1000 + i))
+    gc.collect()
+    assert alive() is not None
+    del held
+    gc.collect()
+    assert alive() is None
+
+
 @no_device
 def test_weigh_without_query_rows():
     assert weigh(H=0, acc=0) == B.ERR_CUDA
