@@ -102,10 +102,10 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                 const int r = rt * NT * 8 + nt * 8 + g, tok = r / G, head = kh * G + r - tok * G;
                 const size_t off = (size_t)env * a.r.q_env + (size_t)tok * a.r.q_tok + (size_t)head * HD;
                 const void *p = F32 ? (const void *)((const float *)a.r.q + off) : (const void *)((const __nv_bfloat16 *)a.r.q + off);
-                const float f = load_q<HD, F32>(p, r < R, a.r.scale < 0.f, t, q[nt]) * (fabsf(a.r.scale) * LOG2E);
+                const float f = load_q<HD, F32>(p, r < R, a.r.scale < 0.f, t, q[nt]) * fabsf(a.r.scale);
                 // rows that saw nothing (lse = -inf) and rows past the last one add 2^-inf
                 float l = r < R ? a.lse[(size_t)env * a.l_env + (size_t)tok * a.l_tok + (size_t)head * a.l_head] : -INFINITY;
-                l = l == -INFINITY ? INFINITY : l * LOG2E;
+                l = l == -INFINITY ? INFINITY : l;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     fr[nt][c] = __shfl_sync(FULL, f, 8 * t + 4 * c);
@@ -133,8 +133,10 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        v[2 * h] += ex2(fmaf(s[h][nt][0], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[h][nt][1], ks * fr[nt][1], -ls[nt][1]));
-                        v[2 * h + 1] += ex2(fmaf(s[h][nt][2], ks * fr[nt][0], -ls[nt][0])) + ex2(fmaf(s[h][nt][3], ks * fr[nt][1], -ls[nt][1]));
+                        // (the difference in natural units: ks * fr is exact for a power of two, lse as it was given)
+                        const float c0 = ks * fr[nt][0], c1 = ks * fr[nt][1];
+                        v[2 * h] += ex2(LOG2E * fmaf(s[h][nt][0], c0, -ls[nt][0])) + ex2(LOG2E * fmaf(s[h][nt][1], c1, -ls[nt][1]));
+                        v[2 * h + 1] += ex2(LOG2E * fmaf(s[h][nt][2], c0, -ls[nt][0])) + ex2(LOG2E * fmaf(s[h][nt][3], c1, -ls[nt][1]));
                     }
                 // over the quad by halving exchanges: lane t ends with the total of v[t]
                 const float a0 = (t & 2 ? v[2] : v[0]) + __shfl_xor_sync(FULL, t & 2 ? v[0] : v[2], 2);

@@ -119,3 +119,33 @@ def test_weigh_without_query_rows(H, heads):
         want = torch.full((4, 95), 5.0, device="cuda")
         want[3, :90], want[1, :40] = 0.0, 0.0
         assert torch.equal(w, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd,H", [(32, 3), (64, 8), (128, 8), (128, 16), (64, 33)])
+def test_weigh_differences_of_large_scores(hd, H, dtype):
+    """Scores of hundreds next to a log-sum-exp as large.  One column of keys and queries is not zero and everything in it has few
+    bits, so a score is exact; what is left is the difference a = score - lse (rounded: 2^-24 of it), a in units of log 2 (2^-24 for the
+    product, 2^-25 for the constant), the power (2^-22) and the sum over the rows (2^-24 each)."""
+    P = 200
+    lay = p8.Layout(1, 1, hd, P)
+    g = torch.Generator().manual_seed(hd + H)
+    x = torch.zeros((1, 1, 2, P, hd))
+    x[0, 0, 0, :, 5] = torch.randint(32, 38, (P,), generator=g).float()          # kept as 32 or 36
+    pool = p8.new_pool(lay, 1)
+    p8.quantize(lay, pool, x.cuda(), [P])
+    q = torch.zeros((1, H, 1, hd))
+    q[0, :, 0, 5] = torch.randint(30, 60, (H,), generator=g).float()
+    scale = 0.123
+    k, _, _ = decoded(lay, pool, 0, 0, P)
+    s = float(np.float32(scale)) * (rows_of(q, 0, 0, 1) @ k[0].T)                # [H, P] in 64 bits
+    # (rows whose difference is far from 0 add nothing that counts)
+    lse = torch.from_numpy(np.median(s, axis=1)).float().view(1, H, 1) + torch.rand((1, H, 1), generator=g)
+    a = s - lse[0].double().numpy()
+    p = np.exp(a)
+    want = p.sum(0)
+    tol = (p * (np.abs(a) * (2.0 ** -24 + 2.0 ** -24 + 2.0 ** -25) + 2.0 ** -22 + H * 2.0 ** -24)).sum(0) + 1e-37
+    w = torch.zeros((1, P), device="cuda")
+    p8.weigh(lay, pool, q.to(DT[dtype]).cuda(), lse.cuda(), [P], w, scale=scale, accumulate=False)
+    err = np.abs(w[0].double().cpu().numpy() - want)
+    assert (err <= tol).all(), float((err / tol).max())
