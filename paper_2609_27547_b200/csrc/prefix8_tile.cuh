@@ -226,14 +226,22 @@ template <int HD> struct KeyWords {
 
 // Raw scores of a tile's two halves (16 tokens each) and NT column tiles: s = keys x queries.  q(step, nt, w) hands out the queries'
 // operands.  Halves side by side: 2 NT independent chains of products hide one another's latency.
-template <int HD, int NT, bool F32, typename Q> __device__ __forceinline__ void score(float (*s)[NT][4], const KeyWords<HD> *k, Q &&q)
+// The tensor core truncates its sums.  APART: the second terms add up by themselves, so that only the first terms' sum loses bits at its
+// size, and meet it in fp32 (weights of 16 x 20 - 32 tokens x 4 heads of 64 x 8 fp32
+// rows 6.3e-7 -> 2.4e-7 off; time: see weigh).
+template <int HD, int NT, bool F32, bool APART = false, typename Q> __device__ __forceinline__ void score(float (*s)[NT][4], const KeyWords<HD> *k, Q &&q)
 {
+    constexpr bool TWO = F32 && APART;
+    float rest[TWO ? 2 : 1][TWO ? NT : 1][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s[h][nt][c] = 0.f;
+            for (int c = 0; c < 4; ++c) {
+                s[h][nt][c] = 0.f;
+                if constexpr (TWO) rest[h][nt][c] = 0.f;
+            }
 #pragma unroll
     for (int st = 0; st < HD / 16; ++st) {
         uint32_t a[2][4];
@@ -247,10 +255,18 @@ template <int HD, int NT, bool F32, typename Q> __device__ __forceinline__ void 
             q(st, nt, w);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if constexpr (F32) mma(s[h][nt], a[h][0], a[h][1], a[h][2], a[h][3], w[2], w[3]);
+                if constexpr (F32) mma(TWO ? rest[TWO ? h : 0][TWO ? nt : 0] : s[h][nt], a[h][0], a[h][1], a[h][2], a[h][3], w[2], w[3]);
                 mma(s[h][nt], a[h][0], a[h][1], a[h][2], a[h][3], w[0], w[1]);
             }
         }
+    }
+    if constexpr (TWO) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) s[h][nt][c] += rest[h][nt][c];
     }
 }
 

@@ -124,7 +124,7 @@ weigh_kernel(const __grid_constant__ WeighArgs a, const __grid_constant__ Envs e
                 kw[0].load(at, koff, 0);
                 kw[1].load(at, koff, 1);
                 float s[2][NT][4];
-                score<HD, NT, F32>(s, kw, [&](int st, int nt, uint32_t *w) {
+                score<HD, NT, F32, true>(s, kw, [&](int st, int nt, uint32_t *w) {
 #pragma unroll
                     for (int c = 0; c < QW<F32>; ++c) w[c] = q[nt][st][c];
                 });
@@ -195,7 +195,8 @@ template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Env
 // Query rows per product, from the call's rows, head and type alone, so that a batch's other lengths change no bits.  Measured,
 // us with 8 / 16 / 32 on 128 x 768 tokens x 16 heads (two CTAs per SM but for 32 rows and the fp32 forms that hold no more than
 // one): bf16 of 128, 8 rows 48 / 52 / 81, 16 rows 62 / 56 / 87, 32 rows 112 / 89 / 96; bf16 of 64, 8 rows 30 / 36 / 61, 32 rows
-// 90 / 66 / 77.  fp32 of 128, 8 rows 60 / 73 / 118, 32 rows 183 / 135 / 138.  fp32 of 64 (and of 32 alike), 8 rows 34 / 54 / 76, 32
+// 90 / 66 / 77.  fp32 of 128, 8 rows 60 / 73 / 118, 32 rows 183 / 135 / 138 (since second
+// terms add up apart 60 at 8 rows, 85 at 16 and 146 at 32 in the tiles chosen here).  fp32 of 64 (and of 32 alike), 8 rows 34 / 54 / 76, 32
 // rows 101 / 104 / 91 (512 x 64 tokens: 54 / 73 / 70), 64 rows 189 / 194 / 164 (97 / 129 / 122): one size for them all.
 template <int HD> cudaError_t pick(const WeighArgs &a, const Envs &e, bool f32, int max_len, int grid, int sms, cudaStream_t st)
 {

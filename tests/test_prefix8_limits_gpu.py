@@ -149,3 +149,39 @@ def test_weigh_differences_of_large_scores(hd, H, dtype):
     p8.weigh(lay, pool, q.to(DT[dtype]).cuda(), lse.cuda(), [P], w, scale=scale, accumulate=False)
     err = np.abs(w[0].double().cpu().numpy() - want)
     assert (err <= tol).all(), float((err / tol).max())
+
+
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("H", [2, 16, 40])
+def test_weigh_second_terms_of_fp32_queries(H, hd):
+    """Queries of more bits than one f16 term holds, in every 16 columns that are contracted at a time.  The first terms' products add up to
+    whole numbers below 2^24 (exact), the second terms' are 0.75 each: a sum that loses a fraction at every step would be off by up to hd / 16
+    units of 1.3e7, which scores of hundreds show.  The total is a whole number again, so scores are exact; the tolerance is that of the test above."""
+    P = 200
+    lay = p8.Layout(1, 1, hd, P)
+    g = torch.Generator().manual_seed(hd + H)
+    cols = [4 * st for st in range(hd // 16)]                                    # one in every step
+    x, q = torch.zeros((1, 1, 2, P, hd)), torch.zeros((1, H, 1, hd))
+    x[0, 0, 0, :, cols] = 1.0
+    x[0, 0, 0, :, 1] = torch.where(torch.rand(P, generator=g) < 0.5, 448.0, 416.0)
+    x[0, 0, 0, ::32, 1] = 448.0                                                  # (every block's scale is 1)
+    q[0, :, 0, cols] = 4096.75
+    if len(cols) % 4:
+        q[0, :, 0, cols[0]] = 4096.5                                             # 0.5 + 0.5 are whole, too
+        q[0, :, 0, cols[1]] = 4096.5
+    q[0, :, 0, 1] = torch.where(torch.rand(H, generator=g) < 0.5, 28672.0, 26624.0)
+    scale = float(np.float32(1.7e-5))
+    pool = p8.new_pool(lay, 1)
+    p8.quantize(lay, pool, x.cuda(), [P])
+    k, _, _ = decoded(lay, pool, 0, 0, P)
+    s = rows_of(q, 0, 0, 1) @ k[0].T
+    assert (s == np.rint(s)).all() and s.max() < 2 ** 24 and s.min() > 2 ** 23
+    s = scale * s
+    lse = torch.from_numpy(s.max(1)).float().view(1, H, 1) + torch.rand((1, H, 1), generator=g)
+    a = s - lse[0].double().numpy()
+    p = np.exp(a)
+    tol = (p * (np.abs(a) * (2.0 ** -24 + 2.0 ** -24 + 2.0 ** -25) + 2.0 ** -22 + H * 2.0 ** -24)).sum(0) + 1e-37
+    w = torch.zeros((1, P), device="cuda")
+    p8.weigh(lay, pool, q.cuda(), lse.cuda(), [P], w, scale=scale, accumulate=False)
+    err = np.abs(w[0].double().cpu().numpy() - p.sum(0))
+    assert (err <= tol).all(), float((err / tol).max())
