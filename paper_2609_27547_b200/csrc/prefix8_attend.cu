@@ -169,6 +169,14 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[m][nt][c] = 0.f;
         }
+        auto rescale = [&](float by) {
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) o[m][nt][c] *= by;
+        };
         float ks_l = 0.f, vs_l = 0.f;      // scales and visible tokens of tile (i & ~31) + lane
         uint32_t mk_l = 0;
         for (int i = 0; i < ntile; ++i) {
@@ -290,14 +298,6 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                         mma(c, f[h][0], f[h][1], f[h][2], f[h][3], pb[h][nt][0], pb[h][nt][1]);
                     }
                 };
-                auto rescale = [&](float by) {
-#pragma unroll
-                    for (int m = 0; m < MT; ++m)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) o[m][nt][c] *= by;
-                };
                 // fp32 sums that stay in the tensor core lose their last bits to its truncation: fp32 queries take every block's product out
                 bool near = !F32;
                 if (F32 ? vs > unit : vs != unit) {
@@ -356,6 +356,10 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
             return L + __shfl_xor_sync(FULL, L, 16);
         };
         if constexpr (!TEAM) {
+            if (unit < 0x1p-64f) {   // (unit / L has to keep its 24 bits)
+                rescale(0x1p-64f);
+                unit *= 0x1p64f;
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float inv[2];
@@ -391,6 +395,9 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                 }
             if (lane == 0) *reinterpret_cast<float *>(of(warp) + ML + NT * 8 * 8) = unit;
             __syncthreads();
+            float largest = 0.f;   // of the units; where all are small, sums are formed 2^64 as large, so that neither they nor their factors lose bits
+            for (int w = 0; w < warps; ++w) largest = fmaxf(largest, *reinterpret_cast<const float *>(of(w) + ML + NT * 8 * 8));
+            const float up = largest < 0x1p-64f ? 0x1p64f : 1.f, down = 1.f / up;
             float M[NT][2], inv[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -409,13 +416,13 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs
                     float x[4] = {0.f, 0.f, 0.f, 0.f};
                     for (int w = 0; w < warps; ++w) {
                         const float4 v = *reinterpret_cast<const float4 *>(of(w) + ((m * NT + nt) * 32 + lane) * 16);
-                        const float u = *reinterpret_cast<const float *>(of(w) + ML + NT * 8 * 8);
+                        const float u = *reinterpret_cast<const float *>(of(w) + ML + NT * 8 * 8) * up;
                         const float f0 = ex2(ml(w, nt, 0).x - M[nt][0]) * inv[nt][0] * u, f1 = ex2(ml(w, nt, 1).x - M[nt][1]) * inv[nt][1] * u;
                         x[0] = fmaf(f0, v.x, x[0]); x[1] = fmaf(f1, v.y, x[1]); x[2] = fmaf(f0, v.z, x[2]); x[3] = fmaf(f1, v.w, x[3]);
                     }
                     const At at = row_at(nt);
-                    store_o(at, m * 16, x[0], x[1]);
-                    store_o(at, m * 16 + 8, x[2], x[3]);
+                    store_o(at, m * 16, x[0] * down, x[1] * down);
+                    store_o(at, m * 16 + 8, x[2] * down, x[3] * down);
                 }
             }
         }

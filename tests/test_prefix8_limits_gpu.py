@@ -77,6 +77,54 @@ def test_attend_subnormal_scales(dtype, split):
     check_attend(lay, pool, q, [300], out, lse, 0, 1 / 8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("hd", [32, 64, 128])
+@pytest.mark.parametrize("P,split", [(40, -1), (1500, -1), (1500, 0), (1500, 128), (6000, 0)])
+def test_attend_small_values_keep_their_bits(P, split, hd, dtype):
+    """Values 2^-118 times as large give outputs 2^-118 times as large, bit for bit where those are normal numbers: nothing
+    on the way (the unit of the sums divided by the sum of the weights, say) may fall below what fp32 holds with 24 bits.
+
+    Of prefixes that are cut into n pieces, the pieces' means and the sums that join them may fall below 2^-126 where the
+    output does not: rounded to multiples of 2^-149, off by 2^-32 of the large values' unit instead of 2^-24 of themselves.  The
+    factors f of the means are the same in both calls (lse is), and sum to 1.  So the two joins' sums drift apart by f 2^-32 (the mean) +
+    2^-32 + 2 x 2^-24 A (the roundings of either sum, of size A at most) at every piece: 2^-32 (n + 1) + n 2^-23 A in all, and
+    a bf16 output may round the other way (2^-8)."""
+    lay = p8.Layout(1, 2, hd, P)
+    x = torch.randn((1, 1, 2, P, 2 * hd), generator=torch.Generator().manual_seed(P))
+    q = torch.randn((1, 8, 2, hd), generator=torch.Generator().manual_seed(5)).to(DT[dtype]).cuda()
+    pool = p8.new_pool(lay, 1)
+    p8.quantize(lay, pool, x.cuda(), [P])
+    want, lse = p8.attend(lay, pool, q, [P], split_tokens=split)
+    x[:, :, 1] *= 2.0 ** -118
+    p8.quantize(lay, pool, x.cuda(), [P])
+    _, scales, _ = p8.views(lay, pool)
+    assert float(scales[0, 0, 1, :, :-(-P // 32)].max()) <= 2.0 ** -123   # (and 2^-126 at least: none was bounded)
+    out, lse2 = p8.attend(lay, pool, q, [P], split_tokens=split)
+    assert torch.equal(lse, lse2)
+    normal = want.float().abs() >= 2.0 ** -7
+    assert normal.any()
+    got, want = out.float() * 2.0 ** 118, want.float()
+    if split == -1 or (split == 0 and P <= 4096):         # not cut
+        assert torch.equal(got[normal], want[normal])
+        return
+    n = -(-P // (split or 512))                           # (left to itself no piece is shorter than 512 tokens)
+    p8.quantize(lay, pool, (x * torch.tensor([1.0, 2.0 ** 118])[None, None, :, None, None]).cuda(), [P])
+    k, v, _ = decoded(lay, pool, 0, 0, P)
+    for kh in range(2):
+        s = rows_of(q, 0, kh, 1) @ k[kh].T / math.sqrt(hd)
+        w = np.exp(s - s.max(1, keepdims=True))
+        w /= w.sum(1, keepdims=True)
+        A = np.zeros((8, hd))                             # the largest partial sum, wherever the cuts are (they lie between tiles)
+        part = np.zeros((8, hd))
+        for t in range(0, P, 32):
+            part = part + w[:, t:t + 32] @ v[kh, t:t + 32]
+            A = np.maximum(A, np.abs(part))
+        tol = 1.001 * (2.0 ** -32 * (n + 1) + n * 2.0 ** -23 * A)
+        a, b = rows_of(got, 0, kh, 1), rows_of(want, 0, kh, 1)
+        ok = np.abs(a - b) <= tol + (np.abs(b) * 2.0 ** -8 if dtype == "bf16" else 0.0)
+        assert ok[rows_of(normal, 0, kh, 1) != 0].all()
+
+
 @pytest.mark.parametrize("hd", [32, 64, 128])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_evict_largest_values(hd, in_place):
