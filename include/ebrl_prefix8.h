@@ -70,7 +70,8 @@ ebrl_status_t ebrl_prefix8_quantize(const ebrl_prefix8_layout_t *layout, void *p
 /* Softmax attention of each environment's queries over its record's visible tokens, of one layer:
  *     out = softmax(scale * q k^T) v,   lse = log sum_t exp(scale * q k_t)
  *   q      DEVICE, q_dtype (EBRL_F32 or EBRL_BF16): env i, token h, head a at q + i * q_env_stride + h * q_token_stride
- *          + a * head_dim (strides in elements, addresses multiples of 16 bytes).  Head a reads
+ *          + a * head_dim (strides in elements, addresses multiples of 16 bytes; the stride of a single environment
+ *          or token is not looked at).  Head a reads
  *          key/value head a / (n_heads / n_kv_heads).
  *   H      query tokens per environment, 1 .. 1024
  *   out    DEVICE, q_dtype, laid out like q with its own strides; may be q itself

@@ -95,7 +95,13 @@ bool rows_apart(int64_t n, int64_t H, int64_t env, int64_t tok, int64_t width)
     return (tok >= width && env >= (H - 1) * tok + width) || (env >= width && tok >= (n - 1) * env + width);
 }
 
-ebrl_status_t check_queries(const ebrl_prefix8_layout_t *l, int32_t layer, const void *q, int32_t dtype, int32_t H, int32_t heads,
+// Whether rows with these strides start at multiples of 16 bytes from the first; the stride of a single environment or token does not matter.
+bool strides_fit(int64_t n, int64_t H, int64_t env, int64_t tok, int64_t es)
+{
+    return (n <= 1 || (env >= 0 && env * es % 16 == 0)) && (H <= 1 || (tok >= 0 && tok * es % 16 == 0));
+}
+
+ebrl_status_t check_queries(const ebrl_prefix8_layout_t *l, int32_t n, int32_t layer, const void *q, int32_t dtype, int32_t H, int32_t heads,
                             int64_t q_env, int64_t q_tok, float scale, bool none_too = false)
 {
     if (layer < 0 || layer >= l->kv_layers) BAD("layer %d is outside 0..kv_layers - 1", layer);
@@ -105,7 +111,7 @@ ebrl_status_t check_queries(const ebrl_prefix8_layout_t *l, int32_t layer, const
     if (H > 1024 || heads > 1 << 16) return fail(EBRL_ERR_UNSUPPORTED, "H is limited to 1024 and n_heads to 65536");
     if (H == 0 || heads == 0) return EBRL_OK;
     if (!q || ((uintptr_t)q & 15)) BAD("q is NULL or not 16-byte aligned");
-    if (q_env < 0 || q_tok < 0 || q_env * esize(dtype) % 16 || q_tok * esize(dtype) % 16)
+    if (!strides_fit(n, H, q_env, q_tok, (int64_t)esize(dtype)))
         BAD("query strides must be multiples of 16 bytes and not negative");
     if (!std::isfinite(scale)) BAD("scale must be finite");
     return EBRL_OK;
@@ -298,11 +304,11 @@ ebrl_status_t ebrl_prefix8_attend(const ebrl_prefix8_layout_t *layout, const voi
     return guarded([&]() -> ebrl_status_t {
         ebrl_status_t st = check_envs(layout, pool, n_slots, n, slots, len, sm_quota, false);
         if (st != EBRL_OK || n == 0) return st;
-        if ((st = check_queries(layout, layer, q, q_dtype, H, n_heads, q_env_stride, q_token_stride, scale)) != EBRL_OK) return st;
+        if ((st = check_queries(layout, n, layer, q, q_dtype, H, n_heads, q_env_stride, q_token_stride, scale)) != EBRL_OK) return st;
         if (!out || ((uintptr_t)out & 15)) BAD("out is NULL or not 16-byte aligned");
         if (lse && ((uintptr_t)lse & 3)) BAD("lse is not 4-byte aligned");
         const int64_t es = (int64_t)esize(q_dtype), width = (int64_t)n_heads * layout->head_dim;
-        if (o_env_stride < 0 || o_token_stride < 0 || o_env_stride * es % 16 || o_token_stride * es % 16) BAD("output strides must be multiples of 16 bytes and not negative");
+        if (!strides_fit(n, H, o_env_stride, o_token_stride, es)) BAD("output strides must be multiples of 16 bytes and not negative");
         if (!rows_apart(n, H, o_env_stride, o_token_stride, width)) BAD("output rows overlap one another");
         if (out == q && ((n > 1 && o_env_stride != q_env_stride) || (H > 1 && o_token_stride != q_token_stride)))
             BAD("out may be q only with the same strides");
@@ -351,7 +357,7 @@ ebrl_status_t ebrl_prefix8_weigh(const ebrl_prefix8_layout_t *layout, const void
         ebrl_status_t st = check_envs(layout, pool, n_slots, n, slots, len, sm_quota, true);
         if (st != EBRL_OK || n == 0) return st;
         const bool rows = H != 0 && n_heads != 0;   // (without rows there is nothing to read, but a sum to write)
-        if ((st = check_queries(layout, layer, q, q_dtype, H, n_heads, q_env_stride, q_token_stride, scale, true)) != EBRL_OK) return st;
+        if ((st = check_queries(layout, n, layer, q, q_dtype, H, n_heads, q_env_stride, q_token_stride, scale, true)) != EBRL_OK) return st;
         if ((rows && !lse) || !weight || (((uintptr_t)lse | (uintptr_t)weight) & 3)) BAD("lse or weight is NULL or not 4-byte aligned");
         if (rows && (lse_env_stride < 0 || lse_token_stride < 0 || lse_head_stride < 0)) BAD("lse strides must not be negative");
         if (weight_stride < layout->capacity) BAD("weight_stride < capacity");

@@ -233,3 +233,26 @@ def test_weigh_second_terms_of_fp32_queries(H, hd):
     p8.weigh(lay, pool, q.cuda(), lse.cuda(), [P], w, scale=scale, accumulate=False)
     err = np.abs(w[0].double().cpu().numpy() - p.sum(0))
     assert (err <= tol).all(), float((err / tol).max())
+
+
+# ---- strides ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides_of_a_single_environment_or_token_do_not_matter(dtype):
+    lay = p8.Layout(1, 2, 64, 90)
+    pool, _, _ = filled(lay, [90, 41], seed=2)
+    flat = torch.randn(4000, generator=torch.Generator().manual_seed(5)).to(DT[dtype]).cuda()
+    w = torch.zeros((2, 90), device="cuda")
+
+    def both(q, lens):
+        want, lse = p8.attend(lay, pool, q.contiguous(), lens)
+        got, l2 = p8.attend(lay, pool, q, lens)
+        assert torch.equal(got, want) and torch.equal(l2, lse)
+        into = torch.empty(2000, dtype=q.dtype, device="cuda").as_strided(q.shape, q.stride())
+        p8.attend(lay, pool, q, lens, out=into)
+        assert torch.equal(into, want)
+        a = p8.weigh(lay, pool, q, lse, lens, w.clone())
+        assert torch.equal(a, p8.weigh(lay, pool, q.contiguous(), lse, lens, w.clone()))
+    both(flat.as_strided((1, 3, 2, 64), (3, 128, 64, 1)), [90])
+    both(flat.as_strided((2, 1, 2, 64), (256, 7, 64, 1)), [90, 41])
+    both(flat.as_strided((1, 1, 2, 64), (5, 3, 64, 1)), [90])

@@ -40,6 +40,19 @@ def test_a_layout_in_use_outlives_the_cache():
 
 
 @no_device
+def test_strides_of_a_single_environment_or_token_do_not_matter():
+    for call in (attend, weigh):
+        assert call(n=1, len=[7], qe=3) == B.ERR_CUDA
+        assert call(n=1, len=[7], qe=-8) == B.ERR_CUDA
+        assert call(H=1, qt=3) == B.ERR_CUDA
+        assert call(n=1, len=[7], H=1, qe=1, qt=1) == B.ERR_CUDA
+        assert call(qe=4095) == B.ERR_INVALID_ARG and call(qt=511) == B.ERR_INVALID_ARG
+        assert call(n=1, len=[7], qt=511) == B.ERR_INVALID_ARG and call(H=1, qe=4095) == B.ERR_INVALID_ARG
+    assert attend(n=1, len=[7], oe=3) == B.ERR_CUDA and attend(H=1, ot=3) == B.ERR_CUDA
+    assert attend(n=1, len=[7], ot=511) == B.ERR_INVALID_ARG and attend(H=1, oe=4095) == B.ERR_INVALID_ARG
+
+
+@no_device
 def test_weigh_without_query_rows():
     assert weigh(H=0, acc=0) == B.ERR_CUDA
     assert weigh(H=0, acc=0, q=None, lse=None) == B.ERR_CUDA
