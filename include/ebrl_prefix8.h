@@ -115,7 +115,7 @@ ebrl_status_t ebrl_prefix8_weigh(const ebrl_prefix8_layout_t *layout, const void
  * 2^127: a caller's own scales beyond it make values that no e4m3 block holds, and those are saturated.)
  *   dst          pool of the same layout and slot numbers: src itself (in place), or memory that does not overlap it
  *   weight       DEVICE fp32, by slot, as in weigh
- *   weight_out   NULL, or like weight: the kept tokens' weights; may be weight itself
+ *   weight_out   NULL, or like weight: the kept tokens' weights; may be weight itself, or share no memory with it (rows of one stride may alternate)
  *   kept         DEVICE int32, env i of the CALL at kept + i * kept_stride: the kept tokens' old indices, ascending;
  *                kept_stride >= the largest new length.  Entries and rows behind the new length are left as they were.
  * Slots of one call must differ. */

@@ -223,6 +223,17 @@ bool overlap(const void *a, uint64_t na, const void *b, uint64_t nb)
     return x < y + nb && y < x + na;
 }
 
+// Whether two arrays of n rows of `width` fp32 values share memory.  Rows of one stride may lie between one another.
+bool rows_overlap(const float *a, int64_t stride_a, const float *b, int64_t stride_b, int64_t n, int64_t width)
+{
+    auto bytes = [&](int64_t stride) { return (uint64_t)((n - 1) * stride + width) * 4; };
+    if (!overlap(a, bytes(stride_a), b, bytes(stride_b))) return false;
+    if (stride_a != stride_b) return true;
+    const uint64_t stride = (uint64_t)stride_a * 4, w = (uint64_t)width * 4;
+    const uint64_t apart = ((uintptr_t)a > (uintptr_t)b ? (uintptr_t)a - (uintptr_t)b : (uintptr_t)b - (uintptr_t)a) % stride;
+    return apart < w || stride - apart < w;
+}
+
 thread_local Envs t_envs;
 thread_local QuantEnvs t_quant;
 thread_local EvictEnvs t_evict;
@@ -395,7 +406,7 @@ ebrl_status_t ebrl_prefix8_evict(const ebrl_prefix8_layout_t *layout, const void
         if (!weight || !kept || (((uintptr_t)weight | (uintptr_t)weight_out | (uintptr_t)kept) & 3)) BAD("weight or kept is NULL, or an array is not 4-byte aligned");
         if (weight_stride < layout->capacity || (weight_out && weight_out_stride < layout->capacity)) BAD("weight strides must be at least capacity");
         if (weight_out == weight ? weight_out_stride != weight_stride
-                                 : weight_out && overlap(weight, (uint64_t)n_slots * weight_stride * 4, weight_out, (uint64_t)n_slots * weight_out_stride * 4))
+                                 : weight_out && rows_overlap(weight, weight_stride, weight_out, weight_out_stride, n_slots, layout->capacity))
             BAD("weight_out overlaps weight without being it");
         for (int i = 0; i < n; ++i) {
             if (keep[i] < 0) BAD("keep[%d] < 0", i);

@@ -256,3 +256,19 @@ def test_strides_of_a_single_environment_or_token_do_not_matter(dtype):
     both(flat.as_strided((1, 3, 2, 64), (3, 128, 64, 1)), [90])
     both(flat.as_strided((2, 1, 2, 64), (256, 7, 64, 1)), [90, 41])
     both(flat.as_strided((1, 1, 2, 64), (5, 3, 64, 1)), [90])
+
+
+def test_evict_weights_next_to_one_another():
+    """The weights before and after in one tensor, row by row."""
+    lay = p8.Layout(1, 2, 32, 100)
+    lens, keep = [100, 33, 64], [50, 33, 7]
+    src, _, _ = filled(lay, lens, seed=2)
+    both = torch.rand((3, 2, 100), generator=torch.Generator().manual_seed(3)).cuda()
+    for a, b in ((0, 1), (1, 0)):
+        w0, dst = both.clone(), torch.full_like(src, 0x33)
+        _, kept = p8.evict(lay, src, dst, both[:, a], lens, keep, weight_out=both[:, b])
+        check_evict(lay, src, dst, torch.full_like(src, 0x33), w0[:, a], lens, keep, 0, 0, both[:, b], w0[:, b], kept)
+        assert torch.equal(both[:, a], w0[:, a])
+        for i in range(3):
+            k = min(lens[i], keep[i])
+            assert torch.equal(both[i, b, :k], w0[i, a, kept[i, :k].long()])

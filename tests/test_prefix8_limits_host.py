@@ -60,3 +60,14 @@ def test_weigh_without_query_rows():
     for kw in (dict(slots=[1, 2, 1]), dict(w=None), dict(ws=99), dict(layer=2), dict(len=[1, 101, 0]), dict(dt=2), dict(H=-1), dict(heads=-4)):
         assert weigh(**{**dict(H=0, acc=0), **kw}) == B.ERR_INVALID_ARG, kw
     assert attend(H=0) == B.ERR_INVALID_ARG and attend(heads=0) == B.ERR_INVALID_ARG
+
+
+@no_device
+def test_evict_weights_next_to_one_another():
+    assert evict(ws=200, wo=P0 + 400, wos=200) == B.ERR_CUDA          # [n_slots][2][capacity], either way round
+    assert evict(w=P0 + 400, ws=200, wo=P0, wos=200) == B.ERR_CUDA
+    assert evict(ws=250, wo=P0 + 500, wos=250) == B.ERR_CUDA
+    assert evict(ws=200, wo=P0 + 4 * 700, wos=100) == B.ERR_CUDA      # right behind the last row's capacity
+    for kw in (dict(ws=200, wo=P0 + 396, wos=200), dict(ws=200, wo=P0 + 404, wos=200), dict(ws=150, wo=P0 + 400, wos=150), dict(ws=200, wo=P0 + 400, wos=100),
+               dict(ws=200, wo=P0 + 4 * 699, wos=100), dict(wo=P0 + 4, wos=100), dict(w=P0 + 4, wo=P0, wos=100)):
+        assert evict(**kw) == B.ERR_INVALID_ARG, kw
