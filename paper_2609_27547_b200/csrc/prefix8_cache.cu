@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(1024) select_kernel(const __grid_constant__ Ev
                 }
                 __syncthreads();
                 prefix = s_prefix;
-                need = s_need;
+                need = min(max(s_need, 0), keep);   // (it is, unless the weights change meanwhile: see below)
             }
         }
         // tokens in order, four to a thread: above the last kept key, or the first `need` that equal it.  Positions come from a scan of
@@ -255,11 +255,14 @@ __global__ void __launch_bounds__(1024) select_kernel(const __grid_constant__ Ev
             for (int i = 0; i < 4; ++i) {
                 const bool above = (flags >> i) & 1, equal = (flags >> (4 + i)) & 1;
                 const int at = na + min(ne, need);
-                if ((above || (equal && ne < need)) && at < keep) kept[at] = t0 + i;   // (always below keep unless someone changes the weights meanwhile)
+                if ((above || (equal && ne < need)) && at < keep) kept[at] = t0 + i;
                 na += above;
                 ne += equal;
             }
         }
+        // Weights that someone changes while the passes read them (a caller's race) may have given too few or too many: the list is cut above and
+        // filled here, so that whatever it holds lies in the prefix and no access leaves the arrays.
+        for (int j = done_above + min(done_equal, need) + threadIdx.x; j < keep; j += 1024) kept[j] = len - 1;
         __syncthreads();   // the list is there for the whole CTA
         uint32_t *to_mask = reinterpret_cast<uint32_t *>(a.dst + (size_t)ev.slot[env] * a.rec.bytes + a.rec.mask);
         float *to_w = a.weight_out ? a.weight_out + (size_t)ev.slot[env] * a.weight_out_stride : nullptr;

@@ -272,3 +272,30 @@ def test_evict_weights_next_to_one_another():
         for i in range(3):
             k = min(lens[i], keep[i])
             assert torch.equal(both[i, b, :k], w0[i, a, kept[i, :k].long()])
+
+
+# ---- evict beyond what selection keeps in shared memory ---------------------------------------------------------------
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_evict_prefixes_of_any_length_in_one_call(in_place):
+    """Selection holds the keys of up to 49152 tokens in shared memory and makes them anew from the weights beyond: both, at the border, in
+    one call, with ties, hidden tokens and protected ends."""
+    lay = p8.Layout(1, 1, 32, 70000)
+    lens = [49152, 49153, 70000, 50, 70000, 60000, 0]
+    keep = [20000, 20000, 35000, 20, 70000, 1, 5]
+    src, _, _ = filled(lay, lens, hide=0.3, seed=5)
+    weight = torch.rand((len(lens), 70000), generator=torch.Generator().manual_seed(3))
+    weight[1, 10::3] = 0.5
+    weight[2] = (weight[2] * 5).floor()                   # the last kept key is a tie among thousands
+    weight[4, ::7], weight[5] = math.nan, -0.0
+    weight = weight.cuda()
+    src0, w0 = src.clone(), weight.clone()
+    dst = src if in_place else torch.full_like(src, 0x33)
+    dst0 = dst.clone()
+    w_out = weight if in_place else torch.full_like(weight, 9.0)
+    w_out0 = w_out.clone()
+    _, kept = p8.evict(lay, src, dst, weight, lens, keep, protect_first=3, protect_last=40, weight_out=w_out)
+    check_evict(lay, src0, dst, dst0, w0, lens, keep, 3, 40, w_out, w_out0, kept)
+    for i, (n, k) in enumerate(zip(lens, keep)):
+        k = min(n, k)
+        assert torch.equal(w_out[i, :k].view(torch.int32), w0[i, kept[i, :k].long()].view(torch.int32)), i
