@@ -299,3 +299,87 @@ def test_evict_prefixes_of_any_length_in_one_call(in_place):
     for i, (n, k) in enumerate(zip(lens, keep)):
         k = min(n, k)
         assert torch.equal(w_out[i, :k].view(torch.int32), w0[i, kept[i, :k].long()].view(torch.int32)), i
+
+
+# ---- what evict writes beside the records -----------------------------------------------------------------------------
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("quota", [0, 3])
+def test_evict_weights_bit_for_bit(in_place, quota):
+    """The kept tokens' weights, NaN and signed zeros among them, by slot, in place and under a quota."""
+    lay = p8.Layout(2, 2, 64, 300)
+    lens, keep, slots = [300, 0, 33, 257, 64], [150, 4, 33, 99, 0], [5, 1, 0, 3, 4]
+    src, _, _ = filled(lay, lens, hide=0.2, seed=1, n_slots=6, slots=slots)
+    weight = torch.randn((6, 301), generator=torch.Generator().manual_seed(3)).cuda()
+    weight[5, ::4], weight[3, ::5], weight[3, 1::5] = math.nan, -0.0, 0.0
+    src0, w0 = src.clone(), weight.clone()
+    dst = src if in_place else torch.full_like(src, 0x33)
+    dst0 = dst.clone()
+    w_out = weight if in_place else torch.full_like(weight, 9.0)
+    w_out0 = w_out.clone()
+    _, kept = p8.evict(lay, src, dst, weight, lens, keep, slots=slots, protect_first=2, weight_out=w_out, sm_quota=quota)
+    check_evict(lay, src0, dst, dst0, w0, lens, keep, 2, 0, None, None, kept, slots=slots)
+    want = w_out0.clone()
+    for i, sl in enumerate(slots):
+        k = min(lens[i], keep[i])
+        want[sl, :k] = w0[sl, kept[i, :k].long()]
+    assert torch.equal(w_out.view(torch.int32), want.view(torch.int32))
+
+
+# ---- more environments than a launch takes ----------------------------------------------------------------------------
+
+def test_quantize_slots_masks_and_strides_across_launches():
+    lay = p8.Layout(1, 2, 32, 40)
+    n = 2300
+    x = torch.randn((n, 1, 2, 48, 128), generator=torch.Generator().manual_seed(1)).cuda()[:, :, :, :40, 32:96]
+    lens = [(7 * i) % 41 for i in range(n)]
+    g = torch.Generator().manual_seed(2)
+    slots = torch.randperm(n + 20, generator=g)[:n].to(torch.int32)
+    mask = (torch.rand((n, 40), generator=g) > 0.3).cuda()
+    a = p8.new_pool(lay, n + 20)
+    a.fill_(0x55)
+    p8.quantize(lay, a, x, lens, slots=slots, mask=mask)
+    b = torch.full_like(a, 0x55)
+    for i in range(0, n, 500):                            # one launch each
+        j = min(n, i + 500)
+        p8.quantize(lay, b, [x[k, :, :, :lens[k]].contiguous() for k in range(i, j)], lens[i:j], slots=slots[i:j], mask=[mask[k] for k in range(i, j)])
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("quota", [0, 5])
+def test_attend_pieces_of_more_environments_than_a_launch_takes(dtype, quota):
+    lay = p8.Layout(1, 1, 32, 300)
+    n = 1100
+    lens = [(i * 37) % 301 for i in range(n)]
+    x = torch.randn((n, 1, 2, 300, 32), generator=torch.Generator().manual_seed(5)).cuda()
+    pool = p8.new_pool(lay, n)
+    p8.quantize(lay, pool, x, lens)
+    q = torch.randn((n, 3, 2, 32), generator=torch.Generator().manual_seed(6)).to(DT[dtype]).cuda()
+    out, lse = p8.attend(lay, pool, q, lens, split_tokens=128, sm_quota=quota)
+    o, l = p8.attend(lay, pool, q, lens, split_tokens=-1)
+    for i in list(range(1018, 1030)) + [0, 1, n - 1]:
+        check_attend(lay, pool[i:i + 1], q[i:i + 1], lens[i:i + 1], out[i:i + 1], lse[i:i + 1], 0, 1 / math.sqrt(32))
+    # all others against the uncut call: the scores' bits are the same, sums of up to 300 weights are off by (300 / 8 + 64) 2^-24 on either
+    # side, lse (below 15) by 2^-22 (1 + lse) besides, weights by 2^-11, outputs by 2^-8 of themselves
+    sums, vmax = (300 / 8 + 64) * 2.0 ** -24, float(x[:, :, 1].abs().max()) * 1.07
+    assert torch.equal(torch.isneginf(l), torch.isneginf(lse)) and float(lse.max()) < 15
+    assert float((l - lse).nan_to_num(0.0).abs().max()) <= 2 * (sums + 2.0 ** -22 * 16)
+    assert ((o.float() - out.float()).abs() <= 2.0 ** -7 * o.float().abs() + 2 * (2 * sums + 2.0 ** -11) * vmax).all()
+
+
+def test_attend_teams_in_more_than_one_launch():
+    """Few environments with tokens among many without: a team for each of them, and a launch that has none."""
+    lay = p8.Layout(1, 2, 64, 800)
+    n = 2100
+    pool, _, _ = filled(lay, [800, 513, 64], seed=3)
+    lens, slots = [0] * n, [0] * n
+    for i, (at, ln) in enumerate(((3, 800), (1023, 513), (2099, 64))):
+        lens[at], slots[at] = ln, i
+    q = torch.randn((n, 2, 2, 64), generator=torch.Generator().manual_seed(6)).to(torch.bfloat16).cuda()
+    out, lse = p8.attend(lay, pool, q, lens, slots=slots)
+    at = [3, 1023, 2099]
+    check_attend(lay, pool, q[at], [800, 513, 64], out[at], lse[at], 0, 1 / 8)
+    rest = torch.ones(n, dtype=torch.bool)
+    rest[at] = False
+    assert (out[rest.cuda()] == 0).all() and torch.isneginf(lse[rest.cuda()]).all()
