@@ -120,7 +120,7 @@ ebrl_status_t check_queries(const ebrl_prefix8_layout_t *l, int32_t n, int32_t l
 // The SMs of the current device; also checks the quota.
 ebrl_status_t device_sms(int32_t quota, int *sms)
 {
-    static int known[64];
+    static std::atomic<int> known[64];   // (calls may come from several threads)
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) { cudaGetLastError(); return fail(EBRL_ERR_CUDA, "no usable CUDA device"); }
     if (!known[dev]) {

@@ -521,7 +521,7 @@ int tile_for(const AttendArgs &a, const Envs &e, bool f32, int sms)
 template <int HD, int NT, bool F32, bool TEAM = false> cudaError_t go(const AttendArgs &a, const Envs &e, int grid, int sms, cudaStream_t st)
 {
     using C = AttendCfg<HD, NT, F32>;
-    static bool set[64] = {};
+    static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!set[dev]) {

@@ -401,7 +401,7 @@ cudaError_t launch_evict(const EvictArgs &a, const EvictEnvs &e, int max_keep, i
     int longest = 0;
     for (int i = 0; i < e.n; ++i) longest = longest > e.len[i] ? longest : e.len[i];
     const int room = longest < SELECT_KEYS ? longest : SELECT_KEYS;
-    static bool set[64] = {};
+    static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!set[dev]) {

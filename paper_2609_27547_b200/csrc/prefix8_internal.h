@@ -4,6 +4,8 @@
 #include "../../include/ebrl_prefix8.h"
 #include "actgen_internal.h"
 
+#include <atomic>
+
 namespace ebrl {
 namespace p8 {
 

@@ -169,7 +169,7 @@ namespace {
 template <int HD, int NT, bool F32> cudaError_t go(const WeighArgs &a, const Envs &e, int max_len, int grid, int sms, cudaStream_t st)
 {
     using C = WeighCfg<HD, NT, F32>;
-    static bool set[64] = {};
+    static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!set[dev]) {

@@ -1,5 +1,6 @@
 """GPU tests of the operators on 8-bit prefix records at their limits: the smallest and the largest scales, calls without
 query rows, rows of a single environment or token, score-sized sums whose difference is small, how a call is launched."""
+import concurrent.futures
 import ctypes as C
 import math
 
@@ -383,3 +384,37 @@ def test_attend_teams_in_more_than_one_launch():
     rest = torch.ones(n, dtype=torch.bool)
     rest[at] = False
     assert (out[rest.cuda()] == 0).all() and torch.isneginf(lse[rest.cuda()]).all()
+
+
+# ---- several host threads ---------------------------------------------------------------------------------------------
+
+def test_calls_from_several_threads():
+    """Four threads, each with its own stream, pool and weights: every result is that of the same calls one after another."""
+    lay = p8.Layout(1, 2, 64, 700)
+    sets = []
+    for i in range(4):
+        lens = [700 - 100 * i, 33 + i, 64]
+        planes = [planes_of(lay, P, "bf16", P + i).cuda() for P in lens]
+        q = torch.randn((3, 4, 2, 64), generator=torch.Generator().manual_seed(i)).to(torch.bfloat16 if i % 2 else torch.float32).cuda()
+        sets.append((lens, planes, q, torch.cuda.Stream()))
+
+    def life(lens, planes, q, stream):
+        with torch.cuda.stream(stream):
+            pool, w = p8.new_pool(lay, 3), torch.zeros((3, 700), device="cuda")
+            p8.quantize(lay, pool, planes, lens)
+            for split in (-1, 128, 0):
+                out, lse = p8.attend(lay, pool, q, lens, split_tokens=split)
+            p8.weigh(lay, pool, q, lse, lens, w)
+            _, kept = p8.evict(lay, pool, pool, w, lens, [n // 2 for n in lens], kept=torch.zeros((3, 700), dtype=torch.int32, device="cuda"))
+            with pytest.raises(p8.EbrlError, match="layer 7"):
+                p8.attend(lay, pool, q, lens, layer=7)
+            stream.synchronize()
+        return pool, out, lse, w, kept
+    torch.cuda.synchronize()
+    want = [life(*s) for s in sets]
+    for _ in range(5):
+        with concurrent.futures.ThreadPoolExecutor(4) as ex:
+            got = list(ex.map(lambda s: life(*s), sets))
+        for a, b in zip(got, want):
+            for x, y in zip(a, b):
+                assert torch.equal(x, y)
