@@ -240,7 +240,6 @@ thread_local EvictEnvs t_evict;
 
 const Envs &some_envs(int first, int n, const int32_t *slots, const int32_t *len)
 {
-    t_envs.first = first;
     t_envs.n = n;
     for (int i = 0; i < n; ++i) { t_envs.slot[i] = slots ? slots[first + i] : first + i; t_envs.len[i] = len[first + i]; }
     return t_envs;
@@ -421,7 +420,6 @@ ebrl_status_t ebrl_prefix8_evict(const ebrl_prefix8_layout_t *layout, const void
         a.kept_stride = kept_stride;
         for (int first = 0; first < n; first += EVICT_ENVS) {
             EvictEnvs &e = t_evict;
-            e.first = first;
             e.n = std::min(EVICT_ENVS, n - first);
             int most = 0;
             for (int i = 0; i < e.n; ++i) {

@@ -37,7 +37,7 @@
 namespace ebrl {
 namespace p8 {
 
-template <int HD, int NT, bool F32> struct AttendCfg {
+template <int HD, int NT> struct AttendCfg {
     // per SM: as many as their registers allow (128 a thread at 16, 168 at 12, 255 at 8)
     static constexpr int WARPS = HD == 128 ? (NT == 1 ? 12 : 8) : (NT == 1 ? 16 : 12);
     static constexpr int TILE = BLOCK * HD;
@@ -48,10 +48,10 @@ template <int HD, int NT, bool F32> struct AttendCfg {
 };
 
 template <int HD, int NT, bool F32, bool TEAM>
-__global__ void __launch_bounds__(AttendCfg<HD, NT, F32>::WARPS * 32, 1)
+__global__ void __launch_bounds__(AttendCfg<HD, NT>::WARPS * 32, 1)
 attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Envs ev)
 {
-    using C = AttendCfg<HD, NT, F32>;
+    using C = AttendCfg<HD, NT>;
     constexpr int MT = HD / 16, W = HD / 32, ST = HD / 16;
     extern __shared__ __align__(128) char smem[];
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -491,7 +491,7 @@ __global__ void __launch_bounds__(512) attend_join_kernel(const __grid_constant_
     }
 }
 
-int attend_warps(int hd, int tile) { return hd == 128 ? (tile == 8 ? AttendCfg<128, 1, false>::WARPS : AttendCfg<128, 2, false>::WARPS) : (tile == 8 ? AttendCfg<64, 1, false>::WARPS : AttendCfg<64, 2, false>::WARPS); }
+int attend_warps(int hd, int tile) { return hd == 128 ? (tile == 8 ? AttendCfg<128, 1>::WARPS : AttendCfg<128, 2>::WARPS) : (tile == 8 ? AttendCfg<64, 1>::WARPS : AttendCfg<64, 2>::WARPS); }
 
 // Query rows per item: 8, or 16 where that fills its rows and long prefixes make up for fewer warps per SM.  Rows beyond a tile are
 // further items next to this one: they read the same keys and values from L2.  A row's result is the same in every tile.
@@ -520,7 +520,7 @@ int tile_for(const AttendArgs &a, const Envs &e, bool f32, int sms)
 
 template <int HD, int NT, bool F32, bool TEAM = false> cudaError_t go(const AttendArgs &a, const Envs &e, int grid, int sms, cudaStream_t st)
 {
-    using C = AttendCfg<HD, NT, F32>;
+    using C = AttendCfg<HD, NT>;
     static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;

@@ -293,7 +293,6 @@ __global__ void __launch_bounds__(256, 4) gather_kernel(const __grid_constant__ 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int heads = a.rec.kv_layers * 2 * a.rec.kvh;
     const long long items = (long long)ev.n * heads * n_part;
-    pdl_wait();
     for (long long item = blockIdx.x; item < items; item += gridDim.x) {
         long long x = item;
         const int part = (int)(x % n_part); x /= n_part;

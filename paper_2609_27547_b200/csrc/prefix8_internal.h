@@ -22,7 +22,7 @@ struct Record {
 Record record_of(const ebrl_prefix8_layout_t &l);
 
 struct Envs {
-    int n, first;                  // environments of this launch; index of the first in the call
+    int n;                         // environments of this launch
     int slot[CHUNK_ENVS], len[CHUNK_ENVS];
 };
 
@@ -84,7 +84,7 @@ cudaError_t launch_quantize(const Record &rec, char *pool, long long row_stride,
 
 constexpr int EVICT_ENVS = 512;
 struct EvictEnvs {
-    int n, first;
+    int n;
     int slot[EVICT_ENVS], len[EVICT_ENVS], keep[EVICT_ENVS];   // keep = the new length
 };
 struct EvictArgs {
