@@ -55,6 +55,49 @@ def test_the_join_is_not_resident_early_under_a_quota():
     assert edge_types(captured(call(0))) == [1]
 
 
+class _Kernel(C.Structure):
+    _fields_ = [("func", C.c_void_p), ("grid", C.c_uint * 3), ("block", C.c_uint * 3), ("shared", C.c_uint), ("params", C.c_void_p), ("extra", C.c_void_p),
+                ("kern", C.c_void_p), ("ctx", C.c_void_p)]
+
+
+def warps_of(g):
+    """Warps per CTA of a graph's kernels, in ascending order."""
+    cu = C.CDLL("libcuda.so.1")
+    n = C.c_size_t(0)
+    raw = C.c_void_p(g.raw_cuda_graph())
+    assert cu.cuGraphGetNodes(raw, None, C.byref(n)) == 0
+    nodes = (C.c_void_p * n.value)()
+    assert cu.cuGraphGetNodes(raw, nodes, C.byref(n)) == 0
+    out = []
+    for node in nodes:
+        k = _Kernel()
+        assert cu.cuGraphKernelNodeGetParams_v2(C.c_void_p(node), C.byref(k)) == 0
+        out.append(k.block[0] // 32)
+    return sorted(out)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H,G,kvh,hd,lens,want", [
+    (1, 1, 16, 64, [256], [8]),                         # a tile for each of eight warps
+    (1, 2, 2, 128, [33, 0, 1, 32, 31], [2]),            # two tiles at most
+    (19, 1, 2, 32, [700, 64, 0, 511], [8]),
+    (8, 2, 16, 128, [640] * 6 + [7], [4]),
+    (32, 1, 16, 64, [2000] * 14, [2]),
+    (5, 2, 1, 64, [9000, 20, 0, 8999], [4, 16]),        # pieces, each of a team, and their join
+    (2, 1, 3, 128, [5000] + [3] * 40, [4, 16]),
+    (8, 1, 16, 64, [256] * 200, [1]),                   # the SMs are full
+])
+def test_which_form_a_call_takes(H, G, kvh, hd, lens, want, dtype):
+    """The calls that test teams, pieces and both really run them (on 148 SMs)."""
+    if torch.cuda.get_device_properties(0).multi_processor_count != 148:
+        pytest.skip("the choice goes by the number of SMs")
+    lay = p8.Layout(1, kvh, hd, max(lens))
+    pool = p8.new_pool(lay, len(lens))
+    q = torch.zeros((len(lens), H, kvh * G, hd), dtype=DT[dtype], device="cuda")
+    p8.attend(lay, pool, q, lens)
+    assert warps_of(captured(lambda: p8.attend(lay, pool, q, lens))) == want
+
+
 # ---- scales -----------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
