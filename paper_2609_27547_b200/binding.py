@@ -369,13 +369,16 @@ class Queue:
             raise EbrlError(st, "queue create failed")
 
     def _push(self, fn, env_id, prefix, prefix_len, state, out, step_index):
+        if self._gen is not None and torch.is_tensor(prefix):
+            self._gen._check_records([prefix], [prefix_len])
         t = C.c_uint64(0)
         ptr = lambda x: x.data_ptr() if torch.is_tensor(x) else int(x)
         st = fn(self._q, int(env_id), ptr(prefix), int(prefix_len), ptr(state), ptr(out), int(step_index), C.byref(t))
         return st, int(t.value)
 
     def push(self, env_id, prefix, prefix_len, state, out, step_index=0) -> int:
-        """Blocks while the queue is full; returns the ticket.  Tensors (device) or raw addresses."""
+        """Blocks while the queue is full; returns the ticket.  Tensors (device) or raw addresses; the prefix is what the handle's submit takes
+        (planes, hidden states, or a record)."""
         st, t = self._push(self._L.ebrl_queue_push, env_id, prefix, prefix_len, state, out, step_index)
         if st != OK:
             raise EbrlError(st, "queue push failed")

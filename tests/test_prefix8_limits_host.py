@@ -9,6 +9,7 @@ import torch
 from paper_2609_27547_b200 import binding as B
 from paper_2609_27547_b200 import prefix8 as p8
 from test_prefix8_host import LAY, P0, attend, evict, weigh
+from test_queue_host import FakeBackend
 
 no_device = pytest.mark.skipif(torch.cuda.is_available(), reason="this check is for a box without a GPU")
 
@@ -71,3 +72,24 @@ def test_evict_weights_next_to_one_another():
     for kw in (dict(ws=200, wo=P0 + 396, wos=200), dict(ws=200, wo=P0 + 404, wos=200), dict(ws=150, wo=P0 + 400, wos=150), dict(ws=200, wo=P0 + 400, wos=100),
                dict(ws=200, wo=P0 + 4 * 699, wos=100), dict(wo=P0 + 4, wos=100), dict(w=P0 + 4, wo=P0, wos=100)):
         assert evict(**kw) == B.ERR_INVALID_ARG, kw
+
+
+def test_a_queue_takes_records_of_its_handle_only():
+    """What a queue's handle reads is a whole record, whatever the prefix's length: planes, a record of another layout or a part of one are refused
+    like in a submit (raw addresses are the caller's word)."""
+    gen = object.__new__(B.ActGen)
+    gen._h, gen._record_bytes = None, None
+    gen.cfg = B.make_cfg(H=8, A=7, d=256, n_layers=2, n_heads=4, K_steps=4, max_prefix_len=64, max_group_envs=16, kv_dtype=B.E4M3)
+    size = p8.layout_for(gen.cfg).record_bytes
+    be = FakeBackend()
+    q = B.Queue(gen, capacity=8, max_group=4, backend=be.struct)
+    pool, state = torch.zeros((2, size), dtype=torch.uint8), torch.zeros((2, 8, 7))
+    for bad in (torch.zeros((1, 2, 5, 256)), pool[0, :-128], torch.zeros(size * 2, dtype=torch.uint8)[::2], pool):
+        for push in (q.push, q.try_push):
+            with pytest.raises(ValueError):
+                push(1, bad, 5, state[0], state[1], 0)
+    assert q.wait(q.push(1, pool[0], 5, state[0], state[1], 0)) == B.OK
+    assert q.wait(q.push(2, pool[1].data_ptr(), 5, state[0], state[1], 0)) == B.OK
+    assert q.wait(q.try_push(3, pool[1], 5, state[0], state[1], 0)[1]) == B.OK
+    q.destroy()
+    assert [e for g in be.groups for e in g["ids"]] == [1, 2, 3]
