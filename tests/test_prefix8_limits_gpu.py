@@ -9,8 +9,10 @@ import pytest
 import torch
 
 import prefix8_reference as ref
+from paper_2609_27547_b200 import binding as B
 from paper_2609_27547_b200 import prefix8 as p8
 from test_prefix8_gpu import DT, check_attend, check_evict, decoded, filled, planes_of, rows_of
+from test_prefix8_handle_gpu import Case
 
 pytestmark = pytest.mark.gpu
 
@@ -461,3 +463,25 @@ def test_calls_from_several_threads():
         for a, b in zip(got, want):
             for x, y in zip(a, b):
                 assert torch.equal(x, y)
+
+
+# ---- handles ----------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_handle_environments_that_see_nothing(dtype):
+    """All tokens hidden: cross-attention gives 0, as it does over values of 0, and no token gets any weight."""
+    c = Case(dtype=dtype, P=(5, 90))
+    none = [2, 7]
+    gen = B.ActGen(c.cfg, c.wt)
+    w = torch.zeros((12, c.cfg.max_prefix_len), device="cuda")
+    zero = torch.zeros((1, 2, 90, 256), dtype=DT[dtype], device="cuda")
+    base = c.run(gen, [list(range(12))])
+    p8.quantize(c.lay, c.pool, [zero[:, :, :c.P[i]].contiguous() for i in none], [c.P[i] for i in none], slots=none)
+    want = c.run(gen, [list(range(12))])
+    planes = [torch.full((1, 2, c.P[i], 256), math.nan, dtype=DT[dtype], device="cuda") for i in none]
+    p8.quantize(c.lay, c.pool, planes, [c.P[i] for i in none], slots=none, mask=[torch.zeros(c.P[i], dtype=torch.uint8, device="cuda") for i in none])
+    got = c.run(gen, [list(range(12))], weights=w)
+    gen.destroy()
+    rest = [i for i in range(12) if i not in none]
+    assert np.array_equal(got, want) and np.array_equal(got[rest], base[rest]) and not np.array_equal(got[none], base[none])
+    assert (w[none] == 0).all() and (w[rest].sum(1) > 0).all()
