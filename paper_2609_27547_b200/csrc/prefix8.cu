@@ -156,7 +156,7 @@ int longest(const int32_t *len, int n)
 // 146 / 81; 278 x 1732 x 2 heads of 64, 8 rows 49 / 30; two 65 k-token prefixes x 4 heads of 128, 4 rows 1394 / 30 (pieces of 384 tokens without
 // teams 34).  Where SMs are half full short prefixes are not worth a team (512 x 64 - 512 x 4 heads, 8 rows, fp32: 1, 2, 4 warps
 // 26, 29, 38; 96 x 0 - 301 x 2 heads of 32, 64 rows: 9.8, 14.7, 16.5), hence the least number of tiles; teams of eight at head_dim 128 leave 4 of
-// 12 warps idle.  110 random calls: geometric mean 21.3 -> 16.0.
+// 12 warps idle.  110 random calls: geometric mean 21.3 -> 15.6.
 struct Cut { int split, n_split, team; };
 
 Cut cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int heads, int asked, int quota, int sms, bool f32)
@@ -168,7 +168,12 @@ Cut cut(const ebrl_prefix8_layout_t &l, int n, const int32_t *len, int H, int he
         if (most > asked) { c.split = asked; c.n_split = (most + asked - 1) / asked; }
         return c;
     }
-    if (quota) {   // persistent CTAs with a warp for each piece: as many pieces as there are warps for, not below 256 tokens
+    // Under a quota: persistent CTAs with a warp for each piece; as many pieces as there are warps for, not below 256 tokens.  Measured, us on the
+    // device, never cut / this rule, quota 16 and 74: 1 x 1024 tokens x 16 heads of 64, 8 rows 19.9 / 12.4, 19.9 / 12.1; 16 x 2000 x 4 heads of
+    // 128, 8 rows 45 / 36, 46 / 20; two 65 k-token prefixes x 4 heads of 128, 4 rows 1396 / 107, 1396 / 35; 64 x 768 x 16 heads of 128, 16 rows
+    // (not cut) 258, 67.  It loses where items fill nearly half the warps: 4 x 6303 x 8 heads of 128, 128 rows at 74 SMs 177 / 190, 32 x 768 x 16
+    // heads of 64, 8 fp32 rows 23.7 / 28.1.
+    if (quota) {
         sms = std::min(sms, quota);
         long long items = 0;
         for (int i = 0; i < n; ++i) items += len[i] > 0;
