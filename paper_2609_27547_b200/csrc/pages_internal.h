@@ -1,0 +1,107 @@
+// Internal declarations of the operators on paged caches (include/ebrl_pages.h).
+#pragma once
+
+#include "../../include/ebrl_pages.h"
+#include "actgen_internal.h"
+
+#include <atomic>
+
+namespace ebrl {
+namespace pg {
+
+constexpr int WORD = 32;          // tokens of a mask word; what the kernels look a page up for
+constexpr int SEQS = 1024;        // sequences per launch: what is known of them travels as kernel parameters (up to 28 KB)
+
+char *error_text();               // of this thread, 256 bytes
+
+// What the kernels need to find a token.
+struct Geometry {
+    int layers, kvh, hd, T, es;             // T = tokens of a page, es = bytes of an element
+    int t_shift;                            // T = 1 << t_shift
+    size_t head, mask, bytes;               // bytes of one head's [T][hd]; offset of the mask words; bytes of a page
+    __host__ __device__ size_t at(int layer, int p, int h) const { return (((size_t)layer * 2 + p) * kvh + h) * head; }
+};
+Geometry geometry_of(const ebrl_pages_layout_t &l);
+
+// Where a sequence's pages are.
+struct Pages {
+    char *pool;
+    int n_pages;
+    const int *table;
+    long long stride;
+};
+
+// ---- append, copy, gather (pages_cache.cu) ----
+
+struct AppendSeqs {
+    int n, items;                            // an item: a mask word that new tokens fall into
+    int row[SEQS], new_tokens[SEQS], len[SEQS], tab[SEQS], item[SEQS + 1];   // first packed row; row of the table; first item
+};
+struct AppendArgs {
+    Geometry g;
+    Pages p;
+    int layer;
+    const char *k, *v;
+    long long k_stride, v_stride;            // bytes
+    const uint8_t *mask;
+};
+cudaError_t launch_append(const AppendArgs &a, const AppendSeqs &s, int quota, cudaStream_t st);
+
+constexpr int COPY_PAGES = 2048;
+struct CopyPages { int n, from[COPY_PAGES], to[COPY_PAGES], tokens[COPY_PAGES]; };
+cudaError_t launch_copy(const Geometry &g, const char *src, char *dst, const CopyPages &c, int quota, cudaStream_t st);
+
+struct GatherSeqs {
+    int n, items;                            // an item: 32 tokens
+    void *planes[SEQS];
+    uint8_t *mask[SEQS];
+    int len[SEQS], plane_rows[SEQS], item[SEQS + 1];
+    int first;                               // row of the table of sequence 0
+};
+cudaError_t launch_gather(const Geometry &g, const Pages &p, long long row_stride, const GatherSeqs &s, int quota, cudaStream_t st);
+
+// ---- attend ----
+
+struct AttendSeqs {
+    int n, items;
+    int row[SEQS], m[SEQS], len[SEQS], tab[SEQS];      // first packed query; queries; length; row of the table
+    int item[SEQS + 1];                                // first item
+    int part[SEQS];                                    // first (query, piece) pair of the partial results; -1: not cut
+};
+struct AttendArgs {
+    Geometry g;
+    Pages p;
+    int layer, heads, G;                               // G = heads / kv heads
+    const char *q;
+    char *out;
+    long long q_stride, o_stride;                      // elements
+    float *lse;
+    float scale;
+    int causal, window;
+    int split;                                         // tokens of a piece; 0: not cut
+    int team;                                          // warps that share an item
+    float *part_o, *part_ml;                           // [pair][heads][hd] sums, [pair][heads][2] (reference, sum of weights)
+};
+
+// The first token that a query of the sequence sees (rounded down to a mask word): where its first piece begins.
+__host__ __device__ inline int first_token(int len, int m, int window)
+{
+    const int lo = window ? len - m + 1 - window : 0;
+    return lo > 0 ? lo / WORD * WORD : 0;
+}
+__host__ __device__ inline int pieces_of(int len, int m, int window, int split)
+{
+    const int n = len - first_token(len, m, window);
+    return split && n > split ? (int)(((long long)n + split - 1) / split) : 1;
+}
+
+int attend_rows(int hd, bool f32, int rows);           // query rows of an item
+int attend_warps(int hd, bool f32, int rows);          // warps that an SM holds
+cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, int sms, cudaStream_t st);
+cudaError_t launch_attend_join(const AttendArgs &a, const AttendSeqs &s, bool f32, int quota, int sms, cudaStream_t st);
+
+// Whether a bounded wait ran out on the current device since the last call (waits for the device).
+cudaError_t take_status(int *status);
+
+}  // namespace pg
+}  // namespace ebrl
