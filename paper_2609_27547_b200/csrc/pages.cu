@@ -149,8 +149,11 @@ struct Group {
     int split = 0, team = 1;
 };
 
+// Rows from which the tensor-memory kernel takes a sequence.
+constexpr int CHUNK_FROM = 64;
+
 struct Plan {
-    Group groups[2];
+    Group groups[3];                 // 16 rows, 32 rows, CHUNK_ROWS
     std::vector<int64_t> row;        // first packed query of each sequence
     uint64_t pairs = 0;              // (query, piece) pairs of the sequences that are cut
 };
@@ -166,16 +169,21 @@ void cut(const ebrl_pages_layout_t &l, Group &g, const int32_t *m, const int32_t
 {
     if (asked < 0) return;
     if (asked > 0) { g.split = asked; return; }
-    const bool f32 = l.dtype == EBRL_F32;
-    const int warps = attend_warps(l.head_dim, f32, g.rows);
+    const bool chunk = g.rows == CHUNK_ROWS;
+    const int warps = chunk ? 1 : attend_warps(l.head_dim, l.dtype == EBRL_F32);   // items that an SM works on at a time
+    const int tile = chunk ? 4 : 1;                                                // mask words of a tile
     double total = 0;
     int longest = 0;
     for (int i : g.seqs) {
-        const int t = tiles_of(len[i], m[i], window);
+        const int t = (tiles_of(len[i], m[i], window) + tile - 1) / tile;
         total += (double)t * l.n_kv_heads * (((int64_t)m[i] * G + g.rows - 1) / g.rows);
         longest = std::max(longest, t);
     }
     const double per = std::max(1., total / ((double)(quota ? std::min(sms, quota) : sms) * warps)), want = longest / per;
+    if (chunk) {
+        if (want > 1.75 && longest >= 8) g.split = (int)std::max(4., std::ceil(per)) * tile * WORD;
+        return;
+    }
     if (quota) {
         if (want > 1.75 && longest >= 16) g.split = (int)((std::max(8., per) * WORD + 127) / 128) * 128;
         return;
@@ -191,18 +199,18 @@ void cut(const ebrl_pages_layout_t &l, Group &g, const int32_t *m, const int32_t
     while (g.team > 1 && (g.team > most || g.team > longest)) g.team /= 2;
 }
 
-void plan(Plan &p, const ebrl_pages_layout_t &l, int32_t n, const int32_t *m, const int32_t *len, int n_heads, int window, int asked, int quota, int sms)
+void plan(Plan &p, const ebrl_pages_layout_t &l, int32_t n, const int32_t *m, const int32_t *len, int n_heads, int window, int asked, int quota, int sms, bool chunks)
 {
     const int G = n_heads / l.n_kv_heads;
-    const bool f32 = l.dtype == EBRL_F32;
     int64_t at = 0;
     p.row.resize((size_t)n);
     for (int i = 0; i < n; ++i) {
         p.row[i] = at;
         at += m[i];
         if (m[i] == 0) continue;
-        const int rows = attend_rows(l.head_dim, f32, (int)std::min<int64_t>((int64_t)m[i] * G, 1 << 20));
-        Group &g = p.groups[rows == 16 ? 0 : 1];
+        const int64_t all = (int64_t)m[i] * G;
+        const int rows = chunks && all > CHUNK_FROM ? CHUNK_ROWS : attend_rows((int)std::min<int64_t>(all, 1 << 20));
+        Group &g = p.groups[rows == 16 ? 0 : (rows == 32 ? 1 : 2)];
         g.rows = rows;
         g.seqs.push_back(i);
     }
@@ -318,9 +326,11 @@ uint64_t ebrl_pages_attend_workspace(const ebrl_pages_layout_t *layout, int32_t 
             if (len[i] < 0 || len[i] > 1 << 30) BAD("len[%d] = %d is outside 0..2^30", i, len[i]);
         int sms = 0;
         if ((st = device_sms(0, &sms)) != EBRL_OK) return st;
-        Plan p;
-        plan(p, *layout, n, new_tokens, len, n_heads, window, split_tokens, std::max<int>(sm_quota, 0), sms);
-        bytes = part_bytes(*layout, p.pairs, n_heads);
+        for (int chunks = 0; chunks < 2; ++chunks) {   // of either kernel: which one it is may depend on the scale
+            Plan p;
+            plan(p, *layout, n, new_tokens, len, n_heads, window, split_tokens, std::max<int>(sm_quota, 0), sms, chunks && chunk_supported(geometry_of(*layout), 0, 1.f));
+            bytes = std::max(bytes, part_bytes(*layout, p.pairs, n_heads));
+        }
         return EBRL_OK;
     });
     return bytes;
@@ -351,7 +361,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
         int sms = 0;
         if ((st = device_sms(sm_quota, &sms)) != EBRL_OK) return st;
         Plan p;
-        plan(p, *layout, n, new_tokens, len, n_heads, window, split_tokens, sm_quota, sms);
+        plan(p, *layout, n, new_tokens, len, n_heads, window, split_tokens, sm_quota, sms, chunk_supported(g, n_pages, scale));
         const uint64_t need = part_bytes(*layout, p.pairs, n_heads);
         if (p.pairs > INT32_MAX) return fail(EBRL_ERR_UNSUPPORTED, "too many pieces in one call");
         if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need))
@@ -386,7 +396,8 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
                     ++s.n;
                 }
                 s.item[s.n] = s.items = (int)items;
-                if ((st = launched(launch_attend(a, s, f32, gr.rows, sm_quota, sms, (cudaStream_t)stream))) != EBRL_OK) return st;
+                st = launched(gr.rows == CHUNK_ROWS ? launch_chunk(a, s, sm_quota, (cudaStream_t)stream) : launch_attend(a, s, f32, gr.rows, sm_quota, (cudaStream_t)stream));
+                if (st != EBRL_OK) return st;
                 if (!any) continue;
                 // the join's items are the queries of the cut sequences
                 int k = 0, queries = 0;

@@ -66,11 +66,12 @@ __device__ __forceinline__ void mma_tf32(float *c, const uint32_t *a, const uint
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
-// x = hi + lo + what 22 bits do not hold.
+// x as two tf32 terms: the first rounded to 11 bits (2^-11 of x is left), the second cut to 11 bits by the tensor core, which ignores the
+// low 13 (2^-21 of x is lost).  Plain integer instructions: the conversion instruction runs at a sixteenth of their rate.
 __device__ __forceinline__ void two_terms(float x, uint32_t &hi, uint32_t &lo)
 {
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(x));
-    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(lo) : "f"(x - __uint_as_float(hi)));
+    hi = (__float_as_uint(x) + 0x1000u) & 0xffffe000u;
+    lo = __float_as_uint(x - __uint_as_float(hi));
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -120,6 +121,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
             hi = min(hi, first + (r1 - 1) / G + 1);
             if (a.window) lo = max(lo, first + r0 / G - a.window + 1);
         }
+        const int seen = lo;                                              // no row sees a token below
         lo = lo / TK * TK;
         if constexpr (TEAM) {   // this warp's even share
             const int part = (hi - lo + warps * TK - 1) / (warps * TK) * TK;
@@ -147,6 +149,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
                 if ((unsigned)pg < (unsigned)a.p.n_pages) {
                     page = pg;
                     bits = *reinterpret_cast<const unsigned *>(a.p.pool + (size_t)pg * a.g.bytes + a.g.mask + ((w * WORD & (a.g.T - 1)) >> 3));
+                    if (w * WORD < seen) bits = w * WORD + WORD > seen ? bits & (FULL << (seen - w * WORD)) : 0;
                     if (w * WORD < lo) bits &= FULL << (lo - w * WORD);
                     if (w * WORD + WORD > hi) bits &= FULL >> (w * WORD + WORD - hi);
                 }
@@ -241,19 +244,34 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
 #pragma unroll
                             for (int e = 0; e < 4; ++e) two_terms(__uint_as_float(qa[e]), qh[i][e], ql[i][e]);
                         }
+                        // the products of one k-step by themselves, then added: the tensor core's own sums are truncated
+                        float c[MT][NT][4];
+                        uint32_t kh_[NT][2], kl[NT][2];
 #pragma unroll
                         for (int n = 0; n < NT; n += 2) {
-                            uint32_t kb[4], kh_[4], kl[4];
+                            uint32_t kb[4];
                             ldsm4(kt + tile_at<RB>(n * 8 + (lane & 7) + ((lane >> 4) << 3), k * 2 + ((lane >> 3) & 1)), kb);
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) two_terms(__uint_as_float(kb[e]), kh_[e], kl[e]);
-#pragma unroll
-                            for (int i = 0; i < MT; ++i) {
-                                mma_tf32(S[i][n], ql[i], kh_); mma_tf32(S[i][n + 1], ql[i], kh_ + 2);
-                                mma_tf32(S[i][n], qh[i], kl); mma_tf32(S[i][n + 1], qh[i], kl + 2);
-                                mma_tf32(S[i][n], qh[i], kh_); mma_tf32(S[i][n + 1], qh[i], kh_ + 2);
-                            }
+                            for (int e = 0; e < 4; ++e) two_terms(__uint_as_float(kb[e]), kh_[n + e / 2][e & 1], kl[n + e / 2][e & 1]);
                         }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) { c[i][n][0] = c[i][n][1] = c[i][n][2] = c[i][n][3] = 0.f; mma_tf32(c[i][n], ql[i], kh_[n]); }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) mma_tf32(c[i][n], qh[i], kl[n]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) mma_tf32(c[i][n], qh[i], kh_[n]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) S[i][n][e] += c[i][n][e];
                     }
                 }
                 // scores in units of log 2, what a row does not see at -inf
@@ -339,12 +357,32 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
                             two_terms(S[i][k][1], ph[i][2], pl[i][2]); two_terms(S[i][k][3], ph[i][3], pl[i][3]);
                         }
 #pragma unroll
-                        for (int n = 0; n < NV; ++n) {
-                            uint32_t vh[2], vl[2];
+                        for (int n0 = 0; n0 < NV; n0 += 4) {
+                            float c[MT][4][4];
+                            uint32_t vh[4][2], vl[4][2];
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) two_terms(lds32(vt + tile_at<RB>(k * 8 + 2 * t + e, n * 2 + (g >> 2)) + (g & 3) * 4), vh[e], vl[e]);
+                            for (int n = 0; n < 4; ++n)
 #pragma unroll
-                            for (int i = 0; i < MT; ++i) { mma_tf32(O[i][n], pl[i], vh); mma_tf32(O[i][n], ph[i], vl); mma_tf32(O[i][n], ph[i], vh); }
+                                for (int e = 0; e < 2; ++e)
+                                    two_terms(lds32(vt + tile_at<RB>(k * 8 + 2 * t + e, (n0 + n) * 2 + (g >> 2)) + (g & 3) * 4), vh[n][e], vl[n][e]);
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int i = 0; i < MT; ++i) { c[i][n][0] = c[i][n][1] = c[i][n][2] = c[i][n][3] = 0.f; mma_tf32(c[i][n], pl[i], vh[n]); }
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int i = 0; i < MT; ++i) mma_tf32(c[i][n], ph[i], vl[n]);
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int i = 0; i < MT; ++i) mma_tf32(c[i][n], ph[i], vh[n]);
+#pragma unroll
+                            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) O[i][n0 + n][e] += c[i][n][e];
                         }
                     }
                 }
@@ -465,8 +503,8 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
     }
 }
 
-int attend_rows(int, bool, int rows) { return rows <= 16 ? 16 : 32; }
-int attend_warps(int hd, bool f32, int) { return hd * (f32 ? 4 : 2) >= 256 ? 4 : (hd * (f32 ? 4 : 2) == 128 ? 8 : 12); }
+int attend_rows(int rows) { return rows <= 16 ? 16 : 32; }
+int attend_warps(int hd, bool f32) { return hd * (f32 ? 4 : 2) >= 256 ? 4 : (hd * (f32 ? 4 : 2) == 128 ? 8 : 12); }
 
 namespace {
 
@@ -496,7 +534,7 @@ template <int HD, bool F32> cudaError_t pick(const AttendArgs &a, const AttendSe
 
 }  // namespace
 
-cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, int, cudaStream_t st)
+cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, cudaStream_t st)
 {
     if (s.items == 0) return cudaSuccess;
     switch (a.g.hd) {

@@ -1,10 +1,565 @@
-// Waits that ran out (include/ebrl_pages.h: ebrl_pages_check).
+// Softmax attention of many query rows over paged keys and values (include/ebrl_pages.h), bf16, on tcgen05: out = softmax(scale q k^T) v.
+//
+//   Item = (sequence, piece of it, key/value head, 256 query rows), one CTA: two tiles of 128 rows that share every key and value tile (128
+//   tokens), so that the tensor core works on one while the other's softmax is taken.
+//     warps 0 - 3, 4 - 7   the softmax of tile A, of tile B: one thread per row, so that statistics need no shuffles.  Scores come
+//                          from tensor memory, weights go back to it in place (they are the A operand of the second product)
+//     warp 8               copies: TMA boxes of up to 128 tokens of a page, keys and values in turn through one ring
+//     warp 9               products: S = Q K^T of a tile is issued behind the O += P V that last read its weights, and S of one tile and O of the other
+//                          are always queued, in the order  PV_A(j) QK_A(j + 1) PV_B(j) QK_B(j + 1)
+//   A row's reference is raised only when a score exceeds it by 2^8 (weights up to 2^8 keep bf16's 8 bits): sums in tensor memory are
+//   rescaled by the softmax threads themselves, which know from S(j) being there that PV(j - 1) is done.
+//   Tokens that no row may see are masked in S; their value rows are set to zero in shared memory before the product, so that
+//   what stands there (NaN in a row nobody wrote) does not meet a weight of zero.
+//   All waits are bounded: when one runs out the CTA notes it, lets its copies land, frees tensor memory and returns.
 #include "pages_internal.h"
+#include "ptx_helpers.cuh"
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <math.h>
 
 namespace ebrl {
 namespace pg {
 
+namespace {
+
+using namespace ptx;
+
+constexpr unsigned FULL = 0xffffffffu;
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr int ROWS = 128, KEYS = 128, THREADS = 384;
+// 168 registers a thread at launch: 384 x 168 = 64512; then 256 x 208 + 128 x 88 = 64512
+constexpr int SOFTMAX_REGS = 208, OTHER_REGS = 88;
+constexpr unsigned long long LIMIT_NS = 4000000000ull;
+
+template <int HD> struct Shape {
+    static constexpr int SWZ = HD >= 64 ? 128 : 64;                  // bytes of a swizzled row
+    static constexpr int HALVES = HD * 2 / SWZ;                      // column blocks of a row
+    static constexpr int HALF = 128 * SWZ;                           // bytes of 128 rows of one
+    static constexpr int TILE = HALVES * HALF;
+    static constexpr int STAGES = HD == 128 ? 5 : 8;
+    static constexpr int BARS = 2 * STAGES + 8;
+    static constexpr int SMEM = (2 + STAGES) * TILE + 8 * BARS + 16 + 1024;
+};
+
 __device__ int wait_status;       // EBRL_ERR_TIMEOUT once a wait ran out; one on each device
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, uint32_t nbytes)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(nbytes) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *tm, uint32_t bar, int c0, int c1, int c2)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)   // A from tensor memory
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+#define TMEM_REGS32 "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31"
+__device__ __forceinline__ void tmem_ld32(uint32_t a, uint32_t *r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {" TMEM_REGS32 "}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {" TMEM_REGS32 "};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                   "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+                   "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(a) : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Shared-memory matrix descriptors.  Queries and keys: rows of SWZ bytes along the contracted index, groups of 8 rows one behind the other.
+// Values: rows are tokens, the contracted index; a row's SWZ bytes run along the columns, further column blocks follow at LEAD bytes.
+template <int HD, bool VALUES> __device__ __forceinline__ uint64_t smem_desc(uint32_t addr)
+{
+    uint64_t d = (uint64_t)((addr & 0x3FFFFu) >> 4);
+    d |= (uint64_t)(VALUES ? Shape<HD>::HALF >> 4 : 1) << 16;
+    d |= (uint64_t)(8 * Shape<HD>::SWZ >> 4) << 32;
+    d |= (uint64_t)1 << 46;                                  // descriptor version of sm_100
+    d |= (uint64_t)(Shape<HD>::SWZ == 128 ? 2 : 4) << 61;    // 128- or 64-byte swizzle
+    return d;
+}
+// kind::f16: fp32 accumulate, bf16 A and B, M = 128; B along the contracted index, or (VALUES) along its columns.
+__host__ __device__ constexpr uint32_t instr_desc(int N, bool values)
+{
+    return (1u << 4) | (1u << 7) | (1u << 10) | ((values ? 1u : 0u) << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(ROWS >> 4) << 24);
+}
+
+// An item and the tokens lo .. hi (lo a multiple of 128) that some row of it sees.
+struct Item { int s, m, len, R, r0, tiles, kh, piece, lo, hi, seen, n_kv; };   // (seen: no row sees a token below)
+
+__device__ __forceinline__ Item item_of(const AttendArgs &a, const AttendSeqs &sq, int x)
+{
+    Item it;
+    int s = 0, top = sq.n - 1;
+    while (s < top) {
+        const int mid = (s + top + 1) / 2;
+        if (sq.item[mid] <= x) s = mid;
+        else top = mid - 1;
+    }
+    it.s = s; it.m = sq.m[s]; it.len = sq.len[s];
+    it.R = it.m * a.G;
+    const int RT = (it.R + 2 * ROWS - 1) / (2 * ROWS);
+    int rest = x - sq.item[s];
+    const int kh = rest % a.g.kvh; rest /= a.g.kvh;
+    const int rt = RT - 1 - rest % RT;                        // the last rows see most
+    it.kh = kh; it.piece = rest / RT;
+    it.r0 = rt * 2 * ROWS;
+    const int r1 = min(it.R, it.r0 + 2 * ROWS), first = it.len - it.m;
+    it.tiles = r1 - it.r0 > ROWS ? 2 : 1;
+    int lo = first_token(it.len, it.m, a.window), hi = it.len;
+    if (a.split) { lo += it.piece * a.split; hi = min(hi, lo + a.split); }
+    if (a.causal) {
+        hi = min(hi, first + (r1 - 1) / a.G + 1);
+        if (a.window) lo = max(lo, first + it.r0 / a.G - a.window + 1);
+    }
+    it.lo = lo / KEYS * KEYS; it.hi = hi; it.seen = lo;
+    it.n_kv = hi > it.lo ? (hi - it.lo + KEYS - 1) / KEYS : 0;
+    return it;
+}
+
+// Mask words of an item's tokens, 32 of them (8 tiles) held by the lanes of a warp, the next 32 on their way.
+struct Words {
+    const int *tab;
+    const AttendArgs *a;
+    int seen, hi, base;
+    unsigned now, next;
+    __device__ __forceinline__ unsigned fetch(int w) const
+    {
+        unsigned bits = 0;
+        if (w * WORD < hi) {
+            const int page = tab[(w * WORD) >> a->g.t_shift];
+            if ((unsigned)page < (unsigned)a->p.n_pages) {
+                bits = *reinterpret_cast<const unsigned *>(a->p.pool + (size_t)page * a->g.bytes + a->g.mask + ((w * WORD & (a->g.T - 1)) >> 3));
+                if (w * WORD + WORD > hi) bits &= FULL >> (w * WORD + WORD - hi);
+                if (w * WORD < seen) bits = w * WORD + WORD > seen ? bits & (FULL << (seen - w * WORD)) : 0;
+            }
+        }
+        return bits;
+    }
+    __device__ __forceinline__ void start(const AttendArgs &args, const int *table, const Item &it, int lane)
+    {
+        a = &args; tab = table; seen = it.seen; hi = it.hi; base = it.lo / WORD;
+        now = fetch(base + lane);
+        next = fetch(base + 32 + lane);
+    }
+    // the four words of tile j; called for j = 0, 1, 2, ... by all lanes
+    __device__ __forceinline__ void get(int j, int lane, unsigned *w)
+    {
+        if (j && (j & 7) == 0) {
+            base += 32;
+            now = next;
+            next = fetch(base + 32 + lane);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __shfl_sync(FULL, now, (j & 7) * 4 + i);
+    }
+};
+
+template <int HD>
+__global__ void __launch_bounds__(THREADS, 1)
+chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ AttendArgs a, const __grid_constant__ AttendSeqs sq)
+{
+    using C = Shape<HD>;
+    constexpr uint32_t S_COL = 0, O_COL = 2 * KEYS;               // tensor memory: S of A, S of B, O of A, O of B
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const uint32_t q_at = smem_u32(smem), ring = q_at + 2 * C::TILE;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (2 + C::STAGES) * C::TILE);
+    const uint32_t bar0 = smem_u32(bars);
+    auto full = [&](int s) { return bar0 + 8u * s; };
+    auto empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
+    auto q_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + t); };
+    auto s_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 2 + t); };
+    auto p_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 4 + t); };
+    auto o_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 6 + t); };
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars + C::BARS);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(bars + C::BARS + 1);
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (int t = 0; t < 2; ++t) { mbar_init(q_full(t), ROWS); mbar_init(s_full(t), 1); mbar_init(p_full(t), ROWS); mbar_init(o_full(t), 1); }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm)) : "memory");
+    }
+    if (warp == 9) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    bool ok = true;
+
+    if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
+    if (warp == 8) {
+        // ---- copies: the warp looks pages up, one lane issues
+        constexpr int MAX_BOX = KEYS;
+        const int box = a.g.T < MAX_BOX ? a.g.T : MAX_BOX, boxes = KEYS / box;
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
+            const Item it = item_of(a, sq, x);
+            const int *tab = a.p.table + sq.tab[it.s] * a.p.stride;
+            const int first_page = it.lo >> a.g.t_shift, n_pages = it.hi > 0 ? (it.hi - 1) / a.g.T + 1 : 0;   // (of the sequence, those below n_pages hold tokens that are seen)
+            auto fetch = [&](int p) {
+                const int page = p < n_pages ? tab[p] : -1;
+                return (unsigned)page < (unsigned)a.p.n_pages ? page : a.p.n_pages;      // (outside the pool: the copy engine writes zeros)
+            };
+            int base = first_page, now = fetch(base + lane), next = fetch(base + 32 + lane);
+            const int row_k = (int)(a.g.at(a.layer, 0, it.kh) / (HD * 2)), row_v = (int)(a.g.at(a.layer, 1, it.kh) / (HD * 2));
+            for (int j = 0; j < it.n_kv && ok; ++j) {
+                const int tok = it.lo + j * KEYS;
+                if ((tok >> a.g.t_shift) - base >= 32) { base += 32; now = next; next = fetch(base + 32 + lane); }
+                int page[4];
+#pragma unroll
+                for (int b = 0; b < 4; ++b) page[b] = __shfl_sync(FULL, now, ((tok + b * box) >> a.g.t_shift) - base);   // (pages of a tile are in one batch: 32 is a multiple of 4)
+                if (lane == 0) {
+                    for (int kv = 0; kv < 2 && ok; ++kv) {
+                        if (!mbar_wait_relaxed(empty(stage), phase ^ 1u, LIMIT_NS, abort_flag)) { ok = false; break; }
+                        mbar_expect_tx(full(stage), C::TILE);
+                        const uint32_t dst = ring + stage * C::TILE;
+                        const int row = (kv ? row_v : row_k) + (tok & (a.g.T - 1));
+#pragma unroll
+                        for (int b = 0; b < 4; ++b)
+                            if (b < boxes)
+                                for (int h = 0; h < C::HALVES; ++h)
+                                    tma_load_3d(dst + h * C::HALF + b * box * C::SWZ, &tm, full(stage), h * 64, row, page[b]);
+                        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+                    }
+                }
+                ok = __shfl_sync(FULL, ok ? 1 : 0, 0) != 0;
+            }
+        }
+    } else if (warp == 9) {
+        // ---- products
+        constexpr uint32_t id_qk = instr_desc(KEYS, false), id_pv = instr_desc(HD, true);
+        constexpr int PER = C::SWZ / 32;                            // k-steps in a column block
+        int stage = 0;
+        uint32_t phase = 0, qph[2] = {0, 0}, pph[2] = {0, 0};
+        auto advance = [&]() { if (++stage == C::STAGES) { stage = 0; phase ^= 1u; } };
+        auto wait = [&](uint32_t bar, uint32_t parity) {            // by all lanes
+            if (ok) ok = __all_sync(FULL, mbar_wait(bar, parity, LIMIT_NS, abort_flag)) != 0;
+            tc_fence_after();
+        };
+        auto qk = [&](int t, uint32_t k_at) {
+            if (lane == 0) {
+                const uint64_t ad = smem_desc<HD, false>(q_at + t * C::TILE), bd = smem_desc<HD, false>(k_at);
+#pragma unroll
+                for (int k = 0; k < HD / 16; ++k) {
+                    const uint64_t off = (uint64_t)((k / PER * C::HALF + k % PER * 32) >> 4);
+                    mma_ss(tmem + S_COL + t * KEYS, ad + off, bd + off, id_qk, k != 0);
+                }
+                tc_commit(s_full(t));
+            }
+        };
+        auto pv = [&](int t, uint32_t v_at, bool first) {
+            if (lane == 0) {
+                const uint64_t bd = smem_desc<HD, true>(v_at);
+#pragma unroll
+                for (int k = 0; k < KEYS / 16; ++k)
+                    mma_ts(tmem + O_COL + t * HD, tmem + S_COL + t * KEYS + k * 8, bd + (uint64_t)(k * 16 * C::SWZ >> 4), id_pv, !first || k != 0);
+            }
+        };
+        auto commit = [&](uint32_t bar) { if (lane == 0) tc_commit(bar); };
+        for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
+            const Item it = item_of(a, sq, x);
+            if (it.n_kv == 0) continue;
+            Words words;
+            words.start(a, a.p.table + sq.tab[it.s] * a.p.stride, it, lane);
+            // the first keys: S of both tiles
+            wait(full(stage), phase);
+            const uint32_t k0 = ring + stage * C::TILE;
+            for (int t = 0; t < it.tiles && ok; ++t) {
+                wait(q_full(t), qph[t]);
+                qph[t] ^= 1u;
+                if (ok) qk(t, k0);
+            }
+            if (!ok) break;
+            commit(empty(stage));
+            advance();
+            for (int j = 0; j < it.n_kv && ok; ++j) {
+                const int vs = stage;
+                const uint32_t v_at = ring + vs * C::TILE;
+                wait(full(vs), phase);
+                if (!ok) break;
+                advance();
+                unsigned w[4];
+                words.get(j, lane, w);
+                if ((w[0] & w[1] & w[2] & w[3]) != FULL) {          // value rows that nobody sees become zeros
+                    for (int r = lane; r < KEYS; r += 32)
+                        if (!((w[r / 32] >> (r & 31)) & 1))
+#pragma unroll
+                            for (int c = 0; c < HD * 2 / 16; ++c)
+                                *reinterpret_cast<uint4 *>(smem + (2 + vs) * C::TILE + (c / (C::SWZ / 16)) * C::HALF + r * C::SWZ + c % (C::SWZ / 16) * 16) = make_uint4(0, 0, 0, 0);
+                    fence_proxy_async();
+                    __syncwarp();
+                }
+                const bool more = j + 1 < it.n_kv;
+                const int ks = stage;
+                const uint32_t k_at = ring + ks * C::TILE;
+                for (int t = 0; t < it.tiles && ok; ++t) {
+                    wait(p_full(t), pph[t]);
+                    pph[t] ^= 1u;
+                    if (!ok) break;
+                    pv(t, v_at, j == 0);
+                    if (t == it.tiles - 1) commit(empty(vs));
+                    if (more) {
+                        if (t == 0) wait(full(ks), phase);
+                        if (!ok) break;
+                        qk(t, k_at);
+                        if (t == it.tiles - 1) commit(empty(ks));
+                    } else {
+                        commit(o_full(t));
+                    }
+                }
+                if (more) advance();
+            }
+        }
+    }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
+        // ---- softmax: one thread per row of a tile
+        const int t = warp >> 2, tid = threadIdx.x & (ROWS - 1);
+        const uint32_t lanes = tmem + ((uint32_t)(tid & ~31) << 16), s_at = lanes + S_COL + t * KEYS, o_at = lanes + O_COL + t * HD;
+        const float sc = a.scale * LOG2E;
+        uint32_t sph = 0, oph = 0;
+        for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
+            const Item it = item_of(a, sq, x);
+            if (t >= it.tiles) continue;
+            const int r0 = it.r0 + t * ROWS, row = min(r0 + tid, it.R - 1), tok_q = row / a.G, head = it.kh * a.G + row - tok_q * a.G, first = it.len - it.m;
+            float M = -INFINITY, L = 0.f;
+            if (it.n_kv) {
+                // queries: every product that read the last item's is done (its results were waited for)
+                for (int c = tid; c < ROWS * (HD / 8); c += ROWS) {
+                    const int r = c / (HD / 8), p = c % (HD / 8), qr = min(r0 + r, it.R - 1), tok = qr / a.G;
+                    const char *src = a.q + (((long long)sq.row[it.s] + tok) * a.q_stride + (long long)(it.kh * a.G + qr - tok * a.G) * HD + p * 8) * 2;
+                    constexpr int PP = C::SWZ / 16;
+                    const int sw = C::SWZ == 128 ? (r & 7) : ((r >> 1) & 3);
+                    cp16(q_at + t * C::TILE + (p / PP) * C::HALF + r * C::SWZ + (((p % PP) ^ sw) << 4), src, r0 + r < it.R ? 16 : 0);
+                }
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                fence_proxy_async();
+                mbar_arrive(q_full(t));
+                Words words;
+                words.start(a, a.p.table + sq.tab[it.s] * a.p.stride, it, lane);
+                const int last = a.causal ? first + tok_q + 1 : 0x7fffffff, from = a.window ? first + tok_q + 1 - a.window : -0x7fffffff;
+                for (int j = 0; j < it.n_kv && ok; ++j) {
+                    unsigned w[4];
+                    words.get(j, lane, w);
+                    const int tok = it.lo + j * KEYS;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int b = tok + i * WORD;
+                        if (last < b + WORD) w[i] = last > b ? w[i] & (FULL >> (b + WORD - last)) : 0;
+                        if (from > b) w[i] = from < b + WORD ? w[i] & (FULL << (from - b)) : 0;
+                    }
+                    ok = __all_sync(FULL, mbar_wait(s_full(t), sph, LIMIT_NS, abort_flag)) != 0;
+                    sph ^= 1u;
+                    if (!ok) break;
+                    tc_fence_after();
+                    uint32_t S[KEYS];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tmem_ld32(s_at + i * 32, S + i * 32);
+                    tmem_wait_ld();
+                    const bool whole = __all_sync(FULL, (w[0] & w[1] & w[2] & w[3]) == FULL);
+                    if (!whole)
+#pragma unroll
+                        for (int i = 0; i < KEYS; ++i)
+                            if (!((w[i / 32] >> (i & 31)) & 1)) S[i] = 0xff800000u;      // -inf
+                    float top = __uint_as_float(S[0]);
+#pragma unroll
+                    for (int i = 1; i < KEYS; ++i) top = fmaxf(top, __uint_as_float(S[i]));
+                    top *= sc;
+                    // (a row that has seen nothing yet: top and M may both be -inf)
+                    const bool raise = top > M + 8.f;
+                    if (__any_sync(FULL, raise)) {
+                        const float f = raise ? ex2(M - top) : 1.f;          // (0 the first time)
+                        if (raise) M = top;
+                        L *= f;
+                        if (j) {
+#pragma unroll
+                            for (int i = 0; i < HD / 32; ++i) {
+                                uint32_t o[32];
+                                tmem_ld32(o_at + i * 32, o);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
+                                tmem_st32(o_at + i * 32, o);
+                            }
+                        }
+                    }
+                    const float ref = M == -INFINITY ? 0.f : M;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t P[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) {
+                            const float p0 = ex2(fmaf(__uint_as_float(S[h * 64 + 2 * i]), sc, -ref)), p1 = ex2(fmaf(__uint_as_float(S[h * 64 + 2 * i + 1]), sc, -ref));
+                            sum += p0 + p1;
+                            P[i] = pack_bf16(p0, p1);
+                        }
+                        tmem_st32(s_at + h * 32, P);
+                    }
+                    L += sum;
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(p_full(t));
+                }
+                if (!ok) break;
+                ok = __all_sync(FULL, mbar_wait(o_full(t), oph, LIMIT_NS, abort_flag)) != 0;
+                oph ^= 1u;
+                if (!ok) break;
+                tc_fence_after();
+            }
+            // the result: the output, or the piece's partial one
+            const bool mine = r0 + tid < it.R, cut = a.split && sq.part[it.s] >= 0;
+            const float inv = L == 0.f ? 0.f : 1.f / L;
+            const size_t out_row = (size_t)sq.row[it.s] + tok_q;
+            const size_t at = cut ? ((size_t)sq.part[it.s] + (size_t)it.piece * it.m + tok_q) * a.heads + head : 0;
+            __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(a.out) + out_row * a.o_stride + (size_t)head * HD;
+#pragma unroll
+            for (int i = 0; i < HD / 32; ++i) {
+                uint32_t o[32];
+                if (it.n_kv) { tmem_ld32(o_at + i * 32, o); tmem_wait_ld(); }
+                else
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) o[c] = 0;
+                if (mine && cut) {
+                    float4 *po = reinterpret_cast<float4 *>(a.part_o + at * HD + i * 32);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+                        po[c] = make_float4(__uint_as_float(o[4 * c]), __uint_as_float(o[4 * c + 1]), __uint_as_float(o[4 * c + 2]), __uint_as_float(o[4 * c + 3]));
+                } else if (mine) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t v[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v[e] = pack_bf16(__uint_as_float(o[8 * c + 2 * e]) * inv, __uint_as_float(o[8 * c + 2 * e + 1]) * inv);
+                        *reinterpret_cast<uint4 *>(out + i * 32 + c * 8) = make_uint4(v[0], v[1], v[2], v[3]);
+                    }
+                }
+                __syncwarp();
+            }
+            if (mine && cut) { a.part_ml[2 * at] = M; a.part_ml[2 * at + 1] = L; }
+            if (mine && !cut && a.lse) a.lse[out_row * a.heads + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
+            tc_fence_before();
+        }
+    }
+
+    // ---- teardown
+    if (!ok) {
+        *abort_flag = 1;
+        if (lane == 0) atomicExch(&wait_status, (int)EBRL_ERR_TIMEOUT);
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag && threadIdx.x == 0) {
+        // give copies that were still in flight time to land before shared memory is released
+        const unsigned long long t0 = gtimer();
+        while (gtimer() - t0 < 200000ull) { }
+    }
+    __syncthreads();
+    if (warp == 9) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                                  const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn()
+{
+    static const EncodeTiledFn fn = [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess) p = nullptr;
+        return reinterpret_cast<EncodeTiledFn>(p);
+    }();
+    return fn;
+}
+
+// The pool as (column, row of a page, page): boxes of a column block of up to 128 tokens; outside it reads zeros.
+template <int HD> bool make_map(CUtensorMap *out, const Geometry &g, const Pages &p)
+{
+    EncodeTiledFn fn = encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {HD, (cuuint64_t)g.layers * 2 * g.kvh * g.T, (cuuint64_t)p.n_pages};
+    const cuuint64_t strides[2] = {HD * 2, g.bytes};
+    const cuuint32_t box[3] = {Shape<HD>::SWZ / 2, (cuuint32_t)(g.T < KEYS ? g.T : KEYS), 1};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p.pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              Shape<HD>::SWZ == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int HD> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st)
+{
+    static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!set[dev]) {
+        const cudaError_t err = cudaFuncSetAttribute(chunk_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<HD>::SMEM);
+        if (err != cudaSuccess) return err;
+        set[dev] = true;
+    }
+    CUtensorMap tm;
+    if (!make_map<HD>(&tm, a.g, a.p)) return cudaErrorInvalidValue;
+    // one CTA per item, handed out by the hardware as the ones before end; under a quota persistent ones
+    chunk_kernel<HD><<<quota && s.items > quota ? quota : s.items, THREADS, Shape<HD>::SMEM, st>>>(tm, a, s);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+bool chunk_supported(const Geometry &g, int n_pages, float scale)
+{
+    return g.es == 2 && scale > 0.f && (long long)g.layers * 2 * g.kvh * g.T <= INT32_MAX && n_pages < INT32_MAX;
+}
+
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st)
+{
+    if (s.items == 0) return cudaSuccess;
+    return a.g.hd == 128 ? go<128>(a, s, quota, st) : (a.g.hd == 64 ? go<64>(a, s, quota, st) : go<32>(a, s, quota, st));
+}
 
 cudaError_t take_status(int *status)
 {

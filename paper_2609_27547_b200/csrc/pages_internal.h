@@ -83,11 +83,11 @@ struct AttendArgs {
     float *part_o, *part_ml;                           // [pair][heads][hd] sums, [pair][heads][2] (reference, sum of weights)
 };
 
-// The first token that a query of the sequence sees (rounded down to a mask word): where its first piece begins.
+// The first token that a query of the sequence sees (rounded down to 128): where its first piece begins.
 __host__ __device__ inline int first_token(int len, int m, int window)
 {
     const int lo = window ? len - m + 1 - window : 0;
-    return lo > 0 ? lo / WORD * WORD : 0;
+    return lo > 0 ? lo / 128 * 128 : 0;
 }
 __host__ __device__ inline int pieces_of(int len, int m, int window, int split)
 {
@@ -95,10 +95,15 @@ __host__ __device__ inline int pieces_of(int len, int m, int window, int split)
     return split && n > split ? (int)(((long long)n + split - 1) / split) : 1;
 }
 
-int attend_rows(int hd, bool f32, int rows);           // query rows of an item
-int attend_warps(int hd, bool f32, int rows);          // warps that an SM holds
-cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, int sms, cudaStream_t st);
+int attend_rows(int rows);                             // query rows of an item
+int attend_warps(int hd, bool f32);                    // warps that an SM holds
+cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, cudaStream_t st);
 cudaError_t launch_attend_join(const AttendArgs &a, const AttendSeqs &s, bool f32, int quota, int sms, cudaStream_t st);
+
+// The same for many query rows, bf16 (pages_chunk.cu): 256 of them an item, one CTA each.
+constexpr int CHUNK_ROWS = 256;
+bool chunk_supported(const Geometry &g, int n_pages, float scale);
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st);
 
 // Whether a bounded wait ran out on the current device since the last call (waits for the device).
 cudaError_t take_status(int *status);
