@@ -13,6 +13,7 @@
 //   what stands there (NaN in a row nobody wrote) does not meet a weight of zero.
 //   All waits are bounded: when one runs out the CTA notes it, lets its copies land, frees tensor memory and returns.
 #include "pages_internal.h"
+#include "f32x2.cuh"
 #include "ptx_helpers.cuh"
 
 #include <cuda.h>
@@ -64,6 +65,13 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *tm,
 {
     asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(c0), "r"(c1), "r"(c2) : "memory");
+}
+// True in one lane of the warp, always the same one.
+__device__ __forceinline__ bool elect()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
 }
 __device__ __forceinline__ void tc_commit(uint32_t bar)
 {
@@ -208,7 +216,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars + C::BARS);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(bars + C::BARS + 1);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(FULL, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (the same for all lanes, and known to be)
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
         for (int t = 0; t < 2; ++t) { mbar_init(q_full(t), ROWS); mbar_init(s_full(t), 1); mbar_init(p_full(t), ROWS); mbar_init(o_full(t), 1); }
@@ -223,7 +231,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = *tmem_slot;
+    const uint32_t tmem = __shfl_sync(FULL, *tmem_slot, 0);
     bool ok = true;
 
     if (warp >= 8) {
@@ -278,26 +286,31 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
             if (ok) ok = __all_sync(FULL, mbar_wait(bar, parity, LIMIT_NS, abort_flag)) != 0;
             tc_fence_after();
         };
-        auto qk = [&](int t, uint32_t k_at) {
-            if (lane == 0) {
-                const uint64_t ad = smem_desc<HD, false>(q_at + t * C::TILE), bd = smem_desc<HD, false>(k_at);
+        // Operands are the same for all lanes, so that they stay in uniform registers: a product of 64 cycles leaves no time to bring them there
+        // (computed by the issuing lane alone: 152 cycles each).
+        const uint64_t q_desc = smem_desc<HD, false>(q_at), k_desc = smem_desc<HD, false>(ring), v_desc = smem_desc<HD, true>(ring);
+        auto qk = [&](int t, int s) {
+            const uint64_t ad = q_desc + (uint64_t)(t * (C::TILE >> 4)), bd = k_desc + (uint64_t)(s * (C::TILE >> 4));
+            const uint32_t d = tmem + S_COL + t * KEYS;
+            if (elect()) {
 #pragma unroll
                 for (int k = 0; k < HD / 16; ++k) {
                     const uint64_t off = (uint64_t)((k / PER * C::HALF + k % PER * 32) >> 4);
-                    mma_ss(tmem + S_COL + t * KEYS, ad + off, bd + off, id_qk, k != 0);
+                    mma_ss(d, ad + off, bd + off, id_qk, k != 0);
                 }
                 tc_commit(s_full(t));
             }
         };
-        auto pv = [&](int t, uint32_t v_at, bool first) {
-            if (lane == 0) {
-                const uint64_t bd = smem_desc<HD, true>(v_at);
+        auto pv = [&](int t, int s, bool first) {
+            const uint64_t bd = v_desc + (uint64_t)(s * (C::TILE >> 4));
+            const uint32_t d = tmem + O_COL + t * HD, w = tmem + S_COL + t * KEYS, more = first ? 0u : 1u;
+            if (elect()) {
+                mma_ts(d, w, bd, id_pv, more);
 #pragma unroll
-                for (int k = 0; k < KEYS / 16; ++k)
-                    mma_ts(tmem + O_COL + t * HD, tmem + S_COL + t * KEYS + k * 8, bd + (uint64_t)(k * 16 * C::SWZ >> 4), id_pv, !first || k != 0);
+                for (int k = 1; k < KEYS / 16; ++k) mma_ts(d, w + k * 8, bd + (uint64_t)(k * 16 * C::SWZ >> 4), id_pv, 1u);
             }
         };
-        auto commit = [&](uint32_t bar) { if (lane == 0) tc_commit(bar); };
+        auto commit = [&](uint32_t bar) { if (elect()) tc_commit(bar); };
         for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
             const Item it = item_of(a, sq, x);
             if (it.n_kv == 0) continue;
@@ -305,18 +318,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
             words.start(a, a.p.table + sq.tab[it.s] * a.p.stride, it, lane);
             // the first keys: S of both tiles
             wait(full(stage), phase);
-            const uint32_t k0 = ring + stage * C::TILE;
             for (int t = 0; t < it.tiles && ok; ++t) {
                 wait(q_full(t), qph[t]);
                 qph[t] ^= 1u;
-                if (ok) qk(t, k0);
+                if (ok) qk(t, stage);
             }
             if (!ok) break;
             commit(empty(stage));
             advance();
             for (int j = 0; j < it.n_kv && ok; ++j) {
                 const int vs = stage;
-                const uint32_t v_at = ring + vs * C::TILE;
                 wait(full(vs), phase);
                 if (!ok) break;
                 advance();
@@ -333,17 +344,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 }
                 const bool more = j + 1 < it.n_kv;
                 const int ks = stage;
-                const uint32_t k_at = ring + ks * C::TILE;
                 for (int t = 0; t < it.tiles && ok; ++t) {
                     wait(p_full(t), pph[t]);
                     pph[t] ^= 1u;
                     if (!ok) break;
-                    pv(t, v_at, j == 0);
+                    pv(t, vs, j == 0);
                     if (t == it.tiles - 1) commit(empty(vs));
                     if (more) {
                         if (t == 0) wait(full(ks), phase);
                         if (!ok) break;
-                        qk(t, k_at);
+                        qk(t, ks);
                         if (t == it.tiles - 1) commit(empty(ks));
                     } else {
                         commit(o_full(t));
@@ -403,10 +413,15 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
 #pragma unroll
                         for (int i = 0; i < KEYS; ++i)
                             if (!((w[i / 32] >> (i & 31)) & 1)) S[i] = 0xff800000u;      // -inf
-                    float top = __uint_as_float(S[0]);
+                    float part[4];                                            // (independent chains: each step waits for the one before it)
 #pragma unroll
-                    for (int i = 1; i < KEYS; ++i) top = fmaxf(top, __uint_as_float(S[i]));
-                    top *= sc;
+                    for (int i = 0; i < 4; ++i) part[i] = __uint_as_float(S[i]);
+#pragma unroll
+                    for (int i = 4; i < KEYS; i += 8)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            part[c] = i + 4 + c < KEYS ? fmaxf(fmaxf(part[c], __uint_as_float(S[i + c])), __uint_as_float(S[i + 4 + c])) : fmaxf(part[c], __uint_as_float(S[i + c]));
+                    const float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * sc;
                     // (a row that has seen nothing yet: top and M may both be -inf)
                     const bool raise = top > M + 8.f;
                     if (__any_sync(FULL, raise)) {
@@ -426,19 +441,27 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         }
                     }
                     const float ref = M == -INFINITY ? 0.f : M;
-                    float sum = 0.f;
+                    const uint64_t sc2 = pk2(sc, sc), ref2 = pk2(-ref, -ref);
+                    uint64_t sums[4] = {0, 0, 0, 0};                          // (two zeros each)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t P[32];
 #pragma unroll
                         for (int i = 0; i < 32; ++i) {
-                            const float p0 = ex2(fmaf(__uint_as_float(S[h * 64 + 2 * i]), sc, -ref)), p1 = ex2(fmaf(__uint_as_float(S[h * 64 + 2 * i + 1]), sc, -ref));
-                            sum += p0 + p1;
+                            float p0, p1;
+                            upk2(fma2(pk2(__uint_as_float(S[h * 64 + 2 * i]), __uint_as_float(S[h * 64 + 2 * i + 1])), sc2, ref2), p0, p1);
+                            p0 = ex2(p0);
+                            p1 = ex2(p1);
+                            sums[i & 3] = add2(sums[i & 3], pk2(p0, p1));
                             P[i] = pack_bf16(p0, p1);
                         }
                         tmem_st32(s_at + h * 32, P);
                     }
-                    L += sum;
+                    {
+                        float u, v;
+                        upk2(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), u, v);
+                        L += u + v;
+                    }
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(p_full(t));
