@@ -29,9 +29,7 @@ using namespace ptx;
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int ROWS = 128, KEYS = 128, THREADS = 384;
-// 168 registers a thread at launch: 384 x 168 = 64512; then 256 x 208 + 128 x 88 = 64512
-constexpr int SOFTMAX_REGS = 208, OTHER_REGS = 88;
+constexpr int ROWS = 128, KEYS = 128, THREADS = 320;
 constexpr unsigned long long LIMIT_NS = 4000000000ull;
 
 template <int HD> struct Shape {
@@ -105,6 +103,13 @@ __device__ __forceinline__ void tmem_st32(uint32_t a, const uint32_t *r)
                    "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
                    "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(a) : "memory");
 }
+#define TMEM_REGS16 "%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15"
+__device__ __forceinline__ void tmem_st16(uint32_t a, const uint32_t *r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {" TMEM_REGS16 "};"
+                 ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                   "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(a) : "memory");
+}
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
@@ -163,7 +168,7 @@ struct Words {
     const int *tab;
     const AttendArgs *a;
     int seen, hi, base;
-    unsigned now, next;
+    unsigned now, next, full;        // full: which of the 32 words are all ones
     __device__ __forceinline__ unsigned fetch(int w) const
     {
         unsigned bits = 0;
@@ -182,18 +187,20 @@ struct Words {
         a = &args; tab = table; seen = it.seen; hi = it.hi; base = it.lo / WORD;
         now = fetch(base + lane);
         next = fetch(base + 32 + lane);
+        full = __ballot_sync(FULL, now == FULL);
     }
-    // the four words of tile j; called for j = 0, 1, 2, ... by all lanes
-    __device__ __forceinline__ void get(int j, int lane, unsigned *w)
+    // Moves on to tile j; called for j = 0, 1, 2, ... by all lanes.  Whether each of its tokens is seen by some row.
+    __device__ __forceinline__ bool whole(int j, int lane)
     {
         if (j && (j & 7) == 0) {
             base += 32;
             now = next;
+            full = __ballot_sync(FULL, now == FULL);
             next = fetch(base + 32 + lane);
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __shfl_sync(FULL, now, (j & 7) * 4 + i);
+        return ((full >> ((j & 7) * 4)) & 15u) == 15u;
     }
+    __device__ __forceinline__ unsigned word(int j, int i) const { return __shfl_sync(FULL, now, (j & 7) * 4 + i); }
 };
 
 template <int HD>
@@ -234,8 +241,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     const uint32_t tmem = __shfl_sync(FULL, *tmem_slot, 0);
     bool ok = true;
 
-    if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(OTHER_REGS));
     if (warp == 8) {
         // ---- copies: the warp looks pages up, one lane issues
         constexpr int MAX_BOX = KEYS;
@@ -331,11 +336,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 wait(full(vs), phase);
                 if (!ok) break;
                 advance();
-                unsigned w[4];
-                words.get(j, lane, w);
-                if ((w[0] & w[1] & w[2] & w[3]) != FULL) {          // value rows that nobody sees become zeros
-                    for (int r = lane; r < KEYS; r += 32)
-                        if (!((w[r / 32] >> (r & 31)) & 1))
+                if (!words.whole(j, lane)) {                        // value rows that nobody sees become zeros
+                    for (int i = 0; i < 4; ++i)
+                        if (const int r = i * 32 + lane; !((words.word(j, i) >> lane) & 1))
 #pragma unroll
                             for (int c = 0; c < HD * 2 / 16; ++c)
                                 *reinterpret_cast<uint4 *>(smem + (2 + vs) * C::TILE + (c / (C::SWZ / 16)) * C::HALF + r * C::SWZ + c % (C::SWZ / 16) * 16) = make_uint4(0, 0, 0, 0);
@@ -362,9 +365,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 if (more) advance();
             }
         }
-    }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(SOFTMAX_REGS));
         // ---- softmax: one thread per row of a tile
         const int t = warp >> 2, tid = threadIdx.x & (ROWS - 1);
         const uint32_t lanes = tmem + ((uint32_t)(tid & ~31) << 16), s_at = lanes + S_COL + t * KEYS, o_at = lanes + O_COL + t * HD;
@@ -390,78 +391,115 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 Words words;
                 words.start(a, a.p.table + sq.tab[it.s] * a.p.stride, it, lane);
                 const int last = a.causal ? first + tok_q + 1 : 0x7fffffff, from = a.window ? first + tok_q + 1 - a.window : -0x7fffffff;
+                const int all_last = __reduce_min_sync(FULL, last), all_from = __reduce_max_sync(FULL, from);   // what every row of the warp sees
+                const uint64_t sc2 = pk2(sc, sc);
                 for (int j = 0; j < it.n_kv && ok; ++j) {
-                    unsigned w[4];
-                    words.get(j, lane, w);
                     const int tok = it.lo + j * KEYS;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    const bool whole = words.whole(j, lane) && tok + KEYS <= all_last && tok >= all_from;
+                    // What the row does not see of columns i * 32 .. at -inf.
+                    auto hide = [&](uint32_t *v, int i, unsigned w) {
                         const int b = tok + i * WORD;
-                        if (last < b + WORD) w[i] = last > b ? w[i] & (FULL >> (b + WORD - last)) : 0;
-                        if (from > b) w[i] = from < b + WORD ? w[i] & (FULL << (from - b)) : 0;
-                    }
+                        if (last < b + WORD) w = last > b ? w & (FULL >> (b + WORD - last)) : 0;
+                        if (from > b) w = from < b + WORD ? w & (FULL << (from - b)) : 0;
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            if (!((w >> c) & 1)) v[c] = 0xff800000u;
+                    };
+                    // The weights of 32 columns, packed, and two times two sums of theirs.
+                    uint64_t sums[2];
+                    auto weights = [&](const uint32_t *v, uint32_t *P, uint64_t ref2) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float p0, p1;
+                            upk2(fma2(pk2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), sc2, ref2), p0, p1);
+                            p0 = ex2(p0);
+                            p1 = ex2(p1);
+                            sums[i & 1] = add2(sums[i & 1], pk2(p0, p1));
+                            P[i] = pack_bf16(p0, p1);
+                        }
+                    };
+                    auto total = [&]() {
+                        float u, v;
+                        upk2(add2(sums[0], sums[1]), u, v);
+                        return u + v;
+                    };
                     ok = __all_sync(FULL, mbar_wait(s_full(t), sph, LIMIT_NS, abort_flag)) != 0;
                     sph ^= 1u;
                     if (!ok) break;
                     tc_fence_after();
-                    uint32_t S[KEYS];
+                    // First with the reference as it is: weights may grow to 2^30 in sum before anything needs to be done about it, so that the
+                    // maximum of a tile is rarely asked for.
+                    uint32_t P[64];
+                    {
+                        const uint64_t ref2 = pk2(-M, -M);
+                        uint32_t A[32], B[32];
+                        sums[0] = sums[1] = 0;
+                        unsigned w[4];
+                        if (!whole)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) tmem_ld32(s_at + i * 32, S + i * 32);
-                    tmem_wait_ld();
-                    const bool whole = __all_sync(FULL, (w[0] & w[1] & w[2] & w[3]) == FULL);
-                    if (!whole)
+                            for (int i = 0; i < 4; ++i) w[i] = words.word(j, i);
+                        tmem_ld32(s_at, A);
+                        tmem_wait_ld();
+                        tmem_ld32(s_at + 32, B);
+                        if (!whole) hide(A, 0, w[0]);
+                        weights(A, P, ref2);
+                        tmem_wait_ld();
+                        tmem_ld32(s_at + 64, A);
+                        if (!whole) hide(B, 1, w[1]);
+                        weights(B, P + 16, ref2);
+                        tmem_wait_ld();
+                        tmem_ld32(s_at + 96, B);
+                        if (!whole) hide(A, 2, w[2]);
+                        weights(A, P + 32, ref2);
+                        tmem_wait_ld();
+                        if (!whole) hide(B, 3, w[3]);
+                        weights(B, P + 48, ref2);
+                    }
+                    float sum = total();
+                    const bool redo = !(sum <= 1073741824.f) || M == -INFINITY;      // (a NaN, too)
+                    if (!__any_sync(FULL, redo)) {
+                        tmem_st32(s_at, P);
+                        tmem_st32(s_at + 32, P + 32);
+                    } else {
+                        // The scores once more: their maximum, the sums so far in its terms, the weights.
+                        uint32_t A[32];
+                        float top = -INFINITY;
+#pragma unroll 1
+                        for (int i = 0; i < 4; ++i) {
+                            tmem_ld32(s_at + i * 32, A);
+                            const unsigned w = words.word(j, i);
+                            tmem_wait_ld();
+                            hide(A, i, w);
 #pragma unroll
-                        for (int i = 0; i < KEYS; ++i)
-                            if (!((w[i / 32] >> (i & 31)) & 1)) S[i] = 0xff800000u;      // -inf
-                    float part[4];                                            // (independent chains: each step waits for the one before it)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) part[i] = __uint_as_float(S[i]);
-#pragma unroll
-                    for (int i = 4; i < KEYS; i += 8)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            part[c] = i + 4 + c < KEYS ? fmaxf(fmaxf(part[c], __uint_as_float(S[i + c])), __uint_as_float(S[i + 4 + c])) : fmaxf(part[c], __uint_as_float(S[i + c]));
-                    const float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * sc;
-                    // (a row that has seen nothing yet: top and M may both be -inf)
-                    const bool raise = top > M + 8.f;
-                    if (__any_sync(FULL, raise)) {
-                        const float f = raise ? ex2(M - top) : 1.f;          // (0 the first time)
-                        if (raise) M = top;
+                            for (int c = 0; c < 32; ++c) top = fmaxf(top, __uint_as_float(A[c]));
+                        }
+                        top *= sc;
+                        const float f = redo && top > M ? ex2(M - top) : 1.f;        // (0 the first time)
+                        if (redo && top > M) M = top;
                         L *= f;
-                        if (j) {
-#pragma unroll
+                        if (j)
+#pragma unroll 1
                             for (int i = 0; i < HD / 32; ++i) {
-                                uint32_t o[32];
-                                tmem_ld32(o_at + i * 32, o);
+                                tmem_ld32(o_at + i * 32, A);
                                 tmem_wait_ld();
 #pragma unroll
-                                for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * f);
-                                tmem_st32(o_at + i * 32, o);
+                                for (int c = 0; c < 32; ++c) A[c] = __float_as_uint(__uint_as_float(A[c]) * f);
+                                tmem_st32(o_at + i * 32, A);
                             }
+                        const float ref = M == -INFINITY ? 0.f : M;                  // (a row that has seen nothing yet)
+                        sums[0] = sums[1] = 0;
+#pragma unroll 1
+                        for (int i = 0; i < 4; ++i) {
+                            tmem_ld32(s_at + i * 32, A);
+                            const unsigned w = words.word(j, i);
+                            tmem_wait_ld();
+                            hide(A, i, w);
+                            weights(A, P, pk2(-ref, -ref));
+                            tmem_st16(s_at + i * 16, P);                             // (in place of scores that have been read)
                         }
+                        sum = total();
                     }
-                    const float ref = M == -INFINITY ? 0.f : M;
-                    const uint64_t sc2 = pk2(sc, sc), ref2 = pk2(-ref, -ref);
-                    uint64_t sums[4] = {0, 0, 0, 0};                          // (two zeros each)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t P[32];
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            float p0, p1;
-                            upk2(fma2(pk2(__uint_as_float(S[h * 64 + 2 * i]), __uint_as_float(S[h * 64 + 2 * i + 1])), sc2, ref2), p0, p1);
-                            p0 = ex2(p0);
-                            p1 = ex2(p1);
-                            sums[i & 3] = add2(sums[i & 3], pk2(p0, p1));
-                            P[i] = pack_bf16(p0, p1);
-                        }
-                        tmem_st32(s_at + h * 32, P);
-                    }
-                    {
-                        float u, v;
-                        upk2(add2(add2(sums[0], sums[1]), add2(sums[2], sums[3])), u, v);
-                        L += u + v;
-                    }
+                    L += sum;
                     tmem_wait_st();
                     tc_fence_before();
                     mbar_arrive(p_full(t));
