@@ -296,7 +296,6 @@ ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, i
         int row = 0;
         s.n = s.items = 0;
         auto flush = [&]() {
-            s.item[s.n] = s.items;
             const ebrl_status_t r = launched(launch_append(a, s, sm_quota, (cudaStream_t)stream));
             s.n = s.items = 0;
             return r;
@@ -304,7 +303,7 @@ ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, i
         for (int i = 0; i < n; ++i) {
             if (new_tokens[i] == 0) continue;
             const int start = len[i] - new_tokens[i];
-            s.row[s.n] = row; s.new_tokens[s.n] = new_tokens[i]; s.len[s.n] = len[i]; s.tab[s.n] = i; s.item[s.n] = s.items;
+            s.s[s.n] = {s.items, row, new_tokens[i], len[i], i};
             s.items += (len[i] + WORD - 1) / WORD - start / WORD;
             row += new_tokens[i];
             if (++s.n == SEQS && (st = flush()) != EBRL_OK) return st;
@@ -388,27 +387,26 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
                     const int64_t mine = (((int64_t)new_tokens[i] * a.G + gr.rows - 1) / gr.rows) * g.kvh * np;
                     if (mine > 1 << 30) return fail(EBRL_ERR_UNSUPPORTED, "too many pieces in one sequence");
                     if (items + mine > 1 << 30) break;
-                    s.row[s.n] = (int)p.row[i]; s.m[s.n] = new_tokens[i]; s.len[s.n] = len[i]; s.tab[s.n] = i;
-                    s.item[s.n] = (int)items;
-                    s.part[s.n] = np > 1 ? (int)pair : -1;
+                    s.s[s.n] = {(int)items, (int)p.row[i], new_tokens[i], len[i], i, np > 1 ? (int)pair : -1};
                     if (np > 1) { pair += (int64_t)np * new_tokens[i]; any = true; }
                     items += mine;
                     ++s.n;
                 }
-                s.item[s.n] = s.items = (int)items;
+                s.items = (int)items;
                 st = launched(gr.rows == CHUNK_ROWS ? launch_chunk(a, s, sm_quota, (cudaStream_t)stream) : launch_attend(a, s, f32, gr.rows, sm_quota, (cudaStream_t)stream));
                 if (st != EBRL_OK) return st;
                 if (!any) continue;
                 // the join's items are the queries of the cut sequences
                 int k = 0, queries = 0;
                 for (int j = 0; j < s.n; ++j) {
-                    if (s.part[j] < 0) continue;
-                    s.row[k] = s.row[j]; s.m[k] = s.m[j]; s.len[k] = s.len[j]; s.part[k] = s.part[j]; s.item[k] = queries;
-                    queries += s.m[j];
+                    if (s.s[j].part < 0) continue;
+                    s.s[k] = s.s[j];
+                    s.s[k].item = queries;
+                    queries += s.s[k].m;
                     ++k;
                 }
                 s.n = k;
-                s.item[k] = s.items = queries;
+                s.items = queries;
                 if ((st = launched(launch_attend_join(a, s, f32, sm_quota, sms, (cudaStream_t)stream))) != EBRL_OK) return st;
             }
         }
@@ -470,18 +468,16 @@ ebrl_status_t ebrl_pages_gather(const ebrl_pages_layout_t *layout, const void *p
         int sms = 0;
         if ((st = device_sms(sm_quota, &sms)) != EBRL_OK) return st;
         const Pages p = {(char *)const_cast<void *>(pool), n_pages, table, table_stride};
-        for (int first = 0; first < n; first += SEQS) {
+        for (int first = 0; first < n; first += GATHER_SEQS) {
             GatherSeqs &s = t_gather;
-            s.n = std::min(SEQS, n - first);
+            s.n = std::min(GATHER_SEQS, n - first);
             s.first = first;
             s.items = 0;
             for (int i = 0; i < s.n; ++i) {
                 const int k = first + i;
-                s.planes[i] = planes[k]; s.mask[i] = mask ? mask[k] : nullptr; s.len[i] = len[k]; s.plane_rows[i] = plane_rows ? plane_rows[k] : len[k];
-                s.item[i] = s.items;
+                s.s[i] = {planes[k], mask ? mask[k] : nullptr, s.items, len[k], plane_rows ? plane_rows[k] : len[k]};
                 s.items += (len[k] + WORD - 1) / WORD;
             }
-            s.item[s.n] = s.items;
             if ((st = launched(launch_gather(g, p, row_stride * g.es, s, sm_quota, (cudaStream_t)stream))) != EBRL_OK) return st;
         }
         return EBRL_OK;

@@ -21,9 +21,9 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 template <int HD, int MT, bool F32> struct Cfg {
     static constexpr int ES = F32 ? 4 : 2, RB = HD * ES;                 // bytes of a row
-    static constexpr int TK = RB == 512 ? 16 : 32;                       // tokens of a tile
+    static constexpr int TK = F32 && HD >= 64 ? 16 : 32;                 // tokens of a tile
     static constexpr int TILE = TK * RB, Q_BYTES = 16 * MT * RB;
-    static constexpr int WARPS = RB >= 256 ? 4 : (RB == 128 ? 8 : 12);   // per SM
+    static constexpr int WARPS = HD == 128 ? 4 : (RB >= 128 ? 8 : 12);   // per SM
     static constexpr int ROOM = (224 * 1024 / WARPS - Q_BYTES) / (2 * TILE);
     static constexpr int STAGES = ROOM < 4 ? ROOM : 4;
     static constexpr int WARP_BYTES = STAGES * 2 * TILE + Q_BYTES;
@@ -102,14 +102,9 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
 
     for (int x = TEAM ? blockIdx.x : warp * gridDim.x + blockIdx.x; x < sq.items; x += gridDim.x * (TEAM ? 1 : warps)) {
         // which item this is
-        int s = 0, hi_s = sq.n - 1;
-        while (s < hi_s) {
-            const int mid = (s + hi_s + 1) / 2;
-            if (sq.item[mid] <= x) s = mid;
-            else hi_s = mid - 1;
-        }
-        const int m = sq.m[s], len = sq.len[s], R = m * G, RT = (R + ROWS - 1) / ROWS;
-        int rest = x - sq.item[s];
+        const AttendSeq seq = sq.s[find_seq(sq.n, x, [&](int i) { return sq.s[i].item; })];
+        const int m = seq.m, len = seq.len, R = m * G, RT = (R + ROWS - 1) / ROWS;
+        int rest = x - seq.item;
         const int rt = rest % RT; rest /= RT;
         const int kh = rest % kvh, piece = rest / kvh;
         const int r0 = rt * ROWS, r1 = min(R, r0 + ROWS);                 // its rows; row = token * G + member
@@ -133,12 +128,12 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
         // queries into shared memory
         for (int c = lane; c < ROWS * PIECES; c += 32) {
             const int r = c / PIECES, p = c % PIECES, row = min(r0 + r, R - 1), tok = row / G;
-            const char *src = a.q + (((long long)sq.row[s] + tok) * a.q_stride + (long long)(kh * G + row - tok * G) * HD) * C::ES + p * 16;
+            const char *src = a.q + (((long long)seq.row + tok) * a.q_stride + (long long)(kh * G + row - tok * G) * HD) * C::ES + p * 16;
             cp16(q_at + tile_at<RB>(r, p), src, r0 + r < R ? 16 : 0);
         }
 
         // A batch of 32 mask words' pages and bits, one per lane; the next one is on its way while this one is used.
-        const int *tab = a.p.table + sq.tab[s] * a.p.stride;
+        const int *tab = a.p.table + seq.tab * a.p.stride;
         const int word0 = lo / WORD, words = (hi + WORD - 1) / WORD;
         auto look_up = [&](int base, int &page, unsigned &bits) {
             const int w = base + lane;
@@ -399,17 +394,17 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
         __syncwarp();
 
         // Where a row's result goes: the output, or the piece's partial result.
-        const bool cut = a.split && sq.part[s] >= 0;
+        const bool cut = a.split && seq.part >= 0;
         auto finish = [&](int row, int col, const float *v, int nv, float top, float sum) {   // nv consecutive columns of a row
             const int tok = row / G, head = kh * G + row - tok * G;
             if (cut) {
-                const size_t at = ((size_t)sq.part[s] + (size_t)piece * m + tok) * a.heads + head;
+                const size_t at = ((size_t)seq.part + (size_t)piece * m + tok) * a.heads + head;
                 for (int c = 0; c < nv; ++c) a.part_o[at * HD + col + c] = v[c];
                 if (col == 0) { a.part_ml[2 * at] = top; a.part_ml[2 * at + 1] = sum; }
                 return;
             }
             const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            const size_t r = (size_t)sq.row[s] + tok;
+            const size_t r = (size_t)seq.row + tok;
             char *o = a.out + (r * a.o_stride + (size_t)head * HD + col) * C::ES;
             if constexpr (F32) { for (int c = 0; c < nv; ++c) ((float *)o)[c] = v[c] * inv; }
             else { for (int c = 0; c < nv; c += 2) ((uint32_t *)o)[c / 2] = pack_bf16(v[c] * inv, v[c + 1] * inv); }
@@ -469,14 +464,9 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
     const long long rows = (long long)sq.items * a.heads;      // (items: the queries of the cut sequences, counted in sq.item)
     for (long long x = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); x < rows; x += (long long)gridDim.x * 8) {
         const int r = (int)(x / a.heads), head = (int)(x - (long long)r * a.heads);
-        int s = 0, hi = sq.n - 1;
-        while (s < hi) {
-            const int mid = (s + hi + 1) / 2;
-            if (sq.item[mid] <= r) s = mid;
-            else hi = mid - 1;
-        }
-        const int tok = r - sq.item[s], m = sq.m[s], np = pieces_of(sq.len[s], m, a.window, a.split);
-        const size_t at0 = ((size_t)sq.part[s] + tok) * a.heads + head, step = (size_t)m * a.heads;
+        const AttendSeq seq = sq.s[find_seq(sq.n, r, [&](int i) { return sq.s[i].item; })];
+        const int tok = r - seq.item, m = seq.m, np = pieces_of(seq.len, m, a.window, a.split);
+        const size_t at0 = ((size_t)seq.part + tok) * a.heads + head, step = (size_t)m * a.heads;
         float top = -INFINITY, sum = 0.f;
         for (int p = lane; p < np; p += 32) top = fmaxf(top, a.part_ml[2 * (at0 + p * step)]);
 #pragma unroll
@@ -493,7 +483,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
             for (int c = 0; c < W; ++c) v[c] = fmaf(f, o[c], v[c]);
         }
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        const size_t row = (size_t)sq.row[s] + tok, at = row * a.o_stride + (size_t)head * HD + lane * W;
+        const size_t row = (size_t)seq.row + tok, at = row * a.o_stride + (size_t)head * HD + lane * W;
 #pragma unroll
         for (int c = 0; c < W; ++c) {
             if constexpr (F32) ((float *)a.out)[at + c] = v[c] * inv;
@@ -504,14 +494,14 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 }
 
 int attend_rows(int rows) { return rows <= 16 ? 16 : 32; }
-int attend_warps(int hd, bool f32) { return hd * (f32 ? 4 : 2) >= 256 ? 4 : (hd * (f32 ? 4 : 2) == 128 ? 8 : 12); }
+int attend_warps(int hd, bool f32) { return hd == 128 ? 4 : (hd * (f32 ? 4 : 2) >= 128 ? 8 : 12); }
 
 namespace {
 
 template <int HD, int MT, bool F32, bool TEAM> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st)
 {
     using C = Cfg<HD, MT, F32>;
-    static_assert(C::WARPS == (C::RB >= 256 ? 4 : (C::RB == 128 ? 8 : 12)), "attend_warps");
+    static_assert(C::WARPS == (HD == 128 ? 4 : (C::RB >= 128 ? 8 : 12)), "attend_warps");
     static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;

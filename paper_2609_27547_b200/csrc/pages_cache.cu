@@ -15,31 +15,19 @@ constexpr int SLICE = 1024;                          // bytes of a token's row t
 __device__ __forceinline__ uint4 read16(const char *p) { return __ldcs(reinterpret_cast<const uint4 *>(p)); }
 __device__ __forceinline__ void write16(char *p, uint4 v) { *reinterpret_cast<uint4 *>(p) = v; }
 
-// The sequence that item x belongs to: the last one whose first item is not above it.
-template <typename S> __device__ __forceinline__ int seq_of(const S &s, int x)
-{
-    int lo = 0, hi = s.n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (s.item[mid] <= x) lo = mid;
-        else hi = mid - 1;
-    }
-    return lo;
-}
-
 __global__ void append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ AppendSeqs s, int slices)
 {
     const int row_bytes = a.g.kvh * a.g.hd * a.g.es, head_bytes = a.g.hd * a.g.es;
     const long long items = (long long)s.items * 2 * slices;
     for (long long x = blockIdx.x; x < items; x += gridDim.x) {
         const int slice = (int)(x % slices), plane = (int)(x / slices) & 1, word = (int)(x / (2 * slices));
-        const int i = seq_of(s, word), start = s.len[i] - s.new_tokens[i];
-        const int base = (start / WORD + word - s.item[i]) * WORD;                     // the word's first token
-        const int t0 = max(start, base), t1 = min(s.len[i], base + WORD);
-        const int page = a.p.table[s.tab[i] * a.p.stride + (base >> a.g.t_shift)];
+        const AppendSeqs::Seq q = s.s[find_seq(s.n, word, [&](int i) { return s.s[i].item; })];
+        const int start = q.len - q.new_tokens, base = (start / WORD + word - q.item) * WORD;   // (the word's first token)
+        const int t0 = max(start, base), t1 = min(q.len, base + WORD);
+        const int page = a.p.table[q.tab * a.p.stride + (base >> a.g.t_shift)];
         if ((unsigned)page >= (unsigned)a.p.n_pages) continue;
         char *at = a.p.pool + (size_t)page * a.g.bytes;
-        const long long row0 = (long long)s.row[i] - start;                            // packed row of token t: row0 + t
+        const long long row0 = (long long)q.row - start;                            // packed row of token t: row0 + t
         const int slot0 = base & (a.g.T - 1);
         if (plane == 0 && slice == 0 && threadIdx.x < 32) {
             const int t = base + threadIdx.x;
@@ -103,15 +91,17 @@ __global__ void gather_kernel(const __grid_constant__ Geometry g, const __grid_c
     const long long items = (long long)s.items * planes * slices;
     for (long long x = blockIdx.x; x < items; x += gridDim.x) {
         const int slice = (int)(x % slices), plane = (int)(x / slices % planes), word = (int)(x / ((long long)slices * planes));
-        const int i = seq_of(s, word), base = (word - s.item[i]) * WORD, t1 = min(s.len[i], base + WORD);
+        const int i = find_seq(s.n, word, [&](int k) { return s.s[k].item; });
+        const GatherSeqs::Seq q = s.s[i];
+        const int base = (word - q.item) * WORD, t1 = min(q.len, base + WORD);
         const int page = p.table[(s.first + i) * p.stride + (base >> g.t_shift)], slot0 = base & (g.T - 1);
         const bool there = (unsigned)page < (unsigned)p.n_pages;
         const char *at = p.pool + (there ? (size_t)page * g.bytes : 0);
         const unsigned see = there ? reinterpret_cast<const unsigned *>(at + g.mask)[slot0 / WORD] : 0u;
-        if (plane == 0 && slice == 0 && s.mask[i] && threadIdx.x < t1 - base) s.mask[i][base + threadIdx.x] = (see >> threadIdx.x) & 1;
+        if (plane == 0 && slice == 0 && q.mask && threadIdx.x < t1 - base) q.mask[base + threadIdx.x] = (see >> threadIdx.x) & 1;
         const int c0 = slice * SLICE, c1 = min(row_bytes, c0 + SLICE), per = (c1 - c0) / 16, n = (t1 - base) * per;
         const char *src = at + (size_t)plane * g.kvh * g.head;
-        char *dst = (char *)s.planes[i] + ((size_t)plane * s.plane_rows[i] + base) * row_stride;
+        char *dst = (char *)q.planes + ((size_t)plane * q.plane_rows + base) * row_stride;
 #pragma unroll 4
         for (int c = threadIdx.x; c < n; c += blockDim.x) {
             const int r = c / per, col = c0 + (c - r * per) * 16, h = col / head_bytes;

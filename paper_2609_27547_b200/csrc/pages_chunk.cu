@@ -131,21 +131,16 @@ __host__ __device__ constexpr uint32_t instr_desc(int N, bool values)
 }
 
 // An item and the tokens lo .. hi (lo a multiple of 128) that some row of it sees.
-struct Item { int s, m, len, R, r0, tiles, kh, piece, lo, hi, seen, n_kv; };   // (seen: no row sees a token below)
+struct Item { int row, tab, part, m, len, R, r0, tiles, kh, piece, lo, hi, seen, n_kv; };   // (seen: no row sees a token below)
 
 __device__ __forceinline__ Item item_of(const AttendArgs &a, const AttendSeqs &sq, int x)
 {
     Item it;
-    int s = 0, top = sq.n - 1;
-    while (s < top) {
-        const int mid = (s + top + 1) / 2;
-        if (sq.item[mid] <= x) s = mid;
-        else top = mid - 1;
-    }
-    it.s = s; it.m = sq.m[s]; it.len = sq.len[s];
+    const AttendSeq seq = sq.s[find_seq(sq.n, x, [&](int i) { return sq.s[i].item; })];
+    it.m = seq.m; it.len = seq.len; it.row = seq.row; it.part = seq.part; it.tab = seq.tab;
     it.R = it.m * a.G;
     const int RT = (it.R + 2 * ROWS - 1) / (2 * ROWS);
-    int rest = x - sq.item[s];
+    int rest = x - seq.item;
     const int kh = rest % a.g.kvh; rest /= a.g.kvh;
     const int rt = RT - 1 - rest % RT;                        // the last rows see most
     it.kh = kh; it.piece = rest / RT;
@@ -249,7 +244,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         uint32_t phase = 0;
         for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
             const Item it = item_of(a, sq, x);
-            const int *tab = a.p.table + sq.tab[it.s] * a.p.stride;
+            const int *tab = a.p.table + it.tab * a.p.stride;
             const int first_page = it.lo >> a.g.t_shift, n_pages = it.hi > 0 ? (it.hi - 1) / a.g.T + 1 : 0;   // (of the sequence, those below n_pages hold tokens that are seen)
             auto fetch = [&](int p) {
                 const int page = p < n_pages ? tab[p] : -1;
@@ -320,7 +315,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
             const Item it = item_of(a, sq, x);
             if (it.n_kv == 0) continue;
             Words words;
-            words.start(a, a.p.table + sq.tab[it.s] * a.p.stride, it, lane);
+            words.start(a, a.p.table + it.tab * a.p.stride, it, lane);
             // the first keys: S of both tiles
             wait(full(stage), phase);
             for (int t = 0; t < it.tiles && ok; ++t) {
@@ -380,7 +375,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 // queries: every product that read the last item's is done (its results were waited for)
                 for (int c = tid; c < ROWS * (HD / 8); c += ROWS) {
                     const int r = c / (HD / 8), p = c % (HD / 8), qr = min(r0 + r, it.R - 1), tok = qr / a.G;
-                    const char *src = a.q + (((long long)sq.row[it.s] + tok) * a.q_stride + (long long)(it.kh * a.G + qr - tok * a.G) * HD + p * 8) * 2;
+                    const char *src = a.q + (((long long)it.row + tok) * a.q_stride + (long long)(it.kh * a.G + qr - tok * a.G) * HD + p * 8) * 2;
                     constexpr int PP = C::SWZ / 16;
                     const int sw = C::SWZ == 128 ? (r & 7) : ((r >> 1) & 3);
                     cp16(q_at + t * C::TILE + (p / PP) * C::HALF + r * C::SWZ + (((p % PP) ^ sw) << 4), src, r0 + r < it.R ? 16 : 0);
@@ -389,7 +384,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 fence_proxy_async();
                 mbar_arrive(q_full(t));
                 Words words;
-                words.start(a, a.p.table + sq.tab[it.s] * a.p.stride, it, lane);
+                words.start(a, a.p.table + it.tab * a.p.stride, it, lane);
                 const int last = a.causal ? first + tok_q + 1 : 0x7fffffff, from = a.window ? first + tok_q + 1 - a.window : -0x7fffffff;
                 const int all_last = __reduce_min_sync(FULL, last), all_from = __reduce_max_sync(FULL, from);   // what every row of the warp sees
                 const uint64_t sc2 = pk2(sc, sc);
@@ -511,10 +506,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 tc_fence_after();
             }
             // the result: the output, or the piece's partial one
-            const bool mine = r0 + tid < it.R, cut = a.split && sq.part[it.s] >= 0;
+            const bool mine = r0 + tid < it.R, cut = a.split && it.part >= 0;
             const float inv = L == 0.f ? 0.f : 1.f / L;
-            const size_t out_row = (size_t)sq.row[it.s] + tok_q;
-            const size_t at = cut ? ((size_t)sq.part[it.s] + (size_t)it.piece * it.m + tok_q) * a.heads + head : 0;
+            const size_t out_row = (size_t)it.row + tok_q;
+            const size_t at = cut ? ((size_t)it.part + (size_t)it.piece * it.m + tok_q) * a.heads + head : 0;
             __nv_bfloat16 *out = reinterpret_cast<__nv_bfloat16 *>(a.out) + out_row * a.o_stride + (size_t)head * HD;
 #pragma unroll
             for (int i = 0; i < HD / 32; ++i) {

@@ -35,7 +35,7 @@ struct Pages {
 
 struct AppendSeqs {
     int n, items;                            // an item: a mask word that new tokens fall into
-    int row[SEQS], new_tokens[SEQS], len[SEQS], tab[SEQS], item[SEQS + 1];   // first packed row; row of the table; first item
+    struct Seq { int item, row, new_tokens, len, tab; } s[SEQS];   // first item; first packed row; row of the table
 };
 struct AppendArgs {
     Geometry g;
@@ -51,22 +51,23 @@ constexpr int COPY_PAGES = 2048;
 struct CopyPages { int n, from[COPY_PAGES], to[COPY_PAGES], tokens[COPY_PAGES]; };
 cudaError_t launch_copy(const Geometry &g, const char *src, char *dst, const CopyPages &c, int quota, cudaStream_t st);
 
+constexpr int GATHER_SEQS = 512;  // (32 bytes each)
 struct GatherSeqs {
     int n, items;                            // an item: 32 tokens
-    void *planes[SEQS];
-    uint8_t *mask[SEQS];
-    int len[SEQS], plane_rows[SEQS], item[SEQS + 1];
+    struct Seq { void *planes; uint8_t *mask; int item, len, plane_rows; } s[GATHER_SEQS];
     int first;                               // row of the table of sequence 0
 };
 cudaError_t launch_gather(const Geometry &g, const Pages &p, long long row_stride, const GatherSeqs &s, int quota, cudaStream_t st);
 
 // ---- attend ----
 
+struct AttendSeq {
+    int item, row, m, len, tab;                        // first item; first packed query; queries; length; row of the table
+    int part;                                          // first (query, piece) pair of the partial results; -1: not cut
+};
 struct AttendSeqs {
     int n, items;
-    int row[SEQS], m[SEQS], len[SEQS], tab[SEQS];      // first packed query; queries; length; row of the table
-    int item[SEQS + 1];                                // first item
-    int part[SEQS];                                    // first (query, piece) pair of the partial results; -1: not cut
+    AttendSeq s[SEQS];
 };
 struct AttendArgs {
     Geometry g;
@@ -107,6 +108,21 @@ cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, cu
 
 // Whether a bounded wait ran out on the current device since the last call (waits for the device).
 cudaError_t take_status(int *status);
+
+#ifdef __CUDACC__
+// The last of n (at most 1024) whose first item, at(i), is not above x; by all lanes of a warp.  Two looks at 32 of them at once: a search by halves
+// meets a miss of the constant cache, where kernel parameters are read, at every step (a microsecond each at a launch's start).
+template <typename F> __device__ __forceinline__ int find_seq(int n, int x, F at)
+{
+    const int lane = threadIdx.x & 31, step = (n + 31) / 32;
+    int i = lane * step, base = (__popc(__ballot_sync(0xffffffffu, i < n && at(i) <= x)) - 1) * step;
+    if (step > 1) {
+        i = base + lane;
+        base += __popc(__ballot_sync(0xffffffffu, lane < step && i < n && at(i) <= x)) - 1;
+    }
+    return base;
+}
+#endif
 
 }  // namespace pg
 }  // namespace ebrl
