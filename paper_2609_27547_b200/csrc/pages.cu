@@ -150,10 +150,10 @@ struct Group {
 };
 
 // Rows from which the tensor-memory kernel takes a sequence.
-constexpr int CHUNK_FROM = 64;
+constexpr int CHUNK_FROM = 16;
 
 struct Plan {
-    Group groups[3];                 // 16 rows, 32 rows, CHUNK_ROWS
+    Group groups[3];                 // CHUNK_ROWS, 32 rows, 16 rows: in this order, so that short items fill up what long ones leave
     std::vector<int64_t> row;        // first packed query of each sequence
     uint64_t pairs = 0;              // (query, piece) pairs of the sequences that are cut
 };
@@ -163,40 +163,61 @@ int tiles_of(int len, int m, int window)   // mask words that a sequence's longe
     return (len - first_token(len, m, window) + WORD - 1) / WORD;
 }
 
-// How a group's sequences are cut.  Left to itself (asked = 0): where the longest item takes clearly longer than an even share of the
-// warps that the SMs hold, it is shared by a team of warps, and where that does not do, cut into pieces of a team of four each.
+// How long a group takes, in tiles, where `slots` items are worked on at a time, each sequence is cut into pieces of `piece` tiles and an item is shared by a
+// team of warps: the longest piece, or an even share of all there is and, where there is more than one round, half a piece that some wait for.  An item's
+// beginning and end cost 3 tiles.
+double time_of(const std::vector<int> &tiles, const std::vector<int64_t> &items, double slots, int piece, int team)
+{
+    double all = 0, count = 0;
+    int longest = 0;
+    for (size_t k = 0; k < tiles.size(); ++k) {
+        const int n = (tiles[k] + piece - 1) / piece;
+        longest = std::max(longest, std::min(piece, tiles[k]));
+        count += (double)items[k] * n;
+        all += (double)items[k] * ((double)tiles[k] / team + 3 * n);
+    }
+    const double one = (double)longest / team + 3;
+    return std::max(one, all / slots + (count > slots ? one / 2 : 0));
+}
+
+// How a group's sequences are cut.  Left to itself (asked = 0): an item is shared by the team of warps for which time_of is least (16 or 32 rows, no quota), and
+// long sequences are cut into the pieces for which it is, where that saves more than the join costs.
 void cut(const ebrl_pages_layout_t &l, Group &g, const int32_t *m, const int32_t *len, int G, int window, int asked, int quota, int sms)
 {
     if (asked < 0) return;
     if (asked > 0) { g.split = asked; return; }
     const bool chunk = g.rows == CHUNK_ROWS;
-    const int warps = chunk ? 1 : attend_warps(l.head_dim, l.dtype == EBRL_F32);   // items that an SM works on at a time
-    const int tile = chunk ? 4 : 1;                                                // mask words of a tile
-    double total = 0;
-    int longest = 0;
+    const int warps = chunk ? 1 : attend_warps(l.head_dim, l.dtype == EBRL_F32, g.rows);   // items that an SM works on at a time
+    const int tile = chunk ? 4 : 1;                                                        // mask words of a tile
+    const int at_once = quota ? std::min(sms, quota) : sms;
+    auto slots = [&](int team) { return (double)at_once * (warps / team); };
+    std::vector<int> tiles;
+    std::vector<int64_t> items;
+    double all = 0;
+    int longest = 1;
+    double rows = 0;                                                                       // of all heads
     for (int i : g.seqs) {
-        const int t = (tiles_of(len[i], m[i], window) + tile - 1) / tile;
-        total += (double)t * l.n_kv_heads * (((int64_t)m[i] * G + g.rows - 1) / g.rows);
-        longest = std::max(longest, t);
+        rows += (double)m[i] * G * l.n_kv_heads;
+        tiles.push_back((tiles_of(len[i], m[i], window) + tile - 1) / tile);
+        items.push_back((int64_t)l.n_kv_heads * (((int64_t)m[i] * G + g.rows - 1) / g.rows));
+        all += (double)items.back();
+        longest = std::max(longest, tiles.back());
     }
-    const double per = std::max(1., total / ((double)(quota ? std::min(sms, quota) : sms) * warps)), want = longest / per;
-    if (chunk) {
-        if (want > 1.75 && longest >= 8) g.split = (int)std::max(4., std::ceil(per)) * tile * WORD;
-        return;
+    if (all >= 8 * slots(1)) return;                    // (many rounds: nothing to gain)
+    double best = time_of(tiles, items, slots(1), longest, 1);
+    if (!chunk && !quota)
+        for (int team = 2; team <= std::min(8, warps); team *= 2) {
+            const double t = time_of(tiles, items, slots(team), longest, team) + 1;              // (their join)
+            if (t < .95 * best) { best = t; g.team = team; }
+        }
+    if (tiles.size() > 64 || longest * tile < 32) return;
+    const int team = chunk || quota ? 1 : 4, step = chunk ? 1 : 4;                         // pieces are multiples of 128 tokens
+    for (int pieces = 2; pieces <= 64 && longest / pieces >= 4 * team; ++pieces) {
+        const int piece = ((longest + pieces - 1) / pieces + step - 1) / step * step;
+        // the join: a launch, and the partial results written and read, 8 MB in the time of a tile (1 - 2 us)
+        const double t = time_of(tiles, items, slots(team), piece, team) + 6 + rows * pieces * l.head_dim * 8 / 8e6;
+        if (t < .95 * best) { best = t; g.team = team; g.split = piece * tile * WORD; }
     }
-    if (quota) {
-        if (want > 1.75 && longest >= 16) g.split = (int)((std::max(8., per) * WORD + 127) / 128) * 128;
-        return;
-    }
-    if (want < 1.75) return;
-    const int most = std::min(8, warps);
-    if (want > 1.5 * most && longest >= 64) {
-        g.team = 4;
-        g.split = (int)((std::max(4., per) * 4 * WORD + 127) / 128) * 128;
-        return;
-    }
-    g.team = want >= 6 ? 8 : (want >= 3 ? 4 : 2);
-    while (g.team > 1 && (g.team > most || g.team > longest)) g.team /= 2;
 }
 
 void plan(Plan &p, const ebrl_pages_layout_t &l, int32_t n, const int32_t *m, const int32_t *len, int n_heads, int window, int asked, int quota, int sms, bool chunks)
@@ -210,7 +231,7 @@ void plan(Plan &p, const ebrl_pages_layout_t &l, int32_t n, const int32_t *m, co
         if (m[i] == 0) continue;
         const int64_t all = (int64_t)m[i] * G;
         const int rows = chunks && all > CHUNK_FROM ? CHUNK_ROWS : attend_rows((int)std::min<int64_t>(all, 1 << 20));
-        Group &g = p.groups[rows == 16 ? 0 : (rows == 32 ? 1 : 2)];
+        Group &g = p.groups[rows == 16 ? 2 : (rows == 32 ? 1 : 0)];
         g.rows = rows;
         g.seqs.push_back(i);
     }
@@ -376,6 +397,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
         const bool f32 = layout->dtype == EBRL_F32;
         AttendSeqs &s = t_attend;
         int64_t pair = 0;
+        bool beside = false;             // whether a kernel of this call is before this one (a quota allows one at a time; a join waits for all)
         for (const Group &gr : p.groups) {
             a.split = gr.split; a.team = gr.team;
             for (size_t at = 0; at < gr.seqs.size();) {
@@ -393,7 +415,9 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
                     ++s.n;
                 }
                 s.items = (int)items;
-                st = launched(gr.rows == CHUNK_ROWS ? launch_chunk(a, s, sm_quota, (cudaStream_t)stream) : launch_attend(a, s, f32, gr.rows, sm_quota, (cudaStream_t)stream));
+                st = launched(gr.rows == CHUNK_ROWS ? launch_chunk(a, s, sm_quota, beside, (cudaStream_t)stream)
+                                                    : launch_attend(a, s, f32, gr.rows, sm_quota, beside, (cudaStream_t)stream));
+                beside = sm_quota == 0 && !any;
                 if (st != EBRL_OK) return st;
                 if (!any) continue;
                 // the join's items are the queries of the cut sequences

@@ -23,7 +23,7 @@ template <int HD, int MT, bool F32> struct Cfg {
     static constexpr int ES = F32 ? 4 : 2, RB = HD * ES;                 // bytes of a row
     static constexpr int TK = F32 && HD >= 64 ? 16 : 32;                 // tokens of a tile
     static constexpr int TILE = TK * RB, Q_BYTES = 16 * MT * RB;
-    static constexpr int WARPS = HD == 128 ? 4 : (RB >= 128 ? 8 : 12);   // per SM
+    static constexpr int WARPS = HD == 128 ? (F32 ? 4 : (MT == 1 ? 6 : 5)) : (RB >= 128 ? 8 : 12);   // per SM
     static constexpr int ROOM = (224 * 1024 / WARPS - Q_BYTES) / (2 * TILE);
     static constexpr int STAGES = ROOM < 4 ? ROOM : 4;
     static constexpr int WARP_BYTES = STAGES * 2 * TILE + Q_BYTES;
@@ -99,6 +99,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
     __shared__ unsigned stage_word[C::WARPS][C::STAGES];
     const int kvh = a.g.kvh, G = a.G;
     const float sc = a.scale * LOG2E;
+    pdl_launch_dependents();
 
     for (int x = TEAM ? blockIdx.x : warp * gridDim.x + blockIdx.x; x < sq.items; x += gridDim.x * (TEAM ? 1 : warps)) {
         // which item this is
@@ -453,6 +454,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
             __syncthreads();
         }
     }
+    pdl_wait();      // (the end of this kernel is to be that of the ones beside it, too)
 }
 
 // Joins the pieces of cut sequences: one warp per (query, head), sums in the order of the pieces.
@@ -494,14 +496,13 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 }
 
 int attend_rows(int rows) { return rows <= 16 ? 16 : 32; }
-int attend_warps(int hd, bool f32) { return hd == 128 ? 4 : (hd * (f32 ? 4 : 2) >= 128 ? 8 : 12); }
+int attend_warps(int hd, bool f32, int rows) { return hd == 128 ? (f32 ? 4 : (rows == 16 ? 6 : 5)) : (hd * (f32 ? 4 : 2) >= 128 ? 8 : 12); }
 
 namespace {
 
-template <int HD, int MT, bool F32, bool TEAM> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st)
+template <int HD, int MT, bool F32, bool TEAM> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
 {
     using C = Cfg<HD, MT, F32>;
-    static_assert(C::WARPS == (HD == 128 ? 4 : (C::RB >= 128 ? 8 : 12)), "attend_warps");
     static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
@@ -512,25 +513,25 @@ template <int HD, int MT, bool F32, bool TEAM> cudaError_t go(const AttendArgs &
     }
     // Under a quota: persistent CTAs with all of an SM's warps.  Else one CTA per item: the hardware hands out the next as one ends.
     const int warps = TEAM ? a.team : (quota ? C::WARPS : 1), grid = quota && !TEAM && s.items > quota ? quota : s.items;
-    attend_kernel<HD, MT, F32, TEAM><<<grid, warps * 32, warps * C::WARP_BYTES, st>>>(a, s);
-    return cudaGetLastError();
+    const Beside with(beside);
+    return launch_kernel(attend_kernel<HD, MT, F32, TEAM>, grid, warps * 32, (size_t)(warps * C::WARP_BYTES), st, 1, a, s);
 }
 
-template <int HD, bool F32> cudaError_t pick(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, cudaStream_t st)
+template <int HD, bool F32> cudaError_t pick(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, bool beside, cudaStream_t st)
 {
-    if (a.team > 1) return rows == 16 ? go<HD, 1, F32, true>(a, s, quota, st) : go<HD, 2, F32, true>(a, s, quota, st);
-    return rows == 16 ? go<HD, 1, F32, false>(a, s, quota, st) : go<HD, 2, F32, false>(a, s, quota, st);
+    if (a.team > 1) return rows == 16 ? go<HD, 1, F32, true>(a, s, quota, beside, st) : go<HD, 2, F32, true>(a, s, quota, beside, st);
+    return rows == 16 ? go<HD, 1, F32, false>(a, s, quota, beside, st) : go<HD, 2, F32, false>(a, s, quota, beside, st);
 }
 
 }  // namespace
 
-cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, cudaStream_t st)
+cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, bool beside, cudaStream_t st)
 {
     if (s.items == 0) return cudaSuccess;
     switch (a.g.hd) {
-    case 128: return f32 ? pick<128, true>(a, s, rows, quota, st) : pick<128, false>(a, s, rows, quota, st);
-    case 64: return f32 ? pick<64, true>(a, s, rows, quota, st) : pick<64, false>(a, s, rows, quota, st);
-    default: return f32 ? pick<32, true>(a, s, rows, quota, st) : pick<32, false>(a, s, rows, quota, st);
+    case 128: return f32 ? pick<128, true>(a, s, rows, quota, beside, st) : pick<128, false>(a, s, rows, quota, beside, st);
+    case 64: return f32 ? pick<64, true>(a, s, rows, quota, beside, st) : pick<64, false>(a, s, rows, quota, beside, st);
+    default: return f32 ? pick<32, true>(a, s, rows, quota, beside, st) : pick<32, false>(a, s, rows, quota, beside, st);
     }
 }
 

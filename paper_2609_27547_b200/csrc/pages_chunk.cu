@@ -235,6 +235,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(FULL, *tmem_slot, 0);
     bool ok = true;
+    pdl_launch_dependents();
 
     if (warp == 8) {
         // ---- copies: the warp looks pages up, one lane issues
@@ -373,12 +374,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
             float M = -INFINITY, L = 0.f;
             if (it.n_kv) {
                 // queries: every product that read the last item's is done (its results were waited for)
-                for (int c = tid; c < ROWS * (HD / 8); c += ROWS) {
-                    const int r = c / (HD / 8), p = c % (HD / 8), qr = min(r0 + r, it.R - 1), tok = qr / a.G;
-                    const char *src = a.q + (((long long)it.row + tok) * a.q_stride + (long long)(it.kh * a.G + qr - tok * a.G) * HD + p * 8) * 2;
-                    constexpr int PP = C::SWZ / 16;
-                    const int sw = C::SWZ == 128 ? (r & 7) : ((r >> 1) & 3);
-                    cp16(q_at + t * C::TILE + (p / PP) * C::HALF + r * C::SWZ + (((p % PP) ^ sw) << 4), src, r0 + r < it.R ? 16 : 0);
+                constexpr int PIECES = HD / 8, PER_STEP = 32 / PIECES, PP = C::SWZ / 16;     // rows that a warp copies in a step: its own
+                const unsigned long long mine = (unsigned long long)(a.q + (((long long)it.row + tok_q) * a.q_stride + (long long)head * HD) * 2);
+                const int there = min(32, it.R - r0 - (tid & ~31));
+#pragma unroll
+                for (int i = 0; i < 32 / PER_STEP; ++i) {
+                    const int k = i * PER_STEP + lane / PIECES, r = (tid & ~31) + k, p = lane % PIECES, sw = C::SWZ == 128 ? (r & 7) : ((r >> 1) & 3);
+                    const char *src = (const char *)__shfl_sync(FULL, mine, k) + p * 16;
+                    cp16(q_at + t * C::TILE + (p / PP) * C::HALF + r * C::SWZ + (((p % PP) ^ sw) << 4), src, k < there ? 16 : 0);
                 }
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 fence_proxy_async();
@@ -557,6 +560,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
+    pdl_wait();      // (the end of this kernel is to be that of the ones beside it, too)
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
@@ -587,7 +591,7 @@ template <int HD> bool make_map(CUtensorMap *out, const Geometry &g, const Pages
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int HD> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st)
+template <int HD> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
 {
     static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
@@ -600,8 +604,8 @@ template <int HD> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int q
     CUtensorMap tm;
     if (!make_map<HD>(&tm, a.g, a.p)) return cudaErrorInvalidValue;
     // one CTA per item, handed out by the hardware as the ones before end; under a quota persistent ones
-    chunk_kernel<HD><<<quota && s.items > quota ? quota : s.items, THREADS, Shape<HD>::SMEM, st>>>(tm, a, s);
-    return cudaGetLastError();
+    const Beside with(beside);
+    return launch_kernel(chunk_kernel<HD>, quota && s.items > quota ? quota : s.items, THREADS, Shape<HD>::SMEM, st, 1, tm, a, s);
 }
 
 }  // namespace
@@ -611,10 +615,10 @@ bool chunk_supported(const Geometry &g, int n_pages, float scale)
     return g.es == 2 && scale > 0.f && (long long)g.layers * 2 * g.kvh * g.T <= INT32_MAX && n_pages < INT32_MAX;
 }
 
-cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st)
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
 {
     if (s.items == 0) return cudaSuccess;
-    return a.g.hd == 128 ? go<128>(a, s, quota, st) : (a.g.hd == 64 ? go<64>(a, s, quota, st) : go<32>(a, s, quota, st));
+    return a.g.hd == 128 ? go<128>(a, s, quota, beside, st) : (a.g.hd == 64 ? go<64>(a, s, quota, beside, st) : go<32>(a, s, quota, beside, st));
 }
 
 cudaError_t take_status(int *status)

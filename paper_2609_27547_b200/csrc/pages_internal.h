@@ -96,15 +96,25 @@ __host__ __device__ inline int pieces_of(int len, int m, int window, int split)
     return split && n > split ? (int)(((long long)n + split - 1) / split) : 1;
 }
 
+// A launch that may begin as soon as the CTAs of the one before it have begun (beside: they share nothing but what both read), and ends after it: the kernels
+// of one call take turns at the SMs without a gap.
+struct Beside {
+    const bool before = pdl_enabled();
+    explicit Beside(bool on) { pdl_set(on); }
+    ~Beside() { pdl_set(before); }
+    Beside(const Beside &) = delete;
+    Beside &operator=(const Beside &) = delete;
+};
+
 int attend_rows(int rows);                             // query rows of an item
-int attend_warps(int hd, bool f32);                    // warps that an SM holds
-cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, cudaStream_t st);
+int attend_warps(int hd, bool f32, int rows);          // warps that an SM holds
+cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, bool beside, cudaStream_t st);
 cudaError_t launch_attend_join(const AttendArgs &a, const AttendSeqs &s, bool f32, int quota, int sms, cudaStream_t st);
 
 // The same for many query rows, bf16 (pages_chunk.cu): 256 of them an item, one CTA each.
 constexpr int CHUNK_ROWS = 256;
 bool chunk_supported(const Geometry &g, int n_pages, float scale);
-cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, cudaStream_t st);
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st);
 
 // Whether a bounded wait ran out on the current device since the last call (waits for the device).
 cudaError_t take_status(int *status);
