@@ -66,6 +66,11 @@ __device__ __forceinline__ void mma_tf32(float *c, const uint32_t *a, const uint
     asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]));
 }
+__device__ __forceinline__ void mma_tf32_first(float *c, const uint32_t *a, const uint32_t *b)   // c = a b
+{
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b[0]), "r"(b[1]), "f"(0.f));
+}
 // x as two tf32 terms: the first rounded to 11 bits (2^-11 of x is left), the second cut to 11 bits by the tensor core, which ignores the
 // low 13 (2^-21 of x is lost).  Plain integer instructions: the conversion instruction runs at a sixteenth of their rate.
 __device__ __forceinline__ void two_terms(float x, uint32_t &hi, uint32_t &lo)
@@ -93,12 +98,15 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
 {
     using C = Cfg<HD, MT, F32>;
     constexpr int RB = C::RB, TK = C::TK, PIECES = RB / 16, ROWS = 16 * MT, NT = TK / 8, NV = HD / 8;
-    extern __shared__ __align__(128) char smem[];
+    extern __shared__ __align__(1024) char smem[];
     const int warps = blockDim.x >> 5, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const uint32_t ring = ptx::smem_u32(smem + (size_t)warp * C::WARP_BYTES), q_at = ring + C::STAGES * 2 * C::TILE;
     __shared__ unsigned stage_word[C::WARPS][C::STAGES];
     const int kvh = a.g.kvh, G = a.G;
     const float sc = a.scale * LOG2E;
+    // Where a lane reads: piece p of its row stands at the address of piece 0 (or 1) with the bits of 16 p flipped.
+    const uint32_t q_off = tile_at<RB>(lane & 15, lane >> 4), k_off = tile_at<RB>((lane & 7) + ((lane >> 4) << 3), (lane >> 3) & 1);
+    const uint32_t v_off[2] = {F32 ? tile_at<RB>(2 * t, g >> 2) + (g & 3) * 4 : q_off, F32 ? tile_at<RB>(2 * t + 1, g >> 2) + (g & 3) * 4 : 0};
     pdl_launch_dependents();
 
     for (int x = TEAM ? blockIdx.x : warp * gridDim.x + blockIdx.x; x < sq.items; x += gridDim.x * (TEAM ? 1 : warps)) {
@@ -221,11 +229,11 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
                     for (int k = 0; k < HD / 16; ++k) {
                         uint32_t qa[MT][4];
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) ldsm4(q_at + tile_at<RB>(i * 16 + (lane & 15), k * 2 + (lane >> 4)), qa[i]);
+                        for (int i = 0; i < MT; ++i) ldsm4((q_at + i * 16 * RB + q_off) ^ (k * 32), qa[i]);
 #pragma unroll
                         for (int n = 0; n < NT; n += 2) {
                             uint32_t kb[4];
-                            ldsm4(kt + tile_at<RB>(n * 8 + (lane & 7) + ((lane >> 4) << 3), k * 2 + ((lane >> 3) & 1)), kb);
+                            ldsm4((kt + n * 8 * RB + k_off) ^ (k * 32), kb);
 #pragma unroll
                             for (int i = 0; i < MT; ++i) { mma_bf16(S[i][n], qa[i], kb[0], kb[1]); mma_bf16(S[i][n + 1], qa[i], kb[2], kb[3]); }
                         }
@@ -236,7 +244,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
                         uint32_t qa[4], qh[MT][4], ql[MT][4];
 #pragma unroll
                         for (int i = 0; i < MT; ++i) {
-                            ldsm4(q_at + tile_at<RB>(i * 16 + (lane & 15), k * 2 + (lane >> 4)), qa);
+                            ldsm4((q_at + i * 16 * RB + q_off) ^ (k * 32), qa);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) two_terms(__uint_as_float(qa[e]), qh[i][e], ql[i][e]);
                         }
@@ -246,14 +254,14 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
 #pragma unroll
                         for (int n = 0; n < NT; n += 2) {
                             uint32_t kb[4];
-                            ldsm4(kt + tile_at<RB>(n * 8 + (lane & 7) + ((lane >> 4) << 3), k * 2 + ((lane >> 3) & 1)), kb);
+                            ldsm4((kt + n * 8 * RB + k_off) ^ (k * 32), kb);
 #pragma unroll
                             for (int e = 0; e < 4; ++e) two_terms(__uint_as_float(kb[e]), kh_[n + e / 2][e & 1], kl[n + e / 2][e & 1]);
                         }
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
-                            for (int i = 0; i < MT; ++i) { c[i][n][0] = c[i][n][1] = c[i][n][2] = c[i][n][3] = 0.f; mma_tf32(c[i][n], ql[i], kh_[n]); }
+                            for (int i = 0; i < MT; ++i) mma_tf32_first(c[i][n], ql[i], kh_[n]);
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -337,7 +345,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
 #pragma unroll
                         for (int n = 0; n < NV; n += 2) {
                             uint32_t vb[4];
-                            ldsm4t(vt + tile_at<RB>(k * 16 + (lane & 15), n + (lane >> 4)), vb);
+                            ldsm4t((vt + k * 16 * RB + v_off[0]) ^ (n * 16), vb);
 #pragma unroll
                             for (int i = 0; i < MT; ++i) { mma_bf16(O[i][n], pa[i], vb[0], vb[1]); mma_bf16(O[i][n + 1], pa[i], vb[2], vb[3]); }
                         }
@@ -360,11 +368,11 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
                             for (int n = 0; n < 4; ++n)
 #pragma unroll
                                 for (int e = 0; e < 2; ++e)
-                                    two_terms(lds32(vt + tile_at<RB>(k * 8 + 2 * t + e, (n0 + n) * 2 + (g >> 2)) + (g & 3) * 4), vh[n][e], vl[n][e]);
+                                    two_terms(lds32((vt + k * 8 * RB + v_off[e]) ^ ((n0 + n) * 32)), vh[n][e], vl[n][e]);
 #pragma unroll
                             for (int n = 0; n < 4; ++n)
 #pragma unroll
-                                for (int i = 0; i < MT; ++i) { c[i][n][0] = c[i][n][1] = c[i][n][2] = c[i][n][3] = 0.f; mma_tf32(c[i][n], pl[i], vh[n]); }
+                                for (int i = 0; i < MT; ++i) mma_tf32_first(c[i][n], pl[i], vh[n]);
 #pragma unroll
                             for (int n = 0; n < 4; ++n)
 #pragma unroll

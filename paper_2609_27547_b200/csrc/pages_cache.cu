@@ -15,9 +15,17 @@ constexpr int SLICE = 1024;                          // bytes of a token's row t
 __device__ __forceinline__ uint4 read16(const char *p) { return __ldcs(reinterpret_cast<const uint4 *>(p)); }
 __device__ __forceinline__ void write16(char *p, uint4 v) { *reinterpret_cast<uint4 *>(p) = v; }
 
+// An item's pieces: up to 32 rows of `per` pieces each, as (row, piece) without a division.
+struct Split {
+    unsigned per, inv;
+    __device__ __forceinline__ explicit Split(int n) : per(n), inv((1u << 18) / n + 1) {}
+    __device__ __forceinline__ int row(unsigned c) const { return (int)((c * inv) >> 18); }       // (exact for c < 2048, n <= 64)
+};
+constexpr int BATCH = 4;         // reads that a thread has in flight before it writes
+
 __global__ void append_kernel(const __grid_constant__ AppendArgs a, const __grid_constant__ AppendSeqs s, int slices)
 {
-    const int row_bytes = a.g.kvh * a.g.hd * a.g.es, head_bytes = a.g.hd * a.g.es;
+    const int row_bytes = a.g.kvh * a.g.hd * a.g.es, head_shift = 31 - __clz(a.g.hd * a.g.es), lane = threadIdx.x & 31;
     const long long items = (long long)s.items * 2 * slices;
     for (long long x = blockIdx.x; x < items; x += gridDim.x) {
         const int slice = (int)(x % slices), plane = (int)(x / slices) & 1, word = (int)(x / (2 * slices));
@@ -25,30 +33,37 @@ __global__ void append_kernel(const __grid_constant__ AppendArgs a, const __grid
         const int start = q.len - q.new_tokens, base = (start / WORD + word - q.item) * WORD;   // (the word's first token)
         const int t0 = max(start, base), t1 = min(q.len, base + WORD);
         const int page = a.p.table[q.tab * a.p.stride + (base >> a.g.t_shift)];
+        const long long row0 = (long long)q.row - start;                               // packed row of token t: row0 + t
+        const bool mine = base + lane >= t0 && base + lane < t1;
+        const unsigned m = __ballot_sync(0xffffffffu, mine), v = __ballot_sync(0xffffffffu, mine && (!a.mask || a.mask[row0 + base + lane]));
         if ((unsigned)page >= (unsigned)a.p.n_pages) continue;
         char *at = a.p.pool + (size_t)page * a.g.bytes;
-        const long long row0 = (long long)q.row - start;                            // packed row of token t: row0 + t
         const int slot0 = base & (a.g.T - 1);
-        if (plane == 0 && slice == 0 && threadIdx.x < 32) {
-            const int t = base + threadIdx.x;
-            const bool mine = t >= t0 && t < t1, see = mine && (!a.mask || a.mask[row0 + t]);
-            const unsigned m = __ballot_sync(0xffffffffu, mine), v = __ballot_sync(0xffffffffu, see);
-            if (threadIdx.x == 0) {
-                unsigned *w = reinterpret_cast<unsigned *>(at + a.g.mask) + slot0 / WORD;
-                *w = m == 0xffffffffu ? v : ((*w & ~m) | v);
-            }
+        if (plane == 0 && slice == 0 && threadIdx.x == 0) {
+            unsigned *w = reinterpret_cast<unsigned *>(at + a.g.mask) + slot0 / WORD;
+            *w = m == 0xffffffffu ? v : ((*w & ~m) | v);
         }
-        const int c0 = slice * SLICE, c1 = min(row_bytes, c0 + SLICE), per = (c1 - c0) / 16, n = (t1 - t0) * per;
-        const char *src = plane ? a.v : a.k;
+        const int c0 = slice * SLICE, c1 = min(row_bytes, c0 + SLICE);
+        const Split split((c1 - c0) / 16);
+        const unsigned n = (unsigned)(t1 - t0) * split.per;
         const long long stride = plane ? a.v_stride : a.k_stride;
-        char *dst = at + a.g.at(a.layer, plane, 0);
-#pragma unroll 4
-        for (int c = threadIdx.x; c < n; c += blockDim.x) {
-            const int r = c / per, col = c0 + (c - r * per) * 16, t = t0 + r;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (!a.mask || a.mask[row0 + t]) v = read16(src + (row0 + t) * stride + col);
-            const int h = col / head_bytes;
-            write16(dst + (size_t)h * a.g.head + (size_t)(slot0 + t - base) * head_bytes + (col - h * head_bytes), v);
+        const char *src = (plane ? a.v : a.k) + (row0 + t0) * stride + c0;
+        char *dst = at + a.g.at(a.layer, plane, 0) + ((size_t)(slot0 + t0 - base) << head_shift);
+        for (unsigned c = threadIdx.x; c < n; c += BATCH * blockDim.x) {
+            uint4 x4[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const unsigned k = c + i * blockDim.x;
+                x4[i] = make_uint4(0, 0, 0, 0);
+                const int r = split.row(k);
+                if (k < n && (v >> (r + t0 - base)) & 1) x4[i] = read16(src + r * stride + (k - r * split.per) * 16);
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const unsigned k = c + i * blockDim.x;
+                const int r = split.row(k), col = c0 + (int)(k - r * split.per) * 16, h = col >> head_shift;
+                if (k < n) write16(dst + (size_t)h * a.g.head + ((size_t)r << head_shift) + (col - (h << head_shift)), x4[i]);
+            }
         }
     }
 }
@@ -87,7 +102,7 @@ __global__ void copy_kernel(const __grid_constant__ Geometry g, const char *src,
 
 __global__ void gather_kernel(const __grid_constant__ Geometry g, const __grid_constant__ Pages p, long long row_stride, const __grid_constant__ GatherSeqs s, int slices)
 {
-    const int row_bytes = g.kvh * g.hd * g.es, head_bytes = g.hd * g.es, planes = g.layers * 2;
+    const int row_bytes = g.kvh * g.hd * g.es, head_shift = 31 - __clz(g.hd * g.es), planes = g.layers * 2;
     const long long items = (long long)s.items * planes * slices;
     for (long long x = blockIdx.x; x < items; x += gridDim.x) {
         const int slice = (int)(x % slices), plane = (int)(x / slices % planes), word = (int)(x / ((long long)slices * planes));
@@ -99,15 +114,26 @@ __global__ void gather_kernel(const __grid_constant__ Geometry g, const __grid_c
         const char *at = p.pool + (there ? (size_t)page * g.bytes : 0);
         const unsigned see = there ? reinterpret_cast<const unsigned *>(at + g.mask)[slot0 / WORD] : 0u;
         if (plane == 0 && slice == 0 && q.mask && threadIdx.x < t1 - base) q.mask[base + threadIdx.x] = (see >> threadIdx.x) & 1;
-        const int c0 = slice * SLICE, c1 = min(row_bytes, c0 + SLICE), per = (c1 - c0) / 16, n = (t1 - base) * per;
-        const char *src = at + (size_t)plane * g.kvh * g.head;
-        char *dst = (char *)q.planes + ((size_t)plane * q.plane_rows + base) * row_stride;
-#pragma unroll 4
-        for (int c = threadIdx.x; c < n; c += blockDim.x) {
-            const int r = c / per, col = c0 + (c - r * per) * 16, h = col / head_bytes;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if ((see >> r) & 1) v = read16(src + (size_t)h * g.head + (size_t)(slot0 + r) * head_bytes + (col - h * head_bytes));
-            write16(dst + (size_t)r * row_stride + col, v);
+        const int c0 = slice * SLICE, c1 = min(row_bytes, c0 + SLICE);
+        const Split split((c1 - c0) / 16);
+        const unsigned n = (unsigned)(t1 - base) * split.per;
+        const char *src = at + (size_t)plane * g.kvh * g.head + ((size_t)slot0 << head_shift);
+        char *dst = (char *)q.planes + ((size_t)plane * q.plane_rows + base) * row_stride + c0;
+        for (unsigned c = threadIdx.x; c < n; c += BATCH * blockDim.x) {
+            uint4 x4[BATCH];
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const unsigned k = c + i * blockDim.x;
+                x4[i] = make_uint4(0, 0, 0, 0);
+                const int r = split.row(k), col = c0 + (int)(k - r * split.per) * 16, h = col >> head_shift;
+                if (k < n && (see >> r) & 1) x4[i] = read16(src + (size_t)h * g.head + ((size_t)r << head_shift) + (col - (h << head_shift)));
+            }
+#pragma unroll
+            for (int i = 0; i < BATCH; ++i) {
+                const unsigned k = c + i * blockDim.x;
+                const int r = split.row(k);
+                if (k < n) write16(dst + (size_t)r * row_stride + (k - r * split.per) * 16, x4[i]);
+            }
         }
     }
 }

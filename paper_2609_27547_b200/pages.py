@@ -7,6 +7,7 @@ launched.  ``Book`` keeps, on the host, which page belongs to whom.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import math
@@ -16,7 +17,8 @@ import numpy as np
 import torch
 
 from .binding import OK, EbrlError, lib
-from .prefix8 import _DTYPES, _HERE, Planes, _addresses, _elsewhere, _host, _most, _on, _same_device, _stream
+from .prefix8 import _DTYPES, _HERE, Planes, _addresses, _elsewhere, _most, _on, _same_device, _stream
+from .prefix8 import _host as _host_any
 
 
 class _CLayout(C.Structure):
@@ -78,6 +80,20 @@ def _page(layout: Layout):
     return c, int(_load().ebrl_pages_page_bytes(at)), at
 
 
+def _host(v, what: str) -> torch.Tensor:
+    """Host integers as a contiguous CPU int32 tensor."""
+    if type(v) in (list, tuple, range) and len(v):      # (an array takes plain integers ten times as fast as a tensor does)
+        try:
+            return torch.frombuffer(array.array("i", v), dtype=torch.int32)
+        except (TypeError, OverflowError) as e:
+            raise ValueError("%s must be host integers of 32 bits (%s)" % (what, e)) from None
+    return _host_any(v, what)
+
+
+def _sum(v: torch.Tensor) -> int:
+    return sum(v.tolist()) if v.numel() <= 64 else int(v.numpy().sum(dtype=np.int64))
+
+
 def _check(st: int):
     if st != OK:
         raise EbrlError(st, (_load().ebrl_pages_last_error() or b"").decode())
@@ -107,9 +123,12 @@ def _table(table: torch.Tensor, n: int):
     return table.data_ptr(), (table.stride(0) if n > 1 else table.shape[1])
 
 
-def _fits(layout: Layout, table: torch.Tensor, lens: torch.Tensor):
-    if _most(lens) > table.shape[1] * layout.page_tokens:
+def _fits(layout: Layout, table: torch.Tensor, lens: torch.Tensor) -> int:
+    """The longest length."""
+    most = _most(lens)
+    if most > table.shape[1] * layout.page_tokens:
         raise ValueError("a length needs more pages than the table has")
+    return most
 
 
 def _packed(layout: Layout, x: torch.Tensor, heads: Optional[int], what: str):
@@ -147,7 +166,7 @@ def append(layout: Layout, pool: torch.Tensor, table: torch.Tensor, k: torch.Ten
     ``lens`` are the lengths with them.  ``mask``: uint8 or bool [sum(new)], 0 hides a token."""
     cl = _pool(layout, pool)
     N, L = _counts(new, lens)
-    n, total = N.numel(), int(N.sum())
+    n, total = N.numel(), _sum(N)
     _packed(layout, k, layout.n_kv_heads, "k")
     _packed(layout, v, layout.n_kv_heads, "v")
     if k.shape[0] < total or v.shape[0] < total:
@@ -159,7 +178,7 @@ def append(layout: Layout, pool: torch.Tensor, table: torch.Tensor, k: torch.Ten
     _same_device(pool, table, k, v, mask)
     with _on(pool.device):
         st = _stream(pool.device, stream, pool, table, k, v, mask)
-        if total:
+        if n:
             _check(_load().ebrl_pages_append(cl, pool.data_ptr(), pool.shape[0], n, at, stride, N.data_ptr(), L.data_ptr(), int(layer), k.data_ptr(), k.stride(0),
                                              v.data_ptr(), v.stride(0), None if mask is None else mask.data_ptr(), int(sm_quota), st))
 
@@ -171,7 +190,7 @@ def attend(layout: Layout, pool: torch.Tensor, table: torch.Tensor, q: torch.Ten
     [.., heads].  ``scale``: default 1 / sqrt(head_dim).  Rows behind the last query are left as they were (zeros where ``out`` is made here)."""
     cl = _pool(layout, pool)
     N, L = _counts(new, lens)
-    n, total = N.numel(), int(N.sum())
+    n, total = N.numel(), _sum(N)
     _packed(layout, q, None, "q")
     rows, heads, hd = q.shape
     if rows < total:
@@ -183,12 +202,12 @@ def attend(layout: Layout, pool: torch.Tensor, table: torch.Tensor, q: torch.Ten
     if lse is not None and (lse.dim() != 2 or lse.shape[0] < total or lse.shape[1] != heads or lse.dtype != torch.float32 or not lse.is_contiguous()):
         raise ValueError("lse must be contiguous fp32 [>= %d, %d]" % (total, heads))
     at, stride = _table(table, n)
-    _fits(layout, table, L)
+    most = _fits(layout, table, L)
     _same_device(pool, table, q, out, lse)
     dll = _load()
     with _on(pool.device):
         need = 0
-        if total and split_tokens >= 0:
+        if total and (split_tokens > 0 or (split_tokens == 0 and most >= 512)):   # (left to itself the library cuts no shorter sequence)
             need = dll.ebrl_pages_attend_workspace(cl, n, N.data_ptr(), L.data_ptr(), heads, 1 if causal else 0, int(window), int(split_tokens), int(sm_quota))
         # what is allocated here belongs to the stream that writes it; results are used on the current one, too
         with torch.cuda.stream(stream) if _elsewhere(pool.device, stream) else _HERE:
@@ -199,7 +218,7 @@ def attend(layout: Layout, pool: torch.Tensor, table: torch.Tensor, q: torch.Ten
                 lse = make((rows, heads), dtype=torch.float32)
             ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
         st = _stream(pool.device, stream, pool, table, q, out, lse)
-        if total and heads:
+        if n and heads:
             _check(dll.ebrl_pages_attend(cl, pool.data_ptr(), pool.shape[0], n, at, stride, N.data_ptr(), L.data_ptr(), int(layer), q.data_ptr(), q.stride(0), heads,
                                          out.data_ptr(), out.stride(0), lse.data_ptr(), 1.0 / math.sqrt(hd) if scale is None else float(scale),
                                          1 if causal else 0, int(window), int(split_tokens), ws.data_ptr() if need else None, need, int(sm_quota), st))
