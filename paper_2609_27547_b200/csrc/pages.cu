@@ -149,11 +149,11 @@ struct Group {
     int split = 0, team = 1;
 };
 
-// Rows from which the tensor-memory kernel takes a sequence.
-constexpr int CHUNK_FROM = 16;
+// A sequence of more rows is taken by the tensor-memory kernel.
+int chunk_from(int hd) { return hd == 128 ? 16 : 32; }
 
 struct Plan {
-    Group groups[3];                 // CHUNK_ROWS, 32 rows, 16 rows: in this order, so that short items fill up what long ones leave
+    Group groups[4];                 // CHUNK_ROWS, SMALL_CHUNK_ROWS, 32 rows, 16 rows: in this order, so that short items fill up what long ones leave
     std::vector<int64_t> row;        // first packed query of each sequence
     uint64_t pairs = 0;              // (query, piece) pairs of the sequences that are cut
 };
@@ -186,8 +186,8 @@ void cut(const ebrl_pages_layout_t &l, Group &g, const int32_t *m, const int32_t
 {
     if (asked < 0) return;
     if (asked > 0) { g.split = asked; return; }
-    const bool chunk = g.rows == CHUNK_ROWS;
-    const int warps = chunk ? 1 : attend_warps(l.head_dim, l.dtype == EBRL_F32, g.rows);   // items that an SM works on at a time
+    const bool chunk = g.rows >= SMALL_CHUNK_ROWS;
+    const int warps = chunk ? CHUNK_ROWS / g.rows : attend_warps(l.head_dim, l.dtype == EBRL_F32, g.rows);   // items that an SM works on at a time
     const int tile = chunk ? 4 : 1;                                                        // mask words of a tile
     const int at_once = quota ? std::min(sms, quota) : sms;
     auto slots = [&](int team) { return (double)at_once * (warps / team); };
@@ -230,8 +230,8 @@ void plan(Plan &p, const ebrl_pages_layout_t &l, int32_t n, const int32_t *m, co
         at += m[i];
         if (m[i] == 0) continue;
         const int64_t all = (int64_t)m[i] * G;
-        const int rows = chunks && all > CHUNK_FROM ? CHUNK_ROWS : attend_rows((int)std::min<int64_t>(all, 1 << 20));
-        Group &g = p.groups[rows == 16 ? 2 : (rows == 32 ? 1 : 0)];
+        const int rows = chunks && all > chunk_from(l.head_dim) ? (all > SMALL_CHUNK_ROWS ? CHUNK_ROWS : SMALL_CHUNK_ROWS) : attend_rows((int)std::min<int64_t>(all, 1 << 20));
+        Group &g = p.groups[rows == 16 ? 3 : (rows == 32 ? 2 : (rows == SMALL_CHUNK_ROWS ? 1 : 0))];
         g.rows = rows;
         g.seqs.push_back(i);
     }
@@ -415,7 +415,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
                     ++s.n;
                 }
                 s.items = (int)items;
-                st = launched(gr.rows == CHUNK_ROWS ? launch_chunk(a, s, sm_quota, beside, (cudaStream_t)stream)
+                st = launched(gr.rows >= SMALL_CHUNK_ROWS ? launch_chunk(a, s, gr.rows, sm_quota, beside, (cudaStream_t)stream)
                                                     : launch_attend(a, s, f32, gr.rows, sm_quota, beside, (cudaStream_t)stream));
                 beside = sm_quota == 0 && !any;
                 if (st != EBRL_OK) return st;

@@ -29,17 +29,21 @@ using namespace ptx;
 
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr int ROWS = 128, KEYS = 128, THREADS = 320;
+constexpr int ROWS = 128, KEYS = 128;
 constexpr unsigned long long LIMIT_NS = 4000000000ull;
 
-template <int HD> struct Shape {
+template <int HD, int TILES> struct Shape {
+    static constexpr int THREADS = (4 * TILES + 2) * 32;
+    static constexpr int PER_SM = 3 - TILES;                         // CTAs
     static constexpr int SWZ = HD >= 64 ? 128 : 64;                  // bytes of a swizzled row
     static constexpr int HALVES = HD * 2 / SWZ;                      // column blocks of a row
     static constexpr int HALF = 128 * SWZ;                           // bytes of 128 rows of one
     static constexpr int TILE = HALVES * HALF;
-    static constexpr int STAGES = HD == 128 ? 5 : 8;
-    static constexpr int BARS = 2 * STAGES + 8;
-    static constexpr int SMEM = (2 + STAGES) * TILE + 8 * BARS + 16 + 1024;
+    static constexpr int STAGES = TILES == 2 ? (HD == 128 ? 5 : 8) : (HD == 128 ? 2 : 4);
+    static constexpr int BARS = 2 * STAGES + 4 * TILES;
+    static constexpr int SMEM = (TILES + STAGES) * TILE + 8 * BARS + 16 + 1024;
+    static constexpr int O_COL = TILES * KEYS;                       // tensor memory: the scores of each tile, then their sums
+    static constexpr int COLS = TILES * 256;
 };
 
 __device__ int wait_status;       // EBRL_ERR_TIMEOUT once a wait ran out; one on each device
@@ -118,10 +122,10 @@ __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.
 template <int HD, bool VALUES> __device__ __forceinline__ uint64_t smem_desc(uint32_t addr)
 {
     uint64_t d = (uint64_t)((addr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(VALUES ? Shape<HD>::HALF >> 4 : 1) << 16;
-    d |= (uint64_t)(8 * Shape<HD>::SWZ >> 4) << 32;
+    d |= (uint64_t)(VALUES ? Shape<HD, 1>::HALF >> 4 : 1) << 16;
+    d |= (uint64_t)(8 * Shape<HD, 1>::SWZ >> 4) << 32;
     d |= (uint64_t)1 << 46;                                  // descriptor version of sm_100
-    d |= (uint64_t)(Shape<HD>::SWZ == 128 ? 2 : 4) << 61;    // 128- or 64-byte swizzle
+    d |= (uint64_t)(Shape<HD, 1>::SWZ == 128 ? 2 : 4) << 61;    // 128- or 64-byte swizzle
     return d;
 }
 // kind::f16: fp32 accumulate, bf16 A and B, M = 128; B along the contracted index, or (VALUES) along its columns.
@@ -133,19 +137,20 @@ __host__ __device__ constexpr uint32_t instr_desc(int N, bool values)
 // An item and the tokens lo .. hi (lo a multiple of 128) that some row of it sees.
 struct Item { int row, tab, part, m, len, R, r0, tiles, kh, piece, lo, hi, seen, n_kv; };   // (seen: no row sees a token below)
 
-__device__ __forceinline__ Item item_of(const AttendArgs &a, const AttendSeqs &sq, int x)
+template <int TILES> __device__ __forceinline__ Item item_of(const AttendArgs &a, const AttendSeqs &sq, int x)
 {
+    constexpr int ITEM = TILES * ROWS;
     Item it;
     const AttendSeq seq = sq.s[find_seq(sq.n, x, [&](int i) { return sq.s[i].item; })];
     it.m = seq.m; it.len = seq.len; it.row = seq.row; it.part = seq.part; it.tab = seq.tab;
     it.R = it.m * a.G;
-    const int RT = (it.R + 2 * ROWS - 1) / (2 * ROWS);
+    const int RT = (it.R + ITEM - 1) / ITEM;
     int rest = x - seq.item;
     const int kh = rest % a.g.kvh; rest /= a.g.kvh;
     const int rt = RT - 1 - rest % RT;                        // the last rows see most
     it.kh = kh; it.piece = rest / RT;
-    it.r0 = rt * 2 * ROWS;
-    const int r1 = min(it.R, it.r0 + 2 * ROWS), first = it.len - it.m;
+    it.r0 = rt * ITEM;
+    const int r1 = min(it.R, it.r0 + ITEM), first = it.len - it.m;
     it.tiles = r1 - it.r0 > ROWS ? 2 : 1;
     int lo = first_token(it.len, it.m, a.window), hi = it.len;
     if (a.split) { lo += it.piece * a.split; hi = min(hi, lo + a.split); }
@@ -198,36 +203,37 @@ struct Words {
     __device__ __forceinline__ unsigned word(int j, int i) const { return __shfl_sync(FULL, now, (j & 7) * 4 + i); }
 };
 
-template <int HD>
-__global__ void __launch_bounds__(THREADS, 1)
+template <int HD, int TILES>
+__global__ void __launch_bounds__(Shape<HD, TILES>::THREADS, Shape<HD, TILES>::PER_SM)
 chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ AttendArgs a, const __grid_constant__ AttendSeqs sq)
 {
-    using C = Shape<HD>;
-    constexpr uint32_t S_COL = 0, O_COL = 2 * KEYS;               // tensor memory: S of A, S of B, O of A, O of B
+    using C = Shape<HD, TILES>;
+    constexpr uint32_t S_COL = 0, O_COL = C::O_COL;
+    constexpr int COPY_WARP = 4 * TILES, MMA_WARP = COPY_WARP + 1;                     // the warps before take the softmax
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    const uint32_t q_at = smem_u32(smem), ring = q_at + 2 * C::TILE;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (2 + C::STAGES) * C::TILE);
+    const uint32_t q_at = smem_u32(smem), ring = q_at + TILES * C::TILE;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(smem + (TILES + C::STAGES) * C::TILE);
     const uint32_t bar0 = smem_u32(bars);
     auto full = [&](int s) { return bar0 + 8u * s; };
     auto empty = [&](int s) { return bar0 + 8u * (C::STAGES + s); };
     auto q_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + t); };
-    auto s_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 2 + t); };
-    auto p_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 4 + t); };
-    auto o_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 6 + t); };
+    auto s_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + TILES + t); };
+    auto p_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 2 * TILES + t); };
+    auto o_full = [&](int t) { return bar0 + 8u * (2 * C::STAGES + 3 * TILES + t); };
     volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(bars + C::BARS);
     volatile int *abort_flag = reinterpret_cast<volatile int *>(bars + C::BARS + 1);
 
     const int warp = __shfl_sync(FULL, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;   // (the same for all lanes, and known to be)
     if (threadIdx.x == 0) {
         for (int s = 0; s < C::STAGES; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (int t = 0; t < 2; ++t) { mbar_init(q_full(t), ROWS); mbar_init(s_full(t), 1); mbar_init(p_full(t), ROWS); mbar_init(o_full(t), 1); }
+        for (int t = 0; t < TILES; ++t) { mbar_init(q_full(t), ROWS); mbar_init(s_full(t), 1); mbar_init(p_full(t), ROWS); mbar_init(o_full(t), 1); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tm)) : "memory");
     }
-    if (warp == 9) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)), "r"(512u) : "memory");
+    if (warp == MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32((const void *)tmem_slot)), "r"((uint32_t)C::COLS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -237,14 +243,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     bool ok = true;
     pdl_launch_dependents();
 
-    if (warp == 8) {
+    if (warp == COPY_WARP) {
         // ---- copies: the warp looks pages up, one lane issues
         constexpr int MAX_BOX = KEYS;
         const int box = a.g.T < MAX_BOX ? a.g.T : MAX_BOX, boxes = KEYS / box;
         int stage = 0;
         uint32_t phase = 0;
         for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
-            const Item it = item_of(a, sq, x);
+            const Item it = item_of<TILES>(a, sq, x);
             const int *tab = a.p.table + it.tab * a.p.stride;
             const int first_page = it.lo >> a.g.t_shift, n_pages = it.hi > 0 ? (it.hi - 1) / a.g.T + 1 : 0;   // (of the sequence, those below n_pages hold tokens that are seen)
             auto fetch = [&](int p) {
@@ -276,7 +282,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 ok = __shfl_sync(FULL, ok ? 1 : 0, 0) != 0;
             }
         }
-    } else if (warp == 9) {
+    } else if (warp == MMA_WARP) {
         // ---- products
         constexpr uint32_t id_qk = instr_desc(KEYS, false), id_pv = instr_desc(HD, true);
         constexpr int PER = C::SWZ / 32;                            // k-steps in a column block
@@ -313,7 +319,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         };
         auto commit = [&](uint32_t bar) { if (elect()) tc_commit(bar); };
         for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
-            const Item it = item_of(a, sq, x);
+            const Item it = item_of<TILES>(a, sq, x);
             if (it.n_kv == 0) continue;
             Words words;
             words.start(a, a.p.table + it.tab * a.p.stride, it, lane);
@@ -337,7 +343,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         if (const int r = i * 32 + lane; !((words.word(j, i) >> lane) & 1))
 #pragma unroll
                             for (int c = 0; c < HD * 2 / 16; ++c)
-                                *reinterpret_cast<uint4 *>(smem + (2 + vs) * C::TILE + (c / (C::SWZ / 16)) * C::HALF + r * C::SWZ + c % (C::SWZ / 16) * 16) = make_uint4(0, 0, 0, 0);
+                                *reinterpret_cast<uint4 *>(smem + (TILES + vs) * C::TILE + (c / (C::SWZ / 16)) * C::HALF + r * C::SWZ + c % (C::SWZ / 16) * 16) = make_uint4(0, 0, 0, 0);
                     fence_proxy_async();
                     __syncwarp();
                 }
@@ -368,7 +374,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         const float sc = a.scale * LOG2E;
         uint32_t sph = 0, oph = 0;
         for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
-            const Item it = item_of(a, sq, x);
+            const Item it = item_of<TILES>(a, sq, x);
             if (t >= it.tiles) continue;
             const int r0 = it.r0 + t * ROWS, row = min(r0 + tid, it.R - 1), tok_q = row / a.G, head = it.kh * a.G + row - tok_q * a.G, first = it.len - it.m;
             float M = -INFINITY, L = 0.f;
@@ -556,9 +562,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         while (gtimer() - t0 < 200000ull) { }
     }
     __syncthreads();
-    if (warp == 9) {
+    if (warp == MMA_WARP) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)C::COLS) : "memory");
     }
     pdl_wait();      // (the end of this kernel is to be that of the ones beside it, too)
 }
@@ -584,20 +590,20 @@ template <int HD> bool make_map(CUtensorMap *out, const Geometry &g, const Pages
     if (!fn) return false;
     const cuuint64_t dims[3] = {HD, (cuuint64_t)g.layers * 2 * g.kvh * g.T, (cuuint64_t)p.n_pages};
     const cuuint64_t strides[2] = {HD * 2, g.bytes};
-    const cuuint32_t box[3] = {Shape<HD>::SWZ / 2, (cuuint32_t)(g.T < KEYS ? g.T : KEYS), 1};
+    const cuuint32_t box[3] = {Shape<HD, 1>::SWZ / 2, (cuuint32_t)(g.T < KEYS ? g.T : KEYS), 1};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, p.pool, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-              Shape<HD>::SWZ == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              Shape<HD, 1>::SWZ == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int HD> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
+template <int HD, int TILES> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
 {
     static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!set[dev]) {
-        const cudaError_t err = cudaFuncSetAttribute(chunk_kernel<HD>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<HD>::SMEM);
+        const cudaError_t err = cudaFuncSetAttribute(chunk_kernel<HD, TILES>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<HD, TILES>::SMEM);
         if (err != cudaSuccess) return err;
         set[dev] = true;
     }
@@ -605,7 +611,7 @@ template <int HD> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int q
     if (!make_map<HD>(&tm, a.g, a.p)) return cudaErrorInvalidValue;
     // one CTA per item, handed out by the hardware as the ones before end; under a quota persistent ones
     const Beside with(beside);
-    return launch_kernel(chunk_kernel<HD>, quota && s.items > quota ? quota : s.items, THREADS, Shape<HD>::SMEM, st, 1, tm, a, s);
+    return launch_kernel(chunk_kernel<HD, TILES>, quota && s.items > quota ? quota : s.items, Shape<HD, TILES>::THREADS, Shape<HD, TILES>::SMEM, st, 1, tm, a, s);
 }
 
 }  // namespace
@@ -615,10 +621,15 @@ bool chunk_supported(const Geometry &g, int n_pages, float scale)
     return g.es == 2 && scale > 0.f && (long long)g.layers * 2 * g.kvh * g.T <= INT32_MAX && n_pages < INT32_MAX;
 }
 
-cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
+template <int TILES> static cudaError_t pick(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
+{
+    return a.g.hd == 128 ? go<128, TILES>(a, s, quota, beside, st) : (a.g.hd == 64 ? go<64, TILES>(a, s, quota, beside, st) : go<32, TILES>(a, s, quota, beside, st));
+}
+
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, bool beside, cudaStream_t st)
 {
     if (s.items == 0) return cudaSuccess;
-    return a.g.hd == 128 ? go<128>(a, s, quota, beside, st) : (a.g.hd == 64 ? go<64>(a, s, quota, beside, st) : go<32>(a, s, quota, beside, st));
+    return rows == CHUNK_ROWS ? pick<2>(a, s, quota, beside, st) : pick<1>(a, s, quota, beside, st);
 }
 
 cudaError_t take_status(int *status)

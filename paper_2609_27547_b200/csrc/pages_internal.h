@@ -111,10 +111,10 @@ int attend_warps(int hd, bool f32, int rows);          // warps that an SM holds
 cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, int rows, int quota, bool beside, cudaStream_t st);
 cudaError_t launch_attend_join(const AttendArgs &a, const AttendSeqs &s, bool f32, int quota, int sms, cudaStream_t st);
 
-// The same for many query rows, bf16 (pages_chunk.cu): 256 of them an item, one CTA each.
-constexpr int CHUNK_ROWS = 256;
+// The same for many query rows, bf16 (pages_chunk.cu): an item is a CTA of 256 of them, or one of 128, of which an SM holds two.
+constexpr int CHUNK_ROWS = 256, SMALL_CHUNK_ROWS = 128;
 bool chunk_supported(const Geometry &g, int n_pages, float scale);
-cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st);
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, bool beside, cudaStream_t st);
 
 // Whether a bounded wait ran out on the current device since the last call (waits for the device).
 cudaError_t take_status(int *status);
