@@ -149,8 +149,14 @@ struct Group {
     int split = 0, team = 1;
 };
 
-// A sequence of more rows is taken by the tensor-memory kernel.
+// A sequence of more rows is taken by the tensor-memory kernel.  Measured, us, one warp per item / that kernel, 64 x 2000 tokens x 4 heads: heads of 128, 16 rows
+// 55 / -, 32 rows 83 / 53, 64 rows 159 / 54; of 64, 32 rows 41 / 43, 64 rows 115 / 43; of 32, 64 rows 65 / 61 (two tiles per CTA then).
 int chunk_from(int hd) { return hd == 128 ? 16 : 32; }
+
+// Its rows per item.  Two tiles that share what is loaded pay where the products take the time, and are never much worse there: heads of 128, 4 x 2000 new
+// tokens over 8 - 16 k x 16 heads 751 us against 779 in CTAs of one tile, 64 x 100 over 600 88 against 86.  Heads of 64 and 32 wait for the exponentials either way:
+// 4 x 2048 over 8 k 432 against 412, 64 x 100 over 600 75 against 70.
+int chunk_rows(int hd, int64_t rows) { return hd == 128 && rows > SMALL_CHUNK_ROWS ? CHUNK_ROWS : SMALL_CHUNK_ROWS; }
 
 struct Plan {
     Group groups[4];                 // CHUNK_ROWS, SMALL_CHUNK_ROWS, 32 rows, 16 rows: in this order, so that short items fill up what long ones leave
@@ -230,7 +236,7 @@ void plan(Plan &p, const ebrl_pages_layout_t &l, int32_t n, const int32_t *m, co
         at += m[i];
         if (m[i] == 0) continue;
         const int64_t all = (int64_t)m[i] * G;
-        const int rows = chunks && all > chunk_from(l.head_dim) ? (all > SMALL_CHUNK_ROWS ? CHUNK_ROWS : SMALL_CHUNK_ROWS) : attend_rows((int)std::min<int64_t>(all, 1 << 20));
+        const int rows = chunks && all > chunk_from(l.head_dim) ? chunk_rows(l.head_dim, all) : attend_rows((int)std::min<int64_t>(all, 1 << 20));
         Group &g = p.groups[rows == 16 ? 3 : (rows == 32 ? 2 : (rows == SMALL_CHUNK_ROWS ? 1 : 0))];
         g.rows = rows;
         g.seqs.push_back(i);

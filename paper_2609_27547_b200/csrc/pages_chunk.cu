@@ -1,17 +1,26 @@
 // Softmax attention of many query rows over paged keys and values (include/ebrl_pages.h), bf16, on tcgen05: out = softmax(scale q k^T) v.
 //
-//   Item = (sequence, piece of it, key/value head, 256 query rows), one CTA: two tiles of 128 rows that share every key and value tile (128
-//   tokens), so that the tensor core works on one while the other's softmax is taken.
-//     warps 0 - 3, 4 - 7   the softmax of tile A, of tile B: one thread per row, so that statistics need no shuffles.  Scores come
-//                          from tensor memory, weights go back to it in place (they are the A operand of the second product)
-//     warp 8               copies: TMA boxes of up to 128 tokens of a page, keys and values in turn through one ring
-//     warp 9               products: S = Q K^T of a tile is issued behind the O += P V that last read its weights, and S of one tile and O of the other
-//                          are always queued, in the order  PV_A(j) QK_A(j + 1) PV_B(j) QK_B(j + 1)
-//   A row's reference is raised only when a score exceeds it by 2^8 (weights up to 2^8 keep bf16's 8 bits): sums in tensor memory are
-//   rescaled by the softmax threads themselves, which know from S(j) being there that PV(j - 1) is done.
-//   Tokens that no row may see are masked in S; their value rows are set to zero in shared memory before the product, so that
-//   what stands there (NaN in a row nobody wrote) does not meet a weight of zero.
+//   Item = (sequence, piece of it, key/value head, 128 or 256 query rows), one CTA; rows are (token, member) pairs of the heads that share a key/value head.
+//   Keys and values come in tiles of 128 tokens.  A CTA has one tile of 128 rows, and an SM two such CTAs, or two tiles that share every key and value; either
+//   way the tensor core works on one tile while the other's softmax is taken.
+//     softmax    four warps for each tile: one thread per row, so that statistics need no shuffles.  Scores come from tensor memory, weights go
+//                back to it in place (they are the A operand of the second product; values are its B operand as they lie, tokens along the contraction)
+//     copies     one warp: TMA boxes of up to 128 tokens of a page, keys and values in turn through one ring; pages that are not there lie outside the
+//                tensor map, which reads zeros
+//     products   one warp: S = Q K^T of a tile is issued behind the O += P V that reads its last weights, so that with two tiles the order is
+//                PV_A(j) QK_A(j + 1) PV_B(j) QK_B(j + 1)
+//   Weights are first taken against the reference as it stands, and a tile's maximum is looked for only where their sum exceeds 2^16 (or there is no reference
+//   yet): bf16 keeps its 8 bits whatever their size.  Sums in tensor memory are then rescaled by the softmax threads themselves, which know from
+//   S(j) being there that PV(j - 1) is done.
+//   Tokens that no row may see are masked in S; their value rows are set to zero in shared memory before the product, so that what stands there (NaN in a
+//   row nobody wrote) does not meet a weight of zero.
 //   All waits are bounded: when one runs out the CTA notes it, lets its copies land, frees tensor memory and returns.
+//
+//   What bounds it: 4 x 2000 - 2048 new tokens over 8 - 16 k x 16 heads of 128 take 750 us, 1.1 PFLOP/s.  The products alone (softmax skipped) take 630: a
+//   128 x 128 x 128 product from shared memory reads 128 bytes a cycle, all there are, and the copies want a quarter of that, too.  The rest is
+//   the softmax: its 128 exponentials a row keep the unit busy for 2064 of the 3500 cycles that two tiles take.
+//   Tried and not kept (same case): weights handed over in halves of 64 tokens 757, products of 64 tokens with their own barriers 884, two threads per row
+//   765, the scores read twice in short loops 830, a quarter / half of the exponentials by polynomial 870 / 980, registers split 208 / 88 795.
 #include "pages_internal.h"
 #include "f32x2.cuh"
 #include "ptx_helpers.cuh"
@@ -39,7 +48,7 @@ template <int HD, int TILES> struct Shape {
     static constexpr int HALVES = HD * 2 / SWZ;                      // column blocks of a row
     static constexpr int HALF = 128 * SWZ;                           // bytes of 128 rows of one
     static constexpr int TILE = HALVES * HALF;
-    static constexpr int STAGES = TILES == 2 ? (HD == 128 ? 5 : 8) : (HD == 128 ? 2 : 4);
+    static constexpr int STAGES = TILES == 2 ? 5 : (HD == 128 ? 2 : 4);
     static constexpr int BARS = 2 * STAGES + 4 * TILES;
     static constexpr int SMEM = (TILES + STAGES) * TILE + 8 * BARS + 16 + 1024;
     static constexpr int O_COL = TILES * KEYS;                       // tensor memory: the scores of each tile, then their sums
@@ -431,7 +440,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     sph ^= 1u;
                     if (!ok) break;
                     tc_fence_after();
-                    // First with the reference as it is: weights may grow to 2^30 in sum before anything needs to be done about it, so that the
+                    // First with the reference as it is: weights may grow to 2^16 in sum before anything needs to be done about it, so that the
                     // maximum of a tile is rarely asked for.
                     uint32_t P[64];
                     {
@@ -460,7 +469,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         weights(B, P + 48, ref2);
                     }
                     float sum = total();
-                    const bool redo = !(sum <= 1073741824.f) || M == -INFINITY;      // (a NaN, too)
+                    const bool redo = !(sum <= 65536.f) || M == -INFINITY;      // (a NaN, too)
                     if (!__any_sync(FULL, redo)) {
                         tmem_st32(s_at, P);
                         tmem_st32(s_at + 32, P + 32);
@@ -621,15 +630,11 @@ bool chunk_supported(const Geometry &g, int n_pages, float scale)
     return g.es == 2 && scale > 0.f && (long long)g.layers * 2 * g.kvh * g.T <= INT32_MAX && n_pages < INT32_MAX;
 }
 
-template <int TILES> static cudaError_t pick(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
-{
-    return a.g.hd == 128 ? go<128, TILES>(a, s, quota, beside, st) : (a.g.hd == 64 ? go<64, TILES>(a, s, quota, beside, st) : go<32, TILES>(a, s, quota, beside, st));
-}
-
 cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, bool beside, cudaStream_t st)
 {
     if (s.items == 0) return cudaSuccess;
-    return rows == CHUNK_ROWS ? pick<2>(a, s, quota, beside, st) : pick<1>(a, s, quota, beside, st);
+    if (a.g.hd == 128) return rows == CHUNK_ROWS ? go<128, 2>(a, s, quota, beside, st) : go<128, 1>(a, s, quota, beside, st);
+    return a.g.hd == 64 ? go<64, 1>(a, s, quota, beside, st) : go<32, 1>(a, s, quota, beside, st);
 }
 
 cudaError_t take_status(int *status)

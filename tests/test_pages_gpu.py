@@ -380,3 +380,244 @@ def test_gather_more_sequences_than_one_launch_takes():
     pg.gather(lay, cache.pool, cache.table, lens, planes)
     for i in (0, 700, 1023, 1024, 1499):
         assert torch.equal(planes[i, 0, :, :lens[i]].cpu(), cache.kv[i][0, :, 0].float()) and (planes[i, 0, :, lens[i]:] == 0).all()
+
+
+# ---- together, and as a program uses them --------------------------------------------------------------------------------
+
+def dense(q, k, v, scale, causal):
+    """One sequence in 64 bits: q [m, heads, hd] against k, v [heads, n, hd], the queries being the last m tokens."""
+    m, n = q.shape[0], k.shape[1]
+    G = q.shape[1] // k.shape[0]
+    s = scale * (q.double().transpose(0, 1) @ k.double().repeat_interleave(G, 0).transpose(1, 2))
+    if causal:
+        s = s.masked_fill(torch.arange(n, device=s.device) > torch.arange(n - m, n, device=s.device)[:, None], -math.inf)
+    return (torch.softmax(s, -1) @ v.double().repeat_interleave(G, 0)).transpose(0, 1)
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_histories_grow_fork_are_compacted_and_reach_the_action_head(dtype):
+    """Two episodes start, grow, branch into children that go on by themselves, one is reset, the pool is compacted; every chunk's attention is what the
+    dense history gives.  The histories, gathered, are planes that a handle takes: its chunks are those of the dense planes bit for bit."""
+    from paper_2609_27547_b200 import synth
+    w = synth.scaled(synth.WORKLOADS[0], B=4, dtype="bf16" if dtype is BF else "f32", d=256, P=(16, 200))
+    heads, hd, T, layers = w.n_heads, w.d // w.n_heads, 32, 2
+    lay = pg.Layout(layers, heads, hd, T, dtype)
+    book, pool = pg.Book(60, T, 6), pg.new_pool(lay, 60)
+    pool[:, :] = 0x7f                          # whatever a pool holds at first
+    g = torch.Generator().manual_seed(1)
+    hist = {s: torch.zeros((layers, 2, heads, 0, hd), dtype=dtype, device="cuda") for s in range(6)}
+
+    def step(seqs, new):
+        lens = [book.len(s) + k for s, k in zip(seqs, new)]
+        pg.copy(lay, pool, pool, book.extend(seqs, lens))
+        table = book.table(seqs, device="cuda")
+        total = sum(new)
+        for l in range(layers):
+            qkv = torch.randn((total, 3 * heads, hd), generator=g).to(dtype).cuda()
+            q, k, v = qkv[:, :heads], qkv[:, heads:2 * heads], qkv[:, 2 * heads:]
+            pg.append(lay, pool, table, k, v, new, lens, layer=l)
+            at = 0
+            for s, n in zip(seqs, new):
+                if l == 0:
+                    hist[s] = torch.cat([hist[s], torch.zeros((layers, 2, heads, n, hd), dtype=dtype, device="cuda")], 3)
+                hist[s][l, 0, :, hist[s].shape[3] - n:] = k[at:at + n].transpose(0, 1)
+                hist[s][l, 1, :, hist[s].shape[3] - n:] = v[at:at + n].transpose(0, 1)
+                at += n
+            out, _ = pg.attend(lay, pool, table, q, new, lens, layer=l)
+            at = 0
+            for s, n in zip(seqs, new):
+                want = dense(q[at:at + n], hist[s][l, 0], hist[s][l, 1], 1 / math.sqrt(hd), True)
+                off = (out[at:at + n].double() - want).abs().max()
+                # |values| <= 5 and scores' absolute sums <= 8: twice 5 * 2^-8 and twice 5 E, E = 4 * 64 * 2^-23 * 8
+                assert float(off) <= (10 * 2.0 ** -8 if dtype is BF else 0.0) + 10 * 2.0 ** -12, (s, l, float(off))
+                at += n
+
+    step([0, 1], [50, 20])
+    step([0, 1], [1, 13])
+    book.fork([0, 0, 1], [2, 3, 4])
+    for a, b in ((0, 2), (0, 3), (1, 4)):
+        hist[b] = hist[a].clone()
+    step([0, 2, 3, 4], [1, 40, 1, 2])           # the parent goes on, too
+    book.shorten([0], 0)
+    hist[0] = hist[0][:, :, :, :0]
+    pg.copy(lay, pool, pool, book.compact())
+    step([1, 2, 3, 4], [5, 1, 64, 1])
+    step([0, 3], [3, 1])
+    seqs = [1, 2, 3, 4]
+    lens = [book.len(s) for s in seqs]
+    planes = pg.gather(lay, pool, book.table(seqs, device="cuda"), lens)
+    for s, x in zip(seqs, planes):
+        assert torch.equal(x, hist[s].permute(0, 1, 3, 2, 4).flatten(3))
+    pg.check()
+    cfg = dict(max_group_envs=4)
+    outs = []
+    for kv in (planes, [hist[s].permute(0, 1, 3, 2, 4).flatten(3).contiguous() for s in seqs]):
+        gen = B.ActGen(B.cfg_for(w, **cfg), synth.make_weights(w))
+        noise = torch.stack([synth.make_env(w, e).noise for e in range(4)]).cuda()
+        out = torch.empty_like(noise)
+        gen.submit([0, 1, 2, 3], [x[:1].contiguous() for x in kv], noise, out)
+        gen.sync()
+        gen.destroy()
+        outs.append(out)
+    assert torch.equal(*outs) and bool(torch.isfinite(outs[0]).all())
+
+
+def test_gathered_histories_with_hidden_tokens_become_records():
+    lay = pg.Layout(1, 4, 64, 32, BF)
+    lens = [100, 33, 64]
+    cache = Cache(lay, lens, hide=0.3, seed=3)
+    seen = torch.zeros((3, 100), dtype=torch.uint8, device="cuda")
+    planes = pg.gather(lay, cache.pool, cache.table, lens, torch.zeros((3, 1, 2, 100, 256), dtype=BF, device="cuda"), mask=seen)
+    rec = p8.Layout(1, 4, 64, 100)
+    a, b = p8.new_pool(rec, 3), p8.new_pool(rec, 3)
+    p8.quantize(rec, a, planes, lens, mask=seen)
+    p8.quantize(rec, b, [x.permute(0, 1, 3, 2, 4).flatten(3).to(BF).cuda() for x in cache.kv], lens, mask=[s.to(torch.uint8).cuda() for s in cache.see])
+    assert torch.equal(a, b)
+
+
+def test_captured_and_replayed_on_other_pages_and_data():
+    """One graph: append, attend of a mixed batch (several kernels side by side, and pieces), gather.  The replay reads tables, pools and inputs as they are then."""
+    lay = pg.Layout(1, 4, 64, 32, BF)
+    lens, new = [3000, 500, 40, 900], [1, 200, 40, 20]
+    total = sum(new)
+    states = []
+    for seed in (1, 2):
+        c = Cache(lay, lens, seed=seed)
+        g = torch.Generator().manual_seed(seed)
+        states.append((c, torch.randn((total, 12, 64), generator=g).to(BF).cuda()))
+    pool, table, qkv = states[0][0].pool.clone(), states[0][0].table.clone(), states[0][1].clone()
+    planes = [torch.zeros((1, 2, n, 256), dtype=BF, device="cuda") for n in lens]
+
+    def run():
+        pg.append(lay, pool, table, qkv[:, 4:8], qkv[:, 8:], new, lens)
+        out, lse = pg.attend(lay, pool, table, qkv[:, :4], new, lens)
+        pg.gather(lay, pool, table, lens, planes)
+        return out, lse
+    run()                                       # (kernel attributes are set at the first call)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = run()
+    for c, x in states[::-1] + states:
+        pool.copy_(c.pool)
+        table.copy_(c.table)
+        qkv.copy_(x)
+        graph.replay()
+        got = [t.clone() for t in (out, lse, *planes)]
+        torch.cuda.synchronize()
+        pool.copy_(c.pool)
+        eager = run()
+        assert torch.equal(got[0], eager[0]) and torch.equal(got[1], eager[1]) and all(torch.equal(a, b) for a, b in zip(got[2:], planes))
+    del graph
+
+
+def test_two_streams_and_a_stream_that_is_not_current():
+    lay = pg.Layout(1, 4, 128, 64, BF)
+    lens, new = [2500, 700, 300], [1, 100, 30]
+    cache = Cache(lay, lens, seed=5)
+    q = queries(lay, sum(new), 2)
+    want, want_l = pg.attend(lay, cache.pool, cache.table, q, new, lens)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    results = []
+    for _ in range(10):
+        for s in streams:
+            results.append(pg.attend(lay, cache.pool, cache.table, q, new, lens, stream=s))
+    torch.cuda.synchronize()
+    for out, lse in results:
+        assert torch.equal(out, want) and torch.equal(lse, want_l)
+    pg.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_pages_behind_four_gigabytes(dtype):
+    lay = pg.Layout(1, 16, 128, 256, dtype)
+    n_pages = int(4.6e9 / lay.page_bytes) + 2
+    pool = torch.zeros((n_pages, lay.page_bytes), dtype=torch.uint8, device="cuda")
+    small = Cache(lay, [300, 520], seed=2, spare=0)
+    high = [n_pages - 1 - p for p in range(small.n_pages)]
+    pool[high] = small.pool
+    table = torch.where(small.table >= 0, n_pages - 1 - small.table, small.table)
+    for new in ([1, 1], [200, 3]):
+        q = queries(lay, sum(new), 1)
+        out, lse = pg.attend(lay, pool, table, q, new, [300, 520])
+        want = pg.attend(lay, small.pool, small.table, q, new, [300, 520])
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+    x = torch.randn((20, 16, 128), generator=torch.Generator().manual_seed(0)).to(dtype).cuda()
+    pg.append(lay, pool, table, x, -x, [0, 20], [300, 520])
+    pg.append(lay, small.pool, small.table, x, -x, [0, 20], [300, 520])
+    assert torch.equal(pool[high], small.pool)
+    pg.copy(lay, pool, pool, ([high[0]], [0]))
+    e, _ = pg.views(lay, pool[[high[0], 0]])
+    assert torch.equal(e[0].contiguous().view(torch.uint8), e[1].contiguous().view(torch.uint8))
+    for a, b in zip(pg.gather(lay, pool, table, [300, 520]), pg.gather(lay, small.pool, small.table, [300, 520])):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_attend_random_calls(seed):
+    import random
+    rng = random.Random(seed)
+    dtype = rng.choice([BF, BF, F])
+    lay = pg.Layout(rng.randint(1, 2), rng.choice([1, 2, 3]), rng.choice([32, 64, 128]), rng.choice([32, 64, 128, 256]), dtype)
+    n, G = rng.randint(1, 9), rng.choice([1, 2, 3, 6, 16])
+    lens = [rng.choice([rng.randint(0, 40), rng.randint(0, 700), rng.randint(0, 3000)]) for _ in range(n)]
+    new = [rng.choice([0, 1, rng.randint(1, 20), rng.randint(1, 300)]) for _ in range(n)]
+    causal = rng.random() < 0.7
+    window = rng.choice([0, 0, rng.randint(1, 400)]) if causal else 0
+    cache = Cache(lay, lens, hide=rng.choice([0.0, 0.2]), lost=rng.choice([0.0, 0.1]), seed=seed)
+    q = queries(lay, sum(new), G, seed=seed)
+    layer = lay.kv_layers - 1
+    for quota in (0, rng.randint(1, 100)):
+        for split in (0, -1, 128 * rng.randint(1, 8)):
+            out, lse = pg.attend(lay, cache.pool, cache.table, q, new, lens, layer=layer, causal=causal, window=window, split_tokens=split, sm_quota=quota)
+            check(cache, layer, q, new, out, lse, causal=causal, window=window)
+
+
+def test_scores_that_rise_along_a_sequence():
+    """Each tile's scores lie far above those of the ones before it, so that references have to follow; and far below, so that later tiles count for nothing."""
+    lay = pg.Layout(1, 1, 64, 64, BF)
+    cache = Cache(lay, [1500], seed=6)
+    elems, _ = pg.views(lay, cache.pool)
+    ramp = torch.linspace(-60, 60, 1500)
+    for rise in (1, -1):
+        for t in range(1500):
+            k = torch.zeros(64)
+            k[0] = rise * ramp[t]
+            k[1:] = cache.kv[0][0, 0, 0, t, 1:].float() * 0.1
+            cache.kv[0][0, 0, 0, t] = k.to(BF).double()
+        x = cache.kv[0][0, 0, 0].to(BF).cuda()
+        for j, p in enumerate(cache.rows[0]):
+            k = min(64, 1500 - 64 * j)
+            elems[p, 0, 0, 0, :k] = x[64 * j:64 * j + k]
+        for m in (1, 33, 300):
+            q = queries(lay, m, 1)
+            q[:, 0, 0] = 4.0
+            for split in (0, 128):
+                out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [1500], split_tokens=split, scale=1.0)
+                check(cache, 0, q, [m], out, lse, scale=1.0)
+
+
+def test_refusals_on_the_device():
+    lay = pg.Layout(1, 2, 64, 32, BF)
+    cache = Cache(lay, [40], seed=1)
+    q = queries(lay, 3, 2)
+    k = q[:, :2].contiguous()
+    bad_values = (lambda: pg.attend(lay, cache.pool, cache.table, q, [4], [40]), lambda: pg.attend(lay, cache.pool, cache.table, q, [1], [129]),
+                  lambda: pg.attend(lay, cache.pool, cache.table.cpu(), q, [1], [40]), lambda: pg.attend(lay, cache.pool, cache.table, q, [1], [40], lse=q),
+                  lambda: pg.attend(lay, cache.pool, cache.table, q, [1], [40], out=q[:, :2]), lambda: pg.append(lay, cache.pool, cache.table, k, k[:1], [2], [40]),
+                  lambda: pg.append(lay, cache.pool, cache.table, q, q, [2], [40]), lambda: pg.append(lay, cache.pool, cache.table, k, k, [2], [40], mask=torch.ones(1, device="cuda")),
+                  lambda: pg.copy(lay, cache.pool, cache.pool, ([0], [1, 2])), lambda: pg.copy(lay, cache.pool, cache.pool.cpu(), ([0], [1])),
+                  lambda: pg.gather(lay, cache.pool, cache.table, [40], torch.zeros((1, 1, 2, 39, 128), dtype=BF, device="cuda")),
+                  lambda: pg.gather(lay, cache.pool, cache.table, [-1]), lambda: pg.gather(lay, cache.pool, cache.table, [40], [torch.zeros((1, 2, 40, 100), dtype=BF, device="cuda")]))
+    for fn in bad_values:
+        with pytest.raises(ValueError):
+            fn()
+    for fn in (lambda: pg.attend(lay, cache.pool, cache.table, q, [1], [40], window=3, causal=False), lambda: pg.attend(lay, cache.pool, cache.table, q, [1], [40], scale=math.inf),
+               lambda: pg.attend(lay, cache.pool, cache.table, q, [1], [40], layer=1), lambda: pg.attend(lay, cache.pool, cache.table, q, [-1], [40]),
+               lambda: pg.append(lay, cache.pool, cache.table, k, k, [3], [2]), lambda: pg.copy(lay, cache.pool, cache.pool, ([0], [0])),
+               lambda: pg.copy(lay, cache.pool, cache.pool, ([0], [1], [33]))):
+        with pytest.raises(B.EbrlError):
+            fn()
+    with pytest.raises(TypeError):
+        pg.attend(lay, cache.pool, cache.table, q.float(), [1], [40])
