@@ -51,6 +51,10 @@ const char *ebrl_pages_last_error(void);
  * forgets it. */
 ebrl_status_t ebrl_pages_check(void);
 
+/* Tests of that path only: with limit_ns > 0 (2 s at most) this thread's later attend calls issue no copies in the kernels that wait for them, so that the
+ * waits run out after limit_ns and the kernels return; 0 ends it. */
+void ebrl_pages_test_drop_copies(uint64_t limit_ns);
+
 /* Writes the keys and values of new tokens of one layer.
  *   new_tokens  host [n], 0 .. len[i]: sequence i's new tokens are its last ones, positions len[i] - new_tokens[i] .. len[i] - 1
  *   len         host [n]: its length with them, at most table_stride * page_tokens

@@ -139,6 +139,7 @@ thread_local AppendSeqs t_append;
 thread_local GatherSeqs t_gather;
 thread_local AttendSeqs t_attend;
 thread_local CopyPages t_copy;
+thread_local uint64_t t_drop_limit = 0;     // tests of the give-up path
 
 // ---- attend: kernels, pieces ----
 
@@ -193,7 +194,7 @@ void cut(const ebrl_pages_layout_t &l, Group &g, const int32_t *m, const int32_t
     if (asked < 0) return;
     if (asked > 0) { g.split = asked; return; }
     const bool chunk = g.rows >= SMALL_CHUNK_ROWS;
-    const int warps = chunk ? CHUNK_ROWS / g.rows : attend_warps(l.head_dim, l.dtype == EBRL_F32, g.rows);   // items that an SM works on at a time
+    const int warps = chunk ? (quota ? 1 : CHUNK_ROWS / g.rows) : attend_warps(l.head_dim, l.dtype == EBRL_F32, g.rows);   // items that an SM works on at a time
     const int tile = chunk ? 4 : 1;                                                        // mask words of a tile
     const int at_once = quota ? std::min(sms, quota) : sms;
     auto slots = [&](int team) { return (double)at_once * (warps / team); };
@@ -293,6 +294,8 @@ ebrl_status_t ebrl_pages_check(void)
     if (e != cudaSuccess) { cudaGetLastError(); return fail(EBRL_ERR_CUDA, "%s", cudaGetErrorString(e)); }
     return status ? fail(EBRL_ERR_TIMEOUT, "a kernel's wait for its own copies ran out") : EBRL_OK;
 }
+
+void ebrl_pages_test_drop_copies(uint64_t limit_ns) { t_drop_limit = std::min<uint64_t>(limit_ns, 2000000000ull); }
 
 ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, int32_t n_pages, int32_t n, const int32_t *table, int64_t table_stride,
                                 const int32_t *new_tokens, const int32_t *len, int32_t layer, const void *k, int64_t k_stride, const void *v,
@@ -398,6 +401,8 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
         a.layer = layer; a.heads = n_heads; a.G = n_heads / g.kvh;
         a.q = (const char *)q; a.out = (char *)out; a.q_stride = q_stride; a.o_stride = o_stride;
         a.lse = lse; a.scale = scale; a.causal = causal != 0; a.window = window;
+        a.limit_ns = t_drop_limit ? t_drop_limit : 4000000000ull;
+        a.test_drop_copies = t_drop_limit != 0;
         a.part_o = (float *)workspace;
         a.part_ml = (float *)workspace + p.pairs * n_heads * g.hd;
         const bool f32 = layout->dtype == EBRL_F32;

@@ -39,7 +39,6 @@ using namespace ptx;
 constexpr unsigned FULL = 0xffffffffu;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int ROWS = 128, KEYS = 128;
-constexpr unsigned long long LIMIT_NS = 4000000000ull;
 
 template <int HD, int TILES> struct Shape {
     static constexpr int THREADS = (4 * TILES + 2) * 32;
@@ -258,7 +257,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         const int box = a.g.T < MAX_BOX ? a.g.T : MAX_BOX, boxes = KEYS / box;
         int stage = 0;
         uint32_t phase = 0;
-        for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
+        for (int x = blockIdx.x; x < sq.items && ok && !a.test_drop_copies; x += gridDim.x) {
             const Item it = item_of<TILES>(a, sq, x);
             const int *tab = a.p.table + it.tab * a.p.stride;
             const int first_page = it.lo >> a.g.t_shift, n_pages = it.hi > 0 ? (it.hi - 1) / a.g.T + 1 : 0;   // (of the sequence, those below n_pages hold tokens that are seen)
@@ -276,7 +275,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 for (int b = 0; b < 4; ++b) page[b] = __shfl_sync(FULL, now, ((tok + b * box) >> a.g.t_shift) - base);   // (pages of a tile are in one batch: 32 is a multiple of 4)
                 if (lane == 0) {
                     for (int kv = 0; kv < 2 && ok; ++kv) {
-                        if (!mbar_wait_relaxed(empty(stage), phase ^ 1u, LIMIT_NS, abort_flag)) { ok = false; break; }
+                        if (!mbar_wait_relaxed(empty(stage), phase ^ 1u, a.limit_ns, abort_flag)) { ok = false; break; }
                         mbar_expect_tx(full(stage), C::TILE);
                         const uint32_t dst = ring + stage * C::TILE;
                         const int row = (kv ? row_v : row_k) + (tok & (a.g.T - 1));
@@ -299,7 +298,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         uint32_t phase = 0, qph[2] = {0, 0}, pph[2] = {0, 0};
         auto advance = [&]() { if (++stage == C::STAGES) { stage = 0; phase ^= 1u; } };
         auto wait = [&](uint32_t bar, uint32_t parity) {            // by all lanes
-            if (ok) ok = __all_sync(FULL, mbar_wait(bar, parity, LIMIT_NS, abort_flag)) != 0;
+            if (ok) ok = __all_sync(FULL, mbar_wait(bar, parity, a.limit_ns, abort_flag)) != 0;
             tc_fence_after();
         };
         // Operands are the same for all lanes, so that they stay in uniform registers: a product of 64 cycles leaves no time to bring them there
@@ -436,7 +435,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         upk2(add2(sums[0], sums[1]), u, v);
                         return u + v;
                     };
-                    ok = __all_sync(FULL, mbar_wait(s_full(t), sph, LIMIT_NS, abort_flag)) != 0;
+                    ok = __all_sync(FULL, mbar_wait(s_full(t), sph, a.limit_ns, abort_flag)) != 0;
                     sph ^= 1u;
                     if (!ok) break;
                     tc_fence_after();
@@ -518,7 +517,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     mbar_arrive(p_full(t));
                 }
                 if (!ok) break;
-                ok = __all_sync(FULL, mbar_wait(o_full(t), oph, LIMIT_NS, abort_flag)) != 0;
+                ok = __all_sync(FULL, mbar_wait(o_full(t), oph, a.limit_ns, abort_flag)) != 0;
                 oph ^= 1u;
                 if (!ok) break;
                 tc_fence_after();

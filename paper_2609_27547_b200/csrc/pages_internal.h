@@ -81,6 +81,8 @@ struct AttendArgs {
     int causal, window;
     int split;                                         // tokens of a piece; 0: not cut
     int team;                                          // warps that share an item
+    unsigned long long limit_ns;                       // bound of a wait
+    int test_drop_copies;                              // tests of the give-up path: the copying warp issues nothing
     float *part_o, *part_ml;                           // [pair][heads][hd] sums, [pair][heads][2] (reference, sum of weights)
 };
 

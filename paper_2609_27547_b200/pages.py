@@ -49,6 +49,8 @@ def _load():
         L.ebrl_pages_page_bytes.restype = u
         L.ebrl_pages_page_bytes.argtypes = [p]
         L.ebrl_pages_last_error.restype = C.c_char_p
+        L.ebrl_pages_test_drop_copies.argtypes = [u]
+        L.ebrl_pages_test_drop_copies.restype = None
         L.ebrl_pages_append.argtypes = [p, p, i, i, p, l, p, p, i, p, l, p, l, p, i, p]
         L.ebrl_pages_attend_workspace.restype = u
         L.ebrl_pages_attend_workspace.argtypes = [p, i, p, p, i, i, i, i, i]

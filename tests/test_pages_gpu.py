@@ -621,3 +621,24 @@ def test_refusals_on_the_device():
             fn()
     with pytest.raises(TypeError):
         pg.attend(lay, cache.pool, cache.table, q.float(), [1], [40])
+
+
+@pytest.mark.parametrize("hd,m", [(128, 200), (128, 20), (64, 40), (32, 40)])
+def test_a_wait_that_runs_out_is_noted_and_the_device_stays_usable(hd, m):
+    lay = pg.Layout(1, 1, hd, 64, BF)
+    cache = Cache(lay, [300], seed=1)
+    q = queries(lay, m, 1)
+    L = pg._load()
+    pg.check()
+    L.ebrl_pages_test_drop_copies(20_000_000)
+    try:
+        pg.attend(lay, cache.pool, cache.table, q, [m], [300])
+    finally:
+        L.ebrl_pages_test_drop_copies(0)
+    with pytest.raises(B.EbrlError) as e:
+        pg.check()
+    assert e.value.status == B.ERR_TIMEOUT
+    pg.check()                                  # it is told once
+    out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [300])
+    check(cache, 0, q, [m], out, lse)
+    pg.check()
