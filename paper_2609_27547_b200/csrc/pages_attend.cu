@@ -478,6 +478,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
 {
     constexpr int W = HD / 32;
     const int lane = threadIdx.x & 31;
+    pdl_wait();      // (set up while the last pieces are being worked on)
     const long long rows = (long long)sq.items * a.heads;      // (items: the queries of the cut sequences, counted in sq.item)
     for (long long x = (long long)blockIdx.x * 8 + (threadIdx.x >> 5); x < rows; x += (long long)gridDim.x * 8) {
         const int r = (int)(x / a.heads), head = (int)(x - (long long)r * a.heads);
@@ -550,12 +551,12 @@ cudaError_t launch_attend(const AttendArgs &a, const AttendSeqs &s, bool f32, in
     }
 }
 
-template <bool F32> static void join(const AttendArgs &a, const AttendSeqs &s, int grid, cudaStream_t st)
+template <bool F32> static cudaError_t join(const AttendArgs &a, const AttendSeqs &s, int grid, cudaStream_t st)
 {
     switch (a.g.hd) {
-    case 128: attend_join_kernel<128, F32><<<grid, 256, 0, st>>>(a, s); break;
-    case 64: attend_join_kernel<64, F32><<<grid, 256, 0, st>>>(a, s); break;
-    default: attend_join_kernel<32, F32><<<grid, 256, 0, st>>>(a, s);
+    case 128: return launch_kernel(attend_join_kernel<128, F32>, grid, 256, 0, st, 1, a, s);
+    case 64: return launch_kernel(attend_join_kernel<64, F32>, grid, 256, 0, st, 1, a, s);
+    default: return launch_kernel(attend_join_kernel<32, F32>, grid, 256, 0, st, 1, a, s);
     }
 }
 
@@ -564,9 +565,8 @@ cudaError_t launch_attend_join(const AttendArgs &a, const AttendSeqs &s, bool f3
     if (s.items == 0) return cudaSuccess;
     const long long need = ((long long)s.items * a.heads + 7) / 8, cap = quota ? quota : (long long)sms * 8;
     const int grid = (int)(need < cap ? need : cap);
-    if (f32) join<true>(a, s, grid, st);
-    else join<false>(a, s, grid, st);
-    return cudaGetLastError();
+    const Beside early(quota == 0);      // (under a quota its CTAs would wait on SMs beside the pieces')
+    return f32 ? join<true>(a, s, grid, st) : join<false>(a, s, grid, st);
 }
 
 }  // namespace pg
