@@ -442,7 +442,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     // First with the reference as it is: weights may grow to 2^16 in sum before anything needs to be done about it, so that the
                     // maximum of a tile is rarely asked for.
                     uint32_t P[64];
-                    {
+                    float sum = INFINITY;                                            // (an item's first tile: there is no reference yet)
+                    if (j) {
                         const uint64_t ref2 = pk2(-M, -M);
                         uint32_t A[32], B[32];
                         sums[0] = sums[1] = 0;
@@ -466,8 +467,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         tmem_wait_ld();
                         if (!whole) hide(B, 3, w[3]);
                         weights(B, P + 48, ref2);
+                        sum = total();
                     }
-                    float sum = total();
                     const bool redo = !(sum <= 65536.f) || M == -INFINITY;      // (a NaN, too)
                     if (!__any_sync(FULL, redo)) {
                         tmem_st32(s_at, P);
