@@ -476,17 +476,19 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     } else {
                         // The scores once more: their maximum, the sums so far in its terms, the weights.
                         uint32_t A[32];
-                        float top = -INFINITY;
+                        float part[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};   // (independent chains: each step waits for the one before it)
 #pragma unroll 1
                         for (int i = 0; i < 4; ++i) {
                             tmem_ld32(s_at + i * 32, A);
                             const unsigned w = words.word(j, i);
                             tmem_wait_ld();
-                            hide(A, i, w);
+                            if (!whole) hide(A, i, w);
 #pragma unroll
-                            for (int c = 0; c < 32; ++c) top = fmaxf(top, __uint_as_float(A[c]));
+                            for (int c = 0; c < 32; c += 8)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) part[k] = fmaxf(fmaxf(part[k], __uint_as_float(A[c + k])), __uint_as_float(A[c + 4 + k]));
                         }
-                        top *= sc;
+                        const float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * sc;
                         const float f = redo && top > M ? ex2(M - top) : 1.f;        // (0 the first time)
                         if (redo && top > M) M = top;
                         L *= f;
@@ -506,7 +508,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                             tmem_ld32(s_at + i * 32, A);
                             const unsigned w = words.word(j, i);
                             tmem_wait_ld();
-                            hide(A, i, w);
+                            if (!whole) hide(A, i, w);
                             weights(A, P, pk2(-ref, -ref));
                             tmem_st16(s_at + i * 16, P);                             // (in place of scores that have been read)
                         }
