@@ -151,12 +151,12 @@ struct Group {
 };
 
 // A sequence of more rows is taken by the tensor-memory kernel.  Measured, us, one warp per item / that kernel, 64 x 2000 tokens x 4 heads: heads of 128, 16 rows
-// 55 / -, 32 rows 83 / 53, 64 rows 159 / 54; of 64, 32 rows 41 / 43, 64 rows 115 / 43; of 32, 64 rows 65 / 61 (two tiles per CTA then).
+// 55 / -, 32 rows 83 / 53, 64 rows 159 / 54; of 64, 32 rows 41 / 42, 64 rows 115 / 42; of 32, 64 rows 65 / 61 (with two tiles per CTA).
 int chunk_from(int hd) { return hd == 128 ? 16 : 32; }
 
 // Its rows per item.  Two tiles that share what is loaded pay where the products take the time, and are never much worse there: heads of 128, 4 x 2000 new
 // tokens over 8 - 16 k x 16 heads 751 us against 779 in CTAs of one tile, 64 x 100 over 600 88 against 86.  Heads of 64 and 32 wait for the exponentials either way:
-// 4 x 2048 over 8 k 432 against 412, 64 x 100 over 600 75 against 70.
+// 4 x 2048 over 8 k 432 against 412, 64 x 100 over 600 75 against 70 (59 since such CTAs are persistent).
 int chunk_rows(int hd, int64_t rows) { return hd == 128 && rows > SMALL_CHUNK_ROWS ? CHUNK_ROWS : SMALL_CHUNK_ROWS; }
 
 struct Plan {
@@ -426,7 +426,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
                     ++s.n;
                 }
                 s.items = (int)items;
-                st = launched(gr.rows >= SMALL_CHUNK_ROWS ? launch_chunk(a, s, gr.rows, sm_quota, beside, (cudaStream_t)stream)
+                st = launched(gr.rows >= SMALL_CHUNK_ROWS ? launch_chunk(a, s, gr.rows, sm_quota, sms, beside, (cudaStream_t)stream)
                                                     : launch_attend(a, s, f32, gr.rows, sm_quota, beside, (cudaStream_t)stream));
                 beside = sm_quota == 0 && !any;
                 if (st != EBRL_OK) return st;

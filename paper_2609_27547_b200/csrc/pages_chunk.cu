@@ -25,6 +25,7 @@
 #include "f32x2.cuh"
 #include "ptx_helpers.cuh"
 
+#include <algorithm>
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <math.h>
@@ -249,6 +250,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(FULL, *tmem_slot, 0);
     bool ok = true;
+    // a CTA's items: there and back through the list, which begins with the longest
+    auto item_at = [&](int k) { return k * (int)gridDim.x + (k & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x); };
     pdl_launch_dependents();
 
     if (warp == COPY_WARP) {
@@ -257,7 +260,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         const int box = a.g.T < MAX_BOX ? a.g.T : MAX_BOX, boxes = KEYS / box;
         int stage = 0;
         uint32_t phase = 0;
-        for (int x = blockIdx.x; x < sq.items && ok && !a.test_drop_copies; x += gridDim.x) {
+        for (int k = 0, x; (x = item_at(k)) < sq.items && ok && !a.test_drop_copies; ++k) {
             const Item it = item_of<TILES>(a, sq, x);
             const int *tab = a.p.table + it.tab * a.p.stride;
             const int first_page = it.lo >> a.g.t_shift, n_pages = it.hi > 0 ? (it.hi - 1) / a.g.T + 1 : 0;   // (of the sequence, those below n_pages hold tokens that are seen)
@@ -326,7 +329,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
             }
         };
         auto commit = [&](uint32_t bar) { if (elect()) tc_commit(bar); };
-        for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
+        for (int k = 0, x; (x = item_at(k)) < sq.items && ok; ++k) {
             const Item it = item_of<TILES>(a, sq, x);
             if (it.n_kv == 0) continue;
             Words words;
@@ -381,7 +384,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         const uint32_t lanes = tmem + ((uint32_t)(tid & ~31) << 16), s_at = lanes + S_COL + t * KEYS, o_at = lanes + O_COL + t * HD;
         const float sc = a.scale * LOG2E;
         uint32_t sph = 0, oph = 0;
-        for (int x = blockIdx.x; x < sq.items && ok; x += gridDim.x) {
+        for (int k = 0, x; (x = item_at(k)) < sq.items && ok; ++k) {
             const Item it = item_of<TILES>(a, sq, x);
             if (t >= it.tiles) continue;
             const int r0 = it.r0 + t * ROWS, row = min(r0 + tid, it.R - 1), tok_q = row / a.G, head = it.kh * a.G + row - tok_q * a.G, first = it.len - it.m;
@@ -608,7 +611,7 @@ template <int HD> bool make_map(CUtensorMap *out, const Geometry &g, const Pages
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int HD, int TILES> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, bool beside, cudaStream_t st)
+template <int HD, int TILES> cudaError_t go(const AttendArgs &a, const AttendSeqs &s, int quota, int sms, bool beside, cudaStream_t st)
 {
     static std::atomic<bool> set[64];   // (calls may come from several threads; setting it twice is harmless)
     int dev = 0;
@@ -620,9 +623,11 @@ template <int HD, int TILES> cudaError_t go(const AttendArgs &a, const AttendSeq
     }
     CUtensorMap tm;
     if (!make_map<HD>(&tm, a.g, a.p)) return cudaErrorInvalidValue;
-    // one CTA per item, handed out by the hardware as the ones before end; under a quota persistent ones
+    // Two tiles: one CTA per item, handed out by the hardware as the ones before end.  One tile, or under a quota: persistent CTAs, whose copies and products run on into
+    // the next item (200 x 300 tokens x 64 rows 44 -> 38 us, 200 x 100 - 1500 tokens x 40 - 240 rows 88 -> 82; the most ragged batch tried 61 -> 63).
+    const int grid = std::min(s.items, quota ? quota : (TILES == 1 ? sms * Shape<HD, TILES>::PER_SM : s.items));
     const Beside with(beside);
-    return launch_kernel(chunk_kernel<HD, TILES>, quota && s.items > quota ? quota : s.items, Shape<HD, TILES>::THREADS, Shape<HD, TILES>::SMEM, st, 1, tm, a, s);
+    return launch_kernel(chunk_kernel<HD, TILES>, grid, Shape<HD, TILES>::THREADS, Shape<HD, TILES>::SMEM, st, 1, tm, a, s);
 }
 
 }  // namespace
@@ -632,11 +637,11 @@ bool chunk_supported(const Geometry &g, int n_pages, float scale)
     return g.es == 2 && scale > 0.f && (long long)g.layers * 2 * g.kvh * g.T <= INT32_MAX && n_pages < INT32_MAX;
 }
 
-cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, bool beside, cudaStream_t st)
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, int sms, bool beside, cudaStream_t st)
 {
     if (s.items == 0) return cudaSuccess;
-    if (a.g.hd == 128) return rows == CHUNK_ROWS ? go<128, 2>(a, s, quota, beside, st) : go<128, 1>(a, s, quota, beside, st);
-    return a.g.hd == 64 ? go<64, 1>(a, s, quota, beside, st) : go<32, 1>(a, s, quota, beside, st);
+    if (a.g.hd == 128) return rows == CHUNK_ROWS ? go<128, 2>(a, s, quota, sms, beside, st) : go<128, 1>(a, s, quota, sms, beside, st);
+    return a.g.hd == 64 ? go<64, 1>(a, s, quota, sms, beside, st) : go<32, 1>(a, s, quota, sms, beside, st);
 }
 
 cudaError_t take_status(int *status)

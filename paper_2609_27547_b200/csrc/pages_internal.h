@@ -116,7 +116,7 @@ cudaError_t launch_attend_join(const AttendArgs &a, const AttendSeqs &s, bool f3
 // The same for many query rows, bf16 (pages_chunk.cu): an item is a CTA of 256 of them, or one of 128, of which an SM holds two.
 constexpr int CHUNK_ROWS = 256, SMALL_CHUNK_ROWS = 128;
 bool chunk_supported(const Geometry &g, int n_pages, float scale);
-cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, bool beside, cudaStream_t st);
+cudaError_t launch_chunk(const AttendArgs &a, const AttendSeqs &s, int rows, int quota, int sms, bool beside, cudaStream_t st);
 
 // Whether a bounded wait ran out on the current device since the last call (waits for the device).
 cudaError_t take_status(int *status);
