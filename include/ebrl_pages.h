@@ -71,7 +71,7 @@ ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, i
  *     out = softmax(scale * q k^T) v,   lse = log sum_t exp(scale * q k_t)
  * over the tokens t that query j of sequence i (position p = len[i] - new_tokens[i] + j) sees: t < len[i], its mask bit is set, its page is there, and
  *   causal      != 0: t <= p.  0: every one (tokens of an observation that see one another, or queries that are no tokens of the sequence: cross attention)
- *   window      > 0 (only with causal): t > p - window.  0: no limit
+ *   window      > 0 (only with causal): t > p - window.  0, or any that is not below the longest length: no limit
  *   new_tokens  host [n], >= 0: number of queries (usually appended before; more than len[i] is allowed: with causal, those at negative positions see nothing)
  *   q           DEVICE, layout dtype, queries packed like the tokens of append: query r, head a at q + r * q_stride + a * head_dim
  *               (stride in elements, >= 0, a multiple of 16 bytes; not looked at for a single query).  Head a reads key/value head a / (n_heads / n_kv_heads).
@@ -83,7 +83,7 @@ ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, i
  * tokens, of missing pages and behind the length may hold anything.
  * Where sequences are few, a sequence is divided among warps, which are joined in shared memory, and a long one is cut into pieces besides, which a
  * second kernel joins.  split_tokens = 0 lets the call choose (a sequence's last bits can then depend on its company); -1 never divides or cuts (a
- * sequence's result then depends on nothing but itself); a positive multiple of 128 cuts every sequence into pieces of that many tokens.  The pieces' partial results need
+ * sequence's result then depends on nothing but itself); a positive multiple of 128 cuts every longer sequence into pieces of that many tokens.  The pieces' partial results need
  * ebrl_pages_attend_workspace bytes (of the same arguments) of DEVICE memory, 16-byte aligned, that no other call in flight uses (two captured graphs that
  * may run at once need one each); 0 bytes: workspace may be NULL.
  * bf16: products of bf16 operands, weights rounded to bf16; weights are relative to a reference that may lie below a row's largest score, so that sums of

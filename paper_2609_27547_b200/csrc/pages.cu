@@ -272,6 +272,14 @@ ebrl_status_t check_attend_counts(const ebrl_pages_layout_t *l, int32_t n, const
     return EBRL_OK;
 }
 
+// A call's window and pieces, small enough for 32-bit arithmetic.
+void bound(int32_t n, const int32_t *len, int32_t &window, int32_t &split_tokens)
+{
+    const int longest = *std::max_element(len, len + n);
+    window = bounded_window(window, longest);
+    split_tokens = bounded_split(split_tokens, longest);
+}
+
 uint64_t part_bytes(const ebrl_pages_layout_t &l, uint64_t pairs, int n_heads) { return pairs * n_heads * (l.head_dim + 2) * 4; }
 
 }  // namespace
@@ -355,6 +363,7 @@ uint64_t ebrl_pages_attend_workspace(const ebrl_pages_layout_t *layout, int32_t 
             if (len[i] < 0 || len[i] > 1 << 30) BAD("len[%d] = %d is outside 0..2^30", i, len[i]);
         int sms = 0;
         if ((st = device_sms(0, &sms)) != EBRL_OK) return st;
+        bound(n, len, window, split_tokens);
         for (int chunks = 0; chunks < 2; ++chunks) {   // of either kernel: which one it is may depend on the scale
             Plan p;
             plan(p, *layout, n, new_tokens, len, n_heads, window, split_tokens, std::max<int>(sm_quota, 0), sms, chunks && chunk_supported(geometry_of(*layout), 0, 1.f));
@@ -389,6 +398,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
         if (!std::isfinite(scale)) BAD("scale must be finite");
         int sms = 0;
         if ((st = device_sms(sm_quota, &sms)) != EBRL_OK) return st;
+        bound(n, len, window, split_tokens);
         Plan p;
         plan(p, *layout, n, new_tokens, len, n_heads, window, split_tokens, sm_quota, sms, chunk_supported(g, n_pages, scale));
         const uint64_t need = part_bytes(*layout, p.pairs, n_heads);

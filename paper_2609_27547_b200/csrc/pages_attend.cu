@@ -126,12 +126,8 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
         const int r0 = rt * ROWS, r1 = min(R, r0 + ROWS);                 // its rows; row = token * G + member
         const int first = len - m;                                        // position of query 0
         // the tokens that some row of the item sees: lo .. hi
-        int lo = first_token(len, m, a.window), hi = len;
-        if (a.split) { lo += piece * a.split; hi = min(hi, lo + a.split); }
-        if (a.causal) {
-            hi = min(hi, first + (r1 - 1) / G + 1);
-            if (a.window) lo = max(lo, first + r0 / G - a.window + 1);
-        }
+        const Span span = seen_by(len, m, G, r0, r1, a.causal, a.window, a.split, piece);
+        int lo = span.lo, hi = span.hi;
         const int seen = lo;                                              // no row sees a token below
         lo = lo / TK * TK;
         if constexpr (TEAM) {   // this warp's even share
@@ -213,11 +209,11 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
                 M[i][e] = -INFINITY; L[i][e] = 0.f;
                 const int tok = min(r0 + i * 16 + e * 8 + g, R - 1) / G;
                 last[i][e] = a.causal ? first + tok + 1 : 0x7fffffff;
-                from[i][e] = a.window ? first + tok + 1 - a.window : -0x7fffffff;
+                from[i][e] = first_seen(first + tok, a.window);
             }
         }
         const int all_last = a.causal ? first + r0 / G + 1 : 0x7fffffff;                  // tokens below are seen by every row ...
-        const int all_from = a.window ? first + (r1 - 1) / G + 1 - a.window : -0x7fffffff; // ... and from here on
+        const int all_from = first_seen(first + (r1 - 1) / G, a.window);                  // ... and from here on
 
         for (int j = 0; j < tiles; ++j) {
             cp_wait<C::STAGES - 2>();

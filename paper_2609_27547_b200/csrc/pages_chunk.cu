@@ -159,16 +159,11 @@ template <int TILES> __device__ __forceinline__ Item item_of(const AttendArgs &a
     const int rt = RT - 1 - rest % RT;                        // the last rows see most
     it.kh = kh; it.piece = rest / RT;
     it.r0 = rt * ITEM;
-    const int r1 = min(it.R, it.r0 + ITEM), first = it.len - it.m;
+    const int r1 = min(it.R, it.r0 + ITEM);
     it.tiles = r1 - it.r0 > ROWS ? 2 : 1;
-    int lo = first_token(it.len, it.m, a.window), hi = it.len;
-    if (a.split) { lo += it.piece * a.split; hi = min(hi, lo + a.split); }
-    if (a.causal) {
-        hi = min(hi, first + (r1 - 1) / a.G + 1);
-        if (a.window) lo = max(lo, first + it.r0 / a.G - a.window + 1);
-    }
-    it.lo = lo / KEYS * KEYS; it.hi = hi; it.seen = lo;
-    it.n_kv = hi > it.lo ? (hi - it.lo + KEYS - 1) / KEYS : 0;
+    const Span span = seen_by(it.len, it.m, a.G, it.r0, r1, a.causal, a.window, a.split, it.piece);
+    it.lo = span.lo / KEYS * KEYS; it.hi = span.hi; it.seen = span.lo;
+    it.n_kv = it.hi > it.lo ? (it.hi - it.lo + KEYS - 1) / KEYS : 0;
     return it;
 }
 
@@ -405,7 +400,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 mbar_arrive(q_full(t));
                 Words words;
                 words.start(a, a.p.table + it.tab * a.p.stride, it, lane);
-                const int last = a.causal ? first + tok_q + 1 : 0x7fffffff, from = a.window ? first + tok_q + 1 - a.window : -0x7fffffff;
+                const int last = a.causal ? first + tok_q + 1 : 0x7fffffff, from = first_seen(first + tok_q, a.window);
                 const int all_last = __reduce_min_sync(FULL, last), all_from = __reduce_max_sync(FULL, from);   // what every row of the warp sees
                 const uint64_t sc2 = pk2(sc, sc);
                 for (int j = 0; j < it.n_kv && ok; ++j) {

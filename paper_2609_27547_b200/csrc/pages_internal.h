@@ -3,6 +3,7 @@
 
 #include "../../include/ebrl_pages.h"
 #include "actgen_internal.h"
+#include "pages_span.h"
 
 #include <atomic>
 
@@ -85,18 +86,6 @@ struct AttendArgs {
     int test_drop_copies;                              // tests of the give-up path: the copying warp issues nothing
     float *part_o, *part_ml;                           // [pair][heads][hd] sums, [pair][heads][2] (reference, sum of weights)
 };
-
-// The first token that a query of the sequence sees (rounded down to 128): where its first piece begins.
-__host__ __device__ inline int first_token(int len, int m, int window)
-{
-    const int lo = window ? len - m + 1 - window : 0;
-    return lo > 0 ? lo / 128 * 128 : 0;
-}
-__host__ __device__ inline int pieces_of(int len, int m, int window, int split)
-{
-    const int n = len - first_token(len, m, window);
-    return split && n > split ? (int)(((long long)n + split - 1) / split) : 1;
-}
 
 // A launch that may begin as soon as the CTAs of the one before it have begun (beside: they share nothing but what both read), and ends after it: the kernels
 // of one call take turns at the SMs without a gap.
