@@ -9,8 +9,9 @@
 //                tensor map, which reads zeros
 //     products   one warp: S = Q K^T of a tile is issued behind the O += P V that reads its last weights, so that with two tiles the order is
 //                PV_A(j) QK_A(j + 1) PV_B(j) QK_B(j + 1)
-//   Weights are first taken against the reference as it stands, and a tile's maximum is looked for only where their sum exceeds 2^16 (or there is no reference
-//   yet): bf16 keeps its 8 bits whatever their size.  Sums in tensor memory are then rescaled by the softmax threads themselves, which know from
+//   Weights are first taken against the reference as it stands, and a tile's maximum is looked for only where a row's weights would add up to more than 2^16 (or there
+//   is no reference yet): bf16 keeps its 8 bits whatever their size.  Where they do so against the largest score, too (very many tokens), the reference goes 2^8 beyond
+//   it, so that sums of weights times values never exceed 2^16 times the values.  Sums in tensor memory are then rescaled by the softmax threads themselves, which know from
 //   S(j) being there that PV(j - 1) is done.
 //   Tokens that no row may see are masked in S; their value rows are set to zero in shared memory before the product, so that what stands there (NaN in a
 //   row nobody wrote) does not meet a weight of zero.
@@ -437,8 +438,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     sph ^= 1u;
                     if (!ok) break;
                     tc_fence_after();
-                    // First with the reference as it is: weights may grow to 2^16 in sum before anything needs to be done about it, so that the
-                    // maximum of a tile is rarely asked for.
+                    // First with the reference as it is: a row's weights may grow to 2^16 in sum before anything needs to be done about it, so that
+                    // the maximum of a tile is rarely asked for.
                     uint32_t P[64];
                     float sum = INFINITY;                                            // (an item's first tile: there is no reference yet)
                     if (j) {
@@ -467,7 +468,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         weights(B, P + 48, ref2);
                         sum = total();
                     }
-                    const bool redo = !(sum <= 65536.f) || M == -INFINITY;      // (a NaN, too)
+                    const bool redo = !(L + sum <= 65536.f) || M == -INFINITY;  // (a NaN, too)
                     if (!__any_sync(FULL, redo)) {
                         tmem_st32(s_at, P);
                         tmem_st32(s_at + 32, P + 32);
@@ -487,8 +488,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                                 for (int k = 0; k < 4; ++k) part[k] = fmaxf(fmaxf(part[k], __uint_as_float(A[c + k])), __uint_as_float(A[c + 4 + k]));
                         }
                         const float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * sc;
-                        const float f = redo && top > M ? ex2(M - top) : 1.f;        // (0 the first time)
+                        float f = redo && top > M ? ex2(M - top) : 1.f;              // (0 the first time)
                         if (redo && top > M) M = top;
+                        if (redo && L * f > 32768.f) { f *= 1.f / 256; M += 8.f; }   // (this tile adds 128 at most: the row's sum is below 2^16 again)
                         L *= f;
                         if (j)
 #pragma unroll 1

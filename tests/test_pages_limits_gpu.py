@@ -41,3 +41,48 @@ def test_the_largest_pieces_behind_a_window(dtype, hd, G):
     for split in (1024, 2 ** 30, LARGEST // 128 * 128):
         got = pg.attend(lay, cache.pool, cache.table, q, counts, lens, window=10, split_tokens=split)
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def constant(lay, n, key, value, seed=0):
+    """One sequence whose keys are key[t] along the first column and 0 elsewhere, and whose values are value[t] in all columns."""
+    cache = Cache(lay, [n], seed=seed)
+    kv = torch.zeros((1, 2, lay.n_kv_heads, n, lay.head_dim))
+    kv[0, 0, :, :, 0] = key
+    kv[0, 1] = value[:, None]
+    kv = kv.to(lay.dtype)
+    cache.kv = [kv.double()]
+    elems, _ = pg.views(lay, cache.pool)
+    T = lay.page_tokens
+    for j, p in enumerate(cache.rows[0]):
+        k = min(T, n - j * T)
+        elems[p, 0, :, :, :k] = kv[0, :, :, j * T:j * T + k].cuda()
+    return cache
+
+
+@pytest.mark.parametrize("hd,m", [(128, 200), (128, 100), (64, 100), (32, 100)])
+def test_sums_of_large_values_stay_finite(hd, m):
+    """A first tile far below the others, just so much that no single tile's weights (2^8.93 each) ask for another reference: what they add up to is
+    bounded all the same.  Sums may be 2^16 times the values: 4e33 * 2^16 = 2.6e38 is finite, 2^16 times 130 tiles would not be."""
+    lay = pg.Layout(1, 1, hd, 128, BF)
+    n = 130 * 128
+    key = torch.full((n,), 6.1875)
+    key[:128] = 0
+    g = torch.Generator().manual_seed(hd)
+    cache = constant(lay, n, key, 4e33 * (0.5 + 0.5 * torch.rand(n, generator=g)))
+    q = torch.zeros((m, 1, hd), dtype=BF, device="cuda")
+    q[:, 0, 0] = 1
+    for split in (-1, 1024):
+        out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [n], scale=1.0, causal=False, split_tokens=split)
+        check(cache, 0, q, [m], out, lse, scale=1.0, causal=False)
+
+
+@pytest.mark.parametrize("hd", [128, 64])
+def test_many_tokens_of_one_weight(hd):
+    """More tokens than the bound of the sums: the reference leaves the largest score behind."""
+    lay = pg.Layout(1, 1, hd, 256, BF)
+    n, m = 200_000, 130
+    g = torch.Generator().manual_seed(hd)
+    cache = constant(lay, n, torch.zeros(n), 4e33 * (0.5 + 0.5 * torch.rand(n, generator=g)))
+    q = torch.ones((m, 1, hd), dtype=BF, device="cuda")
+    out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [n], causal=False, split_tokens=-1)
+    check(cache, 0, q, [m], out, lse, causal=False)
