@@ -46,8 +46,8 @@ uint64_t ebrl_pages_page_bytes(const ebrl_pages_layout_t *layout);
 /* Text of the last error of this thread's ebrl_pages calls; valid until its next one. */
 const char *ebrl_pages_last_error(void);
 
-/* Waits of the kernels on their own copies are bounded (4 s).  When one runs out, the kernel leaves its results as they are and notes
- * it; this call waits for the current device's work, returns EBRL_ERR_TIMEOUT if that happened on it since the last call, and
+/* Waits of the kernels on their own copies are bounded (4 s).  When one runs out, the rows that were not finished (of cut sequences, all rows that wanted a piece)
+ * are left as they are, and the kernel notes it; this call waits for the current device's work, returns EBRL_ERR_TIMEOUT if that happened on it since the last call, and
  * forgets it. */
 ebrl_status_t ebrl_pages_check(void);
 

@@ -482,10 +482,13 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
         const int tok = r - seq.item, m = seq.m, np = pieces_of(seq.len, m, a.window, a.split);
         const size_t at0 = ((size_t)seq.part + tok) * a.heads + head, step = (size_t)m * a.heads;
         float top = -INFINITY, sum = 0.f;
+        bool there = true;                         // (a piece whose kernel gave up a wait has NaN for a reference)
         for (int p = lane; p < np; p += 32) {      // relative to the piece whose weights add up to most, so that its sums are no larger than its values
             const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at0 + p * step));
             top = fmaxf(top, ml.x + log2f(ml.y));
+            there = there && ml.x == ml.x;
         }
+        if (!__all_sync(FULL, there)) continue;
 #pragma unroll
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
         const float ref = top == -INFINITY ? 0.f : top;

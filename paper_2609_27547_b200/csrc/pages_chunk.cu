@@ -15,7 +15,7 @@
 //   S(j) being there that PV(j - 1) is done.
 //   Tokens that no row may see are masked in S; their value rows are set to zero in shared memory before the product, so that what stands there (NaN in a
 //   row nobody wrote) does not meet a weight of zero.
-//   All waits are bounded: when one runs out the CTA notes it, lets its copies land, frees tensor memory and returns.
+//   All waits are bounded: when one runs out the CTA notes it, marks the pieces that it did not finish, lets its copies land, frees tensor memory and returns.
 //
 //   What bounds it: 4 x 2000 - 2048 new tokens over 8 - 16 k x 16 heads of 128 take 750 us, 1.1 PFLOP/s.  The products alone (softmax skipped) take 630: a
 //   128 x 128 x 128 product from shared memory reads 128 bytes a cycle, all there are, and the copies want a quarter of that, too.  The rest is
@@ -380,7 +380,8 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         const uint32_t lanes = tmem + ((uint32_t)(tid & ~31) << 16), s_at = lanes + S_COL + t * KEYS, o_at = lanes + O_COL + t * HD;
         const float sc = a.scale * LOG2E;
         uint32_t sph = 0, oph = 0;
-        for (int k = 0, x; (x = item_at(k)) < sq.items && ok; ++k) {
+        int k = 0, x;
+        for (; (x = item_at(k)) < sq.items; ++k) {
             const Item it = item_of<TILES>(a, sq, x);
             if (t >= it.tiles) continue;
             const int r0 = it.r0 + t * ROWS, row = min(r0 + tid, it.R - 1), tok_q = row / a.G, head = it.kh * a.G + row - tok_q * a.G, first = it.len - it.m;
@@ -557,6 +558,13 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
             if (mine && cut) { a.part_ml[2 * at] = M; a.part_ml[2 * at + 1] = L; }
             if (mine && !cut && a.lse) a.lse[out_row * a.heads + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
             tc_fence_before();
+        }
+        // Where a wait ran out: pieces that this warp did not finish are marked, so that the join leaves their rows alone.
+        for (; !ok && a.split && (x = item_at(k)) < sq.items; ++k) {
+            const Item it = item_of<TILES>(a, sq, x);
+            const int row = it.r0 + t * ROWS + tid, tok_q = row / a.G;
+            if (it.part >= 0 && row < it.R)
+                a.part_ml[2 * (((size_t)it.part + (size_t)it.piece * it.m + tok_q) * a.heads + it.kh * a.G + row - tok_q * a.G)] = __int_as_float(0x7fffffff);
         }
     }
 

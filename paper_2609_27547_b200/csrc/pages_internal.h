@@ -84,7 +84,7 @@ struct AttendArgs {
     int team;                                          // warps that share an item
     unsigned long long limit_ns;                       // bound of a wait
     int test_drop_copies;                              // tests of the give-up path: the copying warp issues nothing
-    float *part_o, *part_ml;                           // [pair][heads][hd] sums, [pair][heads][2] (reference, sum of weights)
+    float *part_o, *part_ml;                           // [pair][heads][hd] sums, [pair][heads][2] (reference, NaN where there is no result; sum of weights)
 };
 
 // A launch that may begin as soon as the CTAs of the one before it have begun (beside: they share nothing but what both read), and ends after it: the kernels

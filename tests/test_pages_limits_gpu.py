@@ -2,6 +2,7 @@
 import pytest
 import torch
 
+from paper_2609_27547_b200 import binding as B
 from paper_2609_27547_b200 import pages as pg
 from test_pages_gpu import BF, F, Cache, check, queries
 
@@ -86,3 +87,30 @@ def test_many_tokens_of_one_weight(hd):
     q = torch.ones((m, 1, hd), dtype=BF, device="cuda")
     out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [n], causal=False, split_tokens=-1)
     check(cache, 0, q, [m], out, lse, causal=False)
+
+
+@pytest.mark.parametrize("hd,m", [(128, 200), (128, 20), (64, 40), (32, 40)])
+def test_what_a_wait_that_ran_out_left_unfinished_is_not_joined(hd, m):
+    """Cut sequences whose pieces never came to an end leave out and lse as they are; the queries, too, where out is q."""
+    lay = pg.Layout(1, 2, hd, 64, BF)
+    lens, counts = [300, 100, 700], [m, m, m]
+    cache = Cache(lay, lens, seed=1)
+    q = queries(lay, 3 * m, 1)
+    L = pg._load()
+    pg.check()
+    for same in (False, True):
+        out = q.clone() if same else torch.full_like(q, 7.0)
+        lse = torch.full((3 * m, 2), 7.0, device="cuda")
+        L.ebrl_pages_test_drop_copies(20_000_000)
+        try:
+            pg.attend(lay, cache.pool, cache.table, out if same else q, counts, lens, out=out, lse=lse, split_tokens=128)
+        finally:
+            L.ebrl_pages_test_drop_copies(0)
+        with pytest.raises(B.EbrlError) as e:
+            pg.check()
+        assert e.value.status == B.ERR_TIMEOUT
+        assert torch.equal(out, q) if same else bool((out == 7).all())
+        assert bool((lse == 7).all())
+    out, lse = pg.attend(lay, cache.pool, cache.table, q, counts, lens, split_tokens=128)
+    check(cache, 0, q, counts, out, lse)
+    pg.check()
