@@ -13,7 +13,7 @@
  * padded to a multiple of 128 bytes (ebrl_pages_page_bytes).  A pool is n_pages pages in a row, 16-byte aligned.  A table names the
  * pages of a call's sequences: DEVICE int32, row i of it at table + i * table_stride, token t of sequence i lies in page
  * table[i][t / page_tokens].  An entry outside 0 .. n_pages - 1 says that the page is not there: its tokens are not seen, nothing is read from or
- * written to it.  Lengths and numbers of tokens are host arrays, checked and copied before the call returns; pages are looked up
+ * written to it.  Where all lengths are 0 the table may be NULL.  Lengths and numbers of tokens are host arrays, checked and copied before the call returns; pages are looked up
  * on the device.  Rows of a page that no token of a sequence has been written to may hold anything, NaN included.
  *
  * Sequences of a call may share pages that are only read.  append, copy and whatever else writes a page that another call uses are ordered by the
@@ -137,7 +137,7 @@ ebrl_status_t ebrl_pages_book_shorten(ebrl_pages_book_t book, int32_t n, const i
 /* Moves pages in use with the highest numbers to the lowest free ones until they are the first ones of the pool, or `room` moves are made. */
 ebrl_status_t ebrl_pages_book_compact(ebrl_pages_book_t book, int32_t room, int32_t *from, int32_t *to, int32_t *tokens, int32_t *n_moves);
 
-/* Host table of sequences: row i at out + i * stride, -1 behind a sequence's last page.  stride >= the most pages of one. */
+/* Host table of sequences: row i at out + i * stride, -1 behind a sequence's last page.  stride >= the most pages of one; where it is 0, out may be NULL. */
 ebrl_status_t ebrl_pages_book_table(ebrl_pages_book_t book, int32_t n, const int32_t *seqs, int32_t *out, int64_t stride);
 /* Length of a sequence, -1 if there is no such; pages in use (each counted once). */
 int32_t ebrl_pages_book_len(ebrl_pages_book_t book, int32_t seq);

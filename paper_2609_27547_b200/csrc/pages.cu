@@ -76,7 +76,9 @@ ebrl_status_t check_pool(const ebrl_pages_layout_t *l, const void *pool, int32_t
 ebrl_status_t check_seqs(const ebrl_pages_layout_t *l, int32_t n, const int32_t *table, int64_t table_stride, const int32_t *len)
 {
     if (!len) BAD("len is NULL");
-    if (!table || ((uintptr_t)table & 3)) BAD("table is NULL or not 4-byte aligned");
+    bool any = false;                 // (a table without columns has no address)
+    for (int i = 0; i < n; ++i) any = any || len[i] > 0;
+    if ((!table && any) || ((uintptr_t)table & 3)) BAD("table is NULL or not 4-byte aligned");
     if (table_stride < 0) BAD("table_stride must not be negative");
     for (int i = 0; i < n; ++i) {
         if (len[i] < 0 || len[i] > 1 << 30) BAD("len[%d] = %d is outside 0..2^30", i, len[i]);

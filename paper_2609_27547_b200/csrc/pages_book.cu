@@ -250,7 +250,7 @@ ebrl_status_t ebrl_pages_book_table(ebrl_pages_book_t b, int32_t n, const int32_
     return guarded([&]() -> ebrl_status_t {
         const ebrl_status_t st = check_seqs(b, n, seqs, false);
         if (st != EBRL_OK) return st;
-        if (n && (!out || stride < 0)) BAD("out is NULL or stride is negative");
+        if (n && ((!out && stride) || stride < 0)) BAD("out is NULL or stride is negative");
         for (int i = 0; i < n; ++i)
             if ((int64_t)b->seqs[seqs[i]].pages.size() > stride) BAD("sequence %d has %d pages, the table's rows %lld entries", seqs[i], (int)b->seqs[seqs[i]].pages.size(), (long long)stride);
         for (int i = 0; i < n; ++i) {

@@ -1,4 +1,6 @@
 """GPU tests of the operators on paged caches at the ends of their arguments' ranges.  References and tolerances are those of test_pages_gpu.py."""
+import math
+
 import pytest
 import torch
 
@@ -114,3 +116,25 @@ def test_what_a_wait_that_ran_out_left_unfinished_is_not_joined(hd, m):
     out, lse = pg.attend(lay, cache.pool, cache.table, q, counts, lens, split_tokens=128)
     check(cache, 0, q, counts, out, lse)
     pg.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+def test_a_group_that_was_reset_as_a_whole(dtype):
+    """The book's table of sequences without tokens has no columns; every operator takes it."""
+    lay = pg.Layout(1, 2, 64, 32, dtype)
+    book, pool = pg.Book(8, 32, 3), pg.new_pool(lay, 8)
+    table = book.table([0, 1, 2], device="cuda")
+    assert table.shape == (3, 0)
+    before = pool.clone()
+    x = queries(lay, 60, 1)
+    pg.append(lay, pool, table, x[:0], x[:0], [0, 0, 0], [0, 0, 0])
+    for counts in ([0, 0, 0], [1, 0, 2], [3, 50, 1]):
+        q = x[:sum(counts)]
+        for causal in (True, False):
+            out, lse = pg.attend(lay, pool, table, q, counts, [0, 0, 0], causal=causal)
+            assert out.shape == q.shape and bool((out == 0).all()) and bool((lse == -math.inf).all())
+    planes = pg.gather(lay, pool, table, [0, 0, 0])
+    assert [tuple(p.shape) for p in planes] == [(1, 2, 0, 128)] * 3
+    whole = torch.full((3, 1, 2, 5, 128), 7.0, dtype=dtype, device="cuda")
+    pg.gather(lay, pool, table, [0, 0, 0], whole)
+    assert bool((whole == 7).all()) and torch.equal(pool, before)
