@@ -38,6 +38,14 @@ class Layout(NamedTuple):
         return _page(self)[1]
 
 
+def _int32(v, what: str) -> int:
+    """A plain integer that a call takes in 32 bits (ctypes would drop the others)."""
+    v = int(v)
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError("%s = %d does not fit 32 bits" % (what, v))
+    return v
+
+
 _lib = None
 
 
@@ -77,7 +85,7 @@ def _page(layout: Layout):
     """(the C struct, a page's bytes, a reference that calls take; it holds the struct): kept, because a layout is a plain value."""
     if layout.dtype not in _DTYPES:
         raise TypeError("pages hold bf16 or fp32, not %s" % (layout.dtype,))
-    c = _CLayout(*[int(v) for v in layout[:4]], _DTYPES[layout.dtype])
+    c = _CLayout(*[_int32(v, f) for v, f in zip(layout, Layout._fields[:4])], _DTYPES[layout.dtype])
     at = C.byref(c)
     return c, int(_load().ebrl_pages_page_bytes(at)), at
 
@@ -149,6 +157,13 @@ def _counts(new, lens):
     return N, L
 
 
+def _rows32(rows):
+    """The distances of planes, in rows, which a call takes in 32 bits."""
+    if max(rows, default=0) >= 2 ** 31:
+        raise ValueError("planes are 2^31 rows or more apart")
+    return rows
+
+
 def new_pool(layout: Layout, n_pages: int, device="cuda") -> torch.Tensor:
     """A zeroed pool of ``n_pages`` pages."""
     return torch.zeros((int(n_pages), _covered(layout)[1]), dtype=torch.uint8, device=device)
@@ -166,6 +181,7 @@ def append(layout: Layout, pool: torch.Tensor, table: torch.Tensor, k: torch.Ten
            mask: Optional[torch.Tensor] = None, sm_quota: int = 0, stream: Optional[torch.cuda.Stream] = None):
     """``ebrl_pages_append``: writes the keys and values k, v [sum(new), kv_heads, head_dim] of each sequence's ``new`` last tokens, of one layer;
     ``lens`` are the lengths with them.  ``mask``: uint8 or bool [sum(new)], 0 hides a token."""
+    layer, sm_quota = _int32(layer, "layer"), _int32(sm_quota, "sm_quota")
     cl = _pool(layout, pool)
     N, L = _counts(new, lens)
     n, total = N.numel(), _sum(N)
@@ -181,8 +197,8 @@ def append(layout: Layout, pool: torch.Tensor, table: torch.Tensor, k: torch.Ten
     with _on(pool.device):
         st = _stream(pool.device, stream, pool, table, k, v, mask)
         if n:
-            _check(_load().ebrl_pages_append(cl, pool.data_ptr(), pool.shape[0], n, at, stride, N.data_ptr(), L.data_ptr(), int(layer), k.data_ptr(), k.stride(0),
-                                             v.data_ptr(), v.stride(0), None if mask is None else mask.data_ptr(), int(sm_quota), st))
+            _check(_load().ebrl_pages_append(cl, pool.data_ptr(), pool.shape[0], n, at, stride, N.data_ptr(), L.data_ptr(), layer, k.data_ptr(), k.stride(0),
+                                             v.data_ptr(), v.stride(0), None if mask is None else mask.data_ptr(), sm_quota, st))
 
 
 def attend(layout: Layout, pool: torch.Tensor, table: torch.Tensor, q: torch.Tensor, new, lens, *, layer: int = 0, causal: bool = True, window: int = 0,
@@ -190,6 +206,7 @@ def attend(layout: Layout, pool: torch.Tensor, table: torch.Tensor, q: torch.Ten
            stream: Optional[torch.cuda.Stream] = None):
     """``ebrl_pages_attend``: (out, lse) of the queries q [>= sum(new), heads, head_dim], ``new`` of each sequence, over the sequences; lse fp32
     [.., heads].  ``scale``: default 1 / sqrt(head_dim).  Rows behind the last query are left as they were (zeros where ``out`` is made here)."""
+    layer, window, split_tokens, sm_quota = _int32(layer, "layer"), _int32(window, "window"), _int32(split_tokens, "split_tokens"), _int32(sm_quota, "sm_quota")
     cl = _pool(layout, pool)
     N, L = _counts(new, lens)
     n, total = N.numel(), _sum(N)
@@ -210,7 +227,7 @@ def attend(layout: Layout, pool: torch.Tensor, table: torch.Tensor, q: torch.Ten
     with _on(pool.device):
         need = 0
         if total and (split_tokens > 0 or (split_tokens == 0 and most >= 512)):   # (left to itself the library cuts no shorter sequence)
-            need = dll.ebrl_pages_attend_workspace(cl, n, N.data_ptr(), L.data_ptr(), heads, 1 if causal else 0, int(window), int(split_tokens), int(sm_quota))
+            need = dll.ebrl_pages_attend_workspace(cl, n, N.data_ptr(), L.data_ptr(), heads, 1 if causal else 0, window, split_tokens, sm_quota)
         # what is allocated here belongs to the stream that writes it; results are used on the current one, too
         with torch.cuda.stream(stream) if _elsewhere(pool.device, stream) else _HERE:
             make = q.new_empty if rows == total else q.new_zeros
@@ -221,15 +238,16 @@ def attend(layout: Layout, pool: torch.Tensor, table: torch.Tensor, q: torch.Ten
             ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
         st = _stream(pool.device, stream, pool, table, q, out, lse)
         if n and heads:
-            _check(dll.ebrl_pages_attend(cl, pool.data_ptr(), pool.shape[0], n, at, stride, N.data_ptr(), L.data_ptr(), int(layer), q.data_ptr(), q.stride(0), heads,
+            _check(dll.ebrl_pages_attend(cl, pool.data_ptr(), pool.shape[0], n, at, stride, N.data_ptr(), L.data_ptr(), layer, q.data_ptr(), q.stride(0), heads,
                                          out.data_ptr(), out.stride(0), lse.data_ptr(), 1.0 / math.sqrt(hd) if scale is None else float(scale),
-                                         1 if causal else 0, int(window), int(split_tokens), ws.data_ptr() if need else None, need, int(sm_quota), st))
+                                         1 if causal else 0, window, split_tokens, ws.data_ptr() if need else None, need, sm_quota, st))
     return out, lse
 
 
 def copy(layout: Layout, src: torch.Tensor, dst: torch.Tensor, moves, *, sm_quota: int = 0, stream: Optional[torch.cuda.Stream] = None):
     """``ebrl_pages_copy``: pages of ``src`` to pages of ``dst`` (the same pool, or one that does not overlap it).  ``moves``: (from, to, tokens) as
     ``Book`` returns them, or (from, to); host data."""
+    sm_quota = _int32(sm_quota, "sm_quota")
     cl = _pool(layout, src, "src")
     _pool(layout, dst, "dst")
     parts = [_host(m, "moves") for m in moves]
@@ -241,7 +259,7 @@ def copy(layout: Layout, src: torch.Tensor, dst: torch.Tensor, moves, *, sm_quot
         st = _stream(src.device, stream, src, dst)
         if n:
             _check(_load().ebrl_pages_copy(cl, src.data_ptr(), src.shape[0], dst.data_ptr(), dst.shape[0], n, parts[0].data_ptr(), parts[1].data_ptr(),
-                                           parts[2].data_ptr() if len(parts) == 3 else None, int(sm_quota), st))
+                                           parts[2].data_ptr() if len(parts) == 3 else None, sm_quota, st))
 
 
 def gather(layout: Layout, pool: torch.Tensor, table: torch.Tensor, lens, planes: Optional[Planes] = None, *, mask=None, sm_quota: int = 0,
@@ -249,6 +267,7 @@ def gather(layout: Layout, pool: torch.Tensor, table: torch.Tensor, lens, planes
     """``ebrl_pages_gather``: sequences -> planes, the form that ``ActGen.submit`` and ``prefix8.quantize`` take.  ``planes``: one tensor [n,
     kv_layers, 2, P, heads * head_dim], or a sequence of tensors [kv_layers, 2, P_i, ..] (columns contiguous, planes a multiple of the row stride apart); default:
     new ones [kv_layers, 2, lens[i], ..].  ``mask``: uint8 [n, >= P] or a sequence of uint8 tensors / None: gets each token's visibility."""
+    sm_quota = _int32(sm_quota, "sm_quota")
     cl = _pool(layout, pool)
     L = _host(lens, "lens")
     n, d = L.numel(), layout.n_kv_heads * layout.head_dim
@@ -278,6 +297,7 @@ def gather(layout: Layout, pool: torch.Tensor, table: torch.Tensor, lens, planes
             if x.numel() and ((d > 1 and sd[3] != 1) or r != rs or r < d or plane % rs or plane < sh[2] * rs or (layout.kv_layers > 1 and sd[0] != 2 * plane)):
                 raise ValueError("columns must be contiguous, planes share one row stride and lie a whole number of rows apart")
             rows.append(plane // rs)
+        _rows32(rows)
         if whole and n > 1 and planes.numel() and planes.stride(0) < (layout.kv_layers * 2 - 1) * planes.stride(2) + (planes.shape[3] - 1) * rs + d:
             raise ValueError("the planes of the sequences overlap")
         if whole:
@@ -301,7 +321,7 @@ def gather(layout: Layout, pool: torch.Tensor, table: torch.Tensor, lens, planes
         _same_device(pool, table, *views_, *masks)
         st = _stream(pool.device, stream, pool, table, *views_, *masks)
         if n:
-            _check(_load().ebrl_pages_gather(cl, pool.data_ptr(), pool.shape[0], n, at, stride, L.data_ptr(), ptrs, rows, rs, mp, int(sm_quota), st))
+            _check(_load().ebrl_pages_gather(cl, pool.data_ptr(), pool.shape[0], n, at, stride, L.data_ptr(), ptrs, rows, rs, mp, sm_quota, st))
     return planes
 
 
@@ -317,7 +337,7 @@ class Book:
 
     def __init__(self, n_pages: int, page_tokens: int, max_sequences: int, *, _of: Optional["Book"] = None):
         self._L, self._b = _load(), C.c_void_p()
-        self.n_pages, self.page_tokens, self.max_sequences = int(n_pages), int(page_tokens), int(max_sequences)
+        self.n_pages, self.page_tokens, self.max_sequences = _int32(n_pages, "n_pages"), _int32(page_tokens, "page_tokens"), _int32(max_sequences, "max_sequences")
         _check(self._L.ebrl_pages_book_clone(_of._b, C.byref(self._b)) if _of is not None else
                self._L.ebrl_pages_book_create(self.n_pages, self.page_tokens, self.max_sequences, C.byref(self._b)))
 
@@ -346,11 +366,13 @@ class Book:
     def shorten(self, seqs: Sequence[int], lens):
         """``lens``: an int or one per sequence; 0 frees them."""
         s = _host(seqs, "seqs")
-        s, v, fn = self._call(self._L.ebrl_pages_book_shorten, s, torch.full((s.numel(),), lens, dtype=torch.int32) if isinstance(lens, int) else lens, "lens")
+        s, v, fn = self._call(self._L.ebrl_pages_book_shorten, s, [lens] * s.numel() if isinstance(lens, int) else lens, "lens")
         _check(fn(self._b, s.numel(), s.data_ptr(), v.data_ptr()))
 
     def compact(self, most: Optional[int] = None):
-        room = min(self.used, self.n_pages - self.used) if most is None else int(most)
+        room = min(self.used, self.n_pages - self.used)      # (there are no more moves than that)
+        if most is not None:
+            room = max(-1, min(room, int(most)))
         m, k = self._moves(max(0, room))
         _check(self._L.ebrl_pages_book_compact(self._b, room, m[0].data_ptr(), m[1].data_ptr(), m[2].data_ptr(), C.byref(k)))
         return m[0, :k.value], m[1, :k.value], m[2, :k.value]
@@ -365,7 +387,8 @@ class Book:
         return out.to(device, non_blocking=True)
 
     def len(self, seq: int) -> int:
-        return int(self._L.ebrl_pages_book_len(self._b, int(seq)))
+        seq = int(seq)
+        return int(self._L.ebrl_pages_book_len(self._b, seq if 0 <= seq < 2 ** 31 else -1))
 
     @property
     def used(self) -> int:

@@ -8,7 +8,7 @@ import torch
 
 from paper_2609_27547_b200 import binding as B
 from paper_2609_27547_b200 import pages as pg
-from test_pages_host import L, append, attend, gather
+from test_pages_host import LAY, L, append, attend, gather
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -46,3 +46,50 @@ def test_table_of_empty_sequences():
     assert L.ebrl_pages_book_table(book._b, 1, seqs, None, 0) == B.OK
     for stride in (1, -1):
         assert L.ebrl_pages_book_table(book._b, 1, seqs, None, stride) == B.ERR_INVALID_ARG
+
+
+def test_integers_of_more_than_32_bits_are_refused():
+    pool, table = pg.new_pool(LAY, 2, device="cpu"), torch.zeros((1, 2), dtype=torch.int32)
+    q = torch.zeros((1, 4, 64), dtype=torch.bfloat16)
+    for bad in (2 ** 31, 2 ** 32 + 1, -2 ** 31 - 1, 2 ** 64):
+        for name in ("layer", "window", "split_tokens", "sm_quota"):
+            with pytest.raises(ValueError, match=name):
+                pg.attend(LAY, pool, table, q, [1], [1], **{name: bad})
+        for name in ("layer", "sm_quota"):
+            with pytest.raises(ValueError, match=name):
+                pg.append(LAY, pool, table, q, q, [1], [1], **{name: bad})
+        with pytest.raises(ValueError, match="sm_quota"):
+            pg.copy(LAY, pool, pool, ([0], [1]), sm_quota=bad)
+        with pytest.raises(ValueError, match="sm_quota"):
+            pg.gather(LAY, pool, table, [1], sm_quota=bad)
+        for name in LAY._fields[:4]:
+            with pytest.raises(ValueError, match=name):
+                pg.new_pool(LAY._replace(**{name: bad}), 1, device="cpu")
+        for args in ((bad, 32, 1), (1, bad, 1), (1, 32, bad)):
+            with pytest.raises(ValueError):
+                pg.Book(*args)
+        book = pg.Book(4, 32, 2)
+        book.extend([0], [40])
+        assert book.len(bad) == -1
+        for fn in (lambda: book.shorten([0], bad), lambda: book.extend([0], [bad]), lambda: book.fork([0], [bad])):
+            with pytest.raises(ValueError):
+                fn()
+        assert book.used == 2 and book.len(0) == 40
+
+
+def test_compaction_with_any_number_of_moves_at_most():
+    for most, moves in ((2 ** 31 - 1, 2), (2 ** 32 + 1, 2), (2 ** 64, 2), (1, 1), (0, 0)):
+        book = pg.Book(8, 32, 3)
+        book.extend([0, 1], [64, 64])
+        book.shorten([0], 0)
+        assert [len(m) for m in book.compact(most)] == [moves] * 3
+    for most in (-1, -2 ** 31, -2 ** 31 - 1, -2 ** 32):
+        with pytest.raises(B.EbrlError):
+            book.compact(most)
+
+
+def test_planes_too_far_apart_are_refused():
+    """The distance of planes travels as a number of rows in 32 bits."""
+    assert pg._rows32([0, 2 ** 31 - 1]) == [0, 2 ** 31 - 1]
+    with pytest.raises(ValueError):
+        pg._rows32([5, 2 ** 31])
