@@ -405,6 +405,12 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
         plan(p, *layout, n, new_tokens, len, n_heads, window, split_tokens, sm_quota, sms, chunk_supported(g, n_pages, scale));
         const uint64_t need = part_bytes(*layout, p.pairs, n_heads);
         if (p.pairs > INT32_MAX) return fail(EBRL_ERR_UNSUPPORTED, "too many pieces in one call");
+        auto items_of = [&](const Group &gr, int i) {
+            return (((int64_t)new_tokens[i] * (n_heads / g.kvh) + gr.rows - 1) / gr.rows) * g.kvh * pieces_of(len[i], new_tokens[i], window, gr.split);
+        };
+        for (const Group &gr : p.groups)
+            for (int i : gr.seqs)
+                if (items_of(gr, i) > 1 << 30) return fail(EBRL_ERR_UNSUPPORTED, "too many query rows, heads and pieces in sequence %d", i);
         if (need && (!workspace || ((uintptr_t)workspace & 15) || workspace_bytes < need))
             BAD("a 16-byte aligned workspace of %llu bytes is needed", (unsigned long long)need);
         AttendArgs a{};
@@ -429,8 +435,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
                 bool any = false;
                 for (; at < gr.seqs.size() && s.n < SEQS; ++at) {
                     const int i = gr.seqs[at], np = pieces_of(len[i], new_tokens[i], window, gr.split);
-                    const int64_t mine = (((int64_t)new_tokens[i] * a.G + gr.rows - 1) / gr.rows) * g.kvh * np;
-                    if (mine > 1 << 30) return fail(EBRL_ERR_UNSUPPORTED, "too many pieces in one sequence");
+                    const int64_t mine = items_of(gr, i);
                     if (items + mine > 1 << 30) break;
                     s.s[s.n] = {(int)items, (int)p.row[i], new_tokens[i], len[i], i, np > 1 ? (int)pair : -1};
                     if (np > 1) { pair += (int64_t)np * new_tokens[i]; any = true; }

@@ -138,3 +138,21 @@ def test_a_group_that_was_reset_as_a_whole(dtype):
     whole = torch.full((3, 1, 2, 5, 128), 7.0, dtype=dtype, device="cuda")
     pg.gather(lay, pool, table, [0, 0, 0], whole)
     assert bool((whole == 7).all()) and torch.equal(pool, before)
+
+
+def test_a_sequence_with_too_many_items_is_refused_before_anything_is_enqueued():
+    """1024 sequences that fill a launch, and one whose query rows and heads make 2^31 items."""
+    lay = pg.Layout(1, 64, 32, 32, F)
+    n, m, huge = 1025, 17, 2 ** 30 - 1
+    cache = Cache(lay, [2], seed=1)
+    table = cache.table[:1, :1].expand(n, 1).contiguous()
+    q = queries(lay, 1, 1)
+    out = torch.full(((n - 1) * m, 64, 32), 7.0, device="cuda")
+    counts, lens = [m] * (n - 1) + [huge], [2] * (n - 1) + [1]
+    L, ints = pg._load(), lambda v: (pg.C.c_int32 * len(v))(*v)
+    st = L.ebrl_pages_attend(pg._pool(lay, cache.pool), cache.pool.data_ptr(), cache.n_pages, n, table.data_ptr(), 1, ints(counts), ints(lens), 0, q.data_ptr(), 0, 64,
+                             out.data_ptr(), 64 * 32, None, 1.0, 0, 0, -1, None, 0, 0, torch.cuda.current_stream().cuda_stream)
+    assert st == B.ERR_UNSUPPORTED and bool((out == 7).all())
+    L.ebrl_pages_attend(pg._pool(lay, cache.pool), cache.pool.data_ptr(), cache.n_pages, n - 1, table.data_ptr(), 1, ints(counts), ints(lens), 0, q.data_ptr(), 0, 64,
+                        out.data_ptr(), 64 * 32, None, 1.0, 0, 0, -1, None, 0, 0, torch.cuda.current_stream().cuda_stream)
+    assert bool((out[::m] == out[0]).all()) and not bool((out == 7).any())
