@@ -397,7 +397,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
         if (rows > 1 && (q_stride < 0 || o_stride < 0 || q_stride * g.es % 16 || o_stride * g.es % 16)) BAD("strides must be multiples of 16 bytes and not negative");
         if (rows > 1 && o_stride < width) BAD("output rows overlap one another");
         if (rows > 1 && out == q && o_stride != q_stride) BAD("out may be q only with the same stride");
-        if (!std::isfinite(scale)) BAD("scale must be finite");
+        if (!std::isfinite(scale * 1.4426950408889634f)) BAD("scale must be finite, and below 2.3e38");   // (scores are taken in units of log 2)
         int sms = 0;
         if ((st = device_sms(sm_quota, &sms)) != EBRL_OK) return st;
         bound(n, len, window, split_tokens);

@@ -93,3 +93,11 @@ def test_planes_too_far_apart_are_refused():
     assert pg._rows32([0, 2 ** 31 - 1]) == [0, 2 ** 31 - 1]
     with pytest.raises(ValueError):
         pg._rows32([5, 2 ** 31])
+
+
+def test_scales_that_leave_fp32_are_refused():
+    """The kernels take scores in units of log 2: scale * 1.4427 has to be a number."""
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        assert attend(scale=scale) == B.ERR_INVALID_ARG
+    for scale in (2.3e38, -2.3e38, 1e-45, 0.0):
+        assert attend(scale=scale) != B.ERR_INVALID_ARG
