@@ -156,3 +156,17 @@ def test_a_sequence_with_too_many_items_is_refused_before_anything_is_enqueued()
     L.ebrl_pages_attend(pg._pool(lay, cache.pool), cache.pool.data_ptr(), cache.n_pages, n - 1, table.data_ptr(), 1, ints(counts), ints(lens), 0, q.data_ptr(), 0, 64,
                         out.data_ptr(), 64 * 32, None, 1.0, 0, 0, -1, None, 0, 0, torch.cuda.current_stream().cuda_stream)
     assert bool((out[::m] == out[0]).all()) and not bool((out == 7).any())
+
+
+@pytest.mark.parametrize("hd", [128, 64, 32])
+def test_scales_that_are_not_positive_with_many_rows(hd):
+    """bf16 rows that a positive scale would send to the tensor-memory kernel."""
+    lay = pg.Layout(1, 2, hd, 64, BF)
+    lens, counts = [700, 90, 40, 1300], [33, 90, 50, 1]
+    cache = Cache(lay, lens, hide=0.2, lost=0.1, seed=hd)
+    for G in (1, 3):
+        q = queries(lay, sum(counts), G, seed=G)
+        for scale in (0.0, -0.1):
+            for kw in (dict(), dict(split_tokens=-1), dict(split_tokens=256), dict(sm_quota=20), dict(window=37), dict(causal=False)):
+                out, lse = pg.attend(lay, cache.pool, cache.table, q, counts, lens, scale=scale, **kw)
+                check(cache, 0, q, counts, out, lse, scale=scale, causal=kw.get("causal", True), window=kw.get("window", 0))
