@@ -78,7 +78,7 @@ ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, i
  *   n_heads     a multiple of n_kv_heads, at most 65536, and n_heads / n_kv_heads at most 128
  *   out         DEVICE, layout dtype, laid out like q with its own stride; may be q itself.  Rows behind the last query are left as they were.
  *   lse         DEVICE fp32 [queries][n_heads], or NULL
- *   scale       softmax scale, of at most 2.3e38 either way (usually 1 / sqrt(head_dim))
+ *   scale       softmax scale, of at most 2.3e38 either way (usually 1 / sqrt(head_dim)); scores, too, may be as large as that
  * A row that sees no token gives out = 0 and lse = -inf.  Keys and values of tokens that some query of the call sees must be finite; those of hidden
  * tokens, of missing pages and behind the length may hold anything.
  * Where sequences are few, a sequence is divided among warps, which are joined in shared memory, and a long one is cut into pieces besides, which a

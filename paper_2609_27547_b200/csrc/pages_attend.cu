@@ -291,7 +291,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const int c = n * 8 + 2 * t + (e & 1);
-                            S[i][n][e] *= sc;
+                            S[i][n][e] = __fmul_rn(S[i][n][e], sc);       // (rounded, as the maxima are: scores beyond 2^23 would else be off from them)
                             if (!whole && !(((see >> c) & 1) && tok + c < last[i][e >> 1] && tok + c >= from[i][e >> 1])) S[i][n][e] = -INFINITY;
                         }
                 bool moved = false;

@@ -379,6 +379,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         const int t = warp >> 2, tid = threadIdx.x & (ROWS - 1);
         const uint32_t lanes = tmem + ((uint32_t)(tid & ~31) << 16), s_at = lanes + S_COL + t * KEYS, o_at = lanes + O_COL + t * HD;
         const float sc = a.scale * LOG2E;
+        // Up to this reference scores lose 2^-2 at most when they are rounded to its precision.  Beyond it the weights' argument, formed unrounded, would be off from
+        // the rounded reference by as much as that reference's last bits (2^7 at 2^32: weights of 0 or inf), so that scores are rounded first.
+        constexpr float FINE = 4194304.f;
         uint32_t sph = 0, oph = 0;
         int k = 0, x;
         for (; (x = item_at(k)) < sq.items; ++k) {
@@ -419,7 +422,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     };
                     // The weights of 32 columns, packed, and two times two sums of theirs.
                     uint64_t sums[2];
-                    auto weights = [&](const uint32_t *v, uint32_t *P, uint64_t ref2) {
+                    auto weights = [&](const uint32_t *v, uint32_t *P, uint64_t ref2, uint64_t sc2) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             float p0, p1;
@@ -455,21 +458,21 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         tmem_wait_ld();
                         tmem_ld32(s_at + 32, B);
                         if (!whole) hide(A, 0, w[0]);
-                        weights(A, P, ref2);
+                        weights(A, P, ref2, sc2);
                         tmem_wait_ld();
                         tmem_ld32(s_at + 64, A);
                         if (!whole) hide(B, 1, w[1]);
-                        weights(B, P + 16, ref2);
+                        weights(B, P + 16, ref2, sc2);
                         tmem_wait_ld();
                         tmem_ld32(s_at + 96, B);
                         if (!whole) hide(A, 2, w[2]);
-                        weights(A, P + 32, ref2);
+                        weights(A, P + 32, ref2, sc2);
                         tmem_wait_ld();
                         if (!whole) hide(B, 3, w[3]);
-                        weights(B, P + 48, ref2);
+                        weights(B, P + 48, ref2, sc2);
                         sum = total();
                     }
-                    const bool redo = !(L + sum <= 65536.f) || M == -INFINITY;  // (a NaN, too)
+                    const bool redo = !(L + sum <= 65536.f) || !(fabsf(M) < FINE);  // (a NaN or no reference, too)
                     if (!__any_sync(FULL, redo)) {
                         tmem_st32(s_at, P);
                         tmem_st32(s_at + 32, P + 32);
@@ -488,10 +491,10 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) part[k] = fmaxf(fmaxf(part[k], __uint_as_float(A[c + k])), __uint_as_float(A[c + 4 + k]));
                         }
-                        const float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])) * sc;
+                        const float top = __fmul_rn(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])), sc);
                         float f = redo && top > M ? ex2(M - top) : 1.f;              // (0 the first time)
                         if (redo && top > M) M = top;
-                        if (redo && L * f > 32768.f) { f *= 1.f / 256; M += 8.f; }   // (this tile adds 128 at most: the row's sum is below 2^16 again)
+                        if (redo && L * f > 32768.f) { const float up = M + 8.f; f *= ex2(M - up); M = up; }   // (this tile adds 128 at most)
                         L *= f;
                         if (j)
 #pragma unroll 1
@@ -503,6 +506,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                                 tmem_st32(o_at + i * 32, A);
                             }
                         const float ref = M == -INFINITY ? 0.f : M;                  // (a row that has seen nothing yet)
+                        const bool coarse = !(fabsf(ref) < FINE), any_coarse = __any_sync(FULL, coarse);
                         sums[0] = sums[1] = 0;
 #pragma unroll 1
                         for (int i = 0; i < 4; ++i) {
@@ -510,7 +514,11 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                             const unsigned w = words.word(j, i);
                             tmem_wait_ld();
                             if (!whole) hide(A, i, w);
-                            weights(A, P, pk2(-ref, -ref));
+                            if (any_coarse)
+#pragma unroll
+                                for (int c = 0; c < 32; ++c)                         // (a score whose product with sc is the rounded one, relative to the reference)
+                                    if (coarse) A[c] = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(A[c]), sc), -ref));
+                            weights(A, P, coarse ? 0ull : pk2(-ref, -ref), coarse ? pk2(1.f, 1.f) : sc2);
                             tmem_st16(s_at + i * 16, P);                             // (in place of scores that have been read)
                         }
                         sum = total();

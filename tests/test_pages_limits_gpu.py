@@ -170,3 +170,40 @@ def test_scales_that_are_not_positive_with_many_rows(hd):
             for kw in (dict(), dict(split_tokens=-1), dict(split_tokens=256), dict(sm_quota=20), dict(window=37), dict(causal=False)):
                 out, lse = pg.attend(lay, cache.pool, cache.table, q, counts, lens, scale=scale, **kw)
                 check(cache, 0, q, counts, out, lse, scale=scale, causal=kw.get("causal", True), window=kw.get("window", 0))
+
+
+@pytest.mark.parametrize("dtype,hd,m", [(BF, 64, 1), (BF, 128, 1), (BF, 64, 20), (BF, 128, 20), (BF, 128, 200), (BF, 64, 40), (BF, 32, 40), (F, 64, 1), (F, 64, 40), (F, 128, 20)])
+def test_scores_whose_last_bits_are_large(dtype, hd, m):
+    """Scores of one size, however large, are equal weights.  lse: the score is one product, with two constants (log2 e, ln 2) and three roundings around it, each off
+    by 2^-24 of it at most, together less than 2^-21; fp32 operands lose 5 * 2^-22 besides."""
+    lay = pg.Layout(1, 1, hd, 64, dtype)
+    n = 300
+    g = torch.Generator().manual_seed(hd)
+    lose = 2.0 ** -21 + (5 * 2.0 ** -22 if dtype is F else 0)
+    for size in (1e4, 1e7, 1e9, 1e10, 1e12, 1e20, 1e30, 1e38):
+        for sign in (1, -1):
+            cache = constant(lay, n, torch.full((n,), math.sqrt(size)), 0.5 + torch.rand(n, generator=g))
+            q = torch.zeros((m, 1, hd), dtype=dtype, device="cuda")
+            q[:, :, 0] = sign * math.sqrt(size)
+            score = float(q[0, 0, 0].double() * cache.kv[0][0, 0, 0, 0, 0])
+            for split in (0, -1, 128):
+                out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [n], scale=1.0, split_tokens=split)
+                alike = torch.log(torch.arange(n - m + 1, n + 1, device="cuda", dtype=torch.float64))[:, None]
+                check(cache, 0, torch.zeros_like(q), [m], out, alike.float(), scale=1.0)
+                assert bool(((lse.double() - alike - score).abs() <= lose * (abs(score) + alike)).all()), (size, sign, split)
+
+
+def test_one_visible_token_with_any_score():
+    """Its values are the result: off by the rounding of its weight (2^-8; the weight is 2 to the power of what the reference lost when it was rounded, which is not
+    always a bf16 number, while the sum that divides it is not rounded) and by that of the result (2^-8), together (1 + 2^-8)^2 - 1 = 2^-7 + 2^-16 of them at most."""
+    lay = pg.Layout(1, 1, 64, 64, BF)
+    cache = Cache(lay, [200], seed=3)
+    _, words = pg.views(lay, cache.pool)
+    words.zero_()
+    words[cache.rows[0][1], 0] = 1 << 5                  # token 69
+    want = cache.kv[0][0, 1, 0, 69].to(BF).cuda()
+    for m in (1, 20, 100):
+        for size in (1.0, 1e5, 1e8, 1e15):
+            q = (queries(lay, m, 1).float() * size).to(BF)
+            out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [200], causal=False)
+            assert bool(((out.double() - want.double()).abs() <= (2.0 ** -7 + 2.0 ** -16) * want.double().abs()).all()) and bool(torch.isfinite(lse).all())
