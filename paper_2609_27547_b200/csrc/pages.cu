@@ -3,6 +3,7 @@
 #include "pages_internal.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstdarg>
 #include <cstdio>
@@ -418,7 +419,7 @@ ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *p
         a.p = {(char *)pool, n_pages, table, table_stride};
         a.layer = layer; a.heads = n_heads; a.G = n_heads / g.kvh;
         a.q = (const char *)q; a.out = (char *)out; a.q_stride = q_stride; a.o_stride = o_stride;
-        a.lse = lse; a.scale = scale; a.causal = causal != 0; a.window = window;
+        a.lse = lse; a.scale = scale; a.up = std::min(8.f / std::max(scale * 1.4426950408889634f, FLT_MIN * .125f), FLT_MAX); a.causal = causal != 0; a.window = window;
         a.limit_ns = t_drop_limit ? t_drop_limit : 4000000000ull;
         a.test_drop_copies = t_drop_limit != 0;
         a.part_o = (float *)workspace;

@@ -468,7 +468,7 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
     pdl_wait();      // (the end of this kernel is to be that of the ones beside it, too)
 }
 
-// Joins the pieces of cut sequences: one warp per (query, head), sums in the order of the pieces.
+// Joins the pieces of cut sequences: one warp per (query, head), sums in a fixed order.
 template <int HD, bool F32>
 __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ AttendSeqs sq)
 {
@@ -493,15 +493,28 @@ __global__ void __launch_bounds__(256) attend_join_kernel(const __grid_constant_
         for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(FULL, top, o));
         const float ref = top == -INFINITY ? 0.f : top;
         float v[W] = {};
-#pragma unroll 4
-        for (int p = 0; p < np; ++p) {
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at0 + p * step));
-            const float f = ex2(ml.x - ref);
-            sum = fmaf(f, ml.y, sum);
-            const float *o = a.part_o + (at0 + p * step) * HD + lane * W;
+        for (int base = 0; base < np; base += 32) {      // each lane weighs a piece
+            const int mine = base + lane, n = min(32, np - base);
+            const float2 ml = mine < np ? *reinterpret_cast<const float2 *>(a.part_ml + 2 * (at0 + mine * step)) : make_float2(-INFINITY, 0.f);
+            const float f_mine = ex2(ml.x - ref);
+            sum = fmaf(f_mine, ml.y, sum);
+            const float *o = a.part_o + (at0 + base * step) * HD + lane * W;
+            for (int p0 = 0; p0 < n; p0 += 16) {         // (16 pieces at once: two 65 k-token histories 64 us, four at once 69)
+                float x[16][W];
 #pragma unroll
-            for (int c = 0; c < W; ++c) v[c] = fmaf(f, o[c], v[c]);
+                for (int p = 0; p < 16; ++p)
+#pragma unroll
+                    for (int c = 0; c < W; ++c) x[p][c] = p0 + p < n ? o[(p0 + p) * step * HD + c] : 0.f;
+#pragma unroll
+                for (int p = 0; p < 16; ++p) {
+                    const float f = __shfl_sync(FULL, f_mine, p0 + p);
+#pragma unroll
+                    for (int c = 0; c < W; ++c) v[c] = fmaf(f, x[p][c], v[c]);
+                }
+            }
         }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(FULL, sum, o);
         const float inv = sum == 0.f ? 0.f : 1.f / sum;
         const size_t row = (size_t)seq.row + tok, at = row * a.o_stride + (size_t)head * HD + lane * W;
 #pragma unroll

@@ -15,7 +15,7 @@
 //   S(j) being there that PV(j - 1) is done.
 //   Tokens that no row may see are masked in S; their value rows are set to zero in shared memory before the product, so that what stands there (NaN in a
 //   row nobody wrote) does not meet a weight of zero.
-//   All waits are bounded: when one runs out the CTA notes it, marks the pieces that it did not finish, lets its copies land, frees tensor memory and returns.
+//   All waits are bounded: when one runs out the CTA notes it, marks its pieces, lets its copies land, frees tensor memory and returns.
 //
 //   What bounds it: 4 x 2000 - 2048 new tokens over 8 - 16 k x 16 heads of 128 take 750 us, 1.1 PFLOP/s.  The products alone (softmax skipped) take 630: a
 //   128 x 128 x 128 product from shared memory reads 128 bytes a cycle, all there are, and the copies want a quarter of that, too.  The rest is
@@ -168,6 +168,9 @@ template <int TILES> __device__ __forceinline__ Item item_of(const AttendArgs &a
     return it;
 }
 
+// A CTA's items: there and back through the list, which begins with the longest.
+__device__ __forceinline__ int item_at(int k) { return k * (int)gridDim.x + (k & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x); }
+
 // Mask words of an item's tokens, 32 of them (8 tiles) held by the lanes of a warp, the next 32 on their way.
 struct Words {
     const int *tab;
@@ -208,6 +211,16 @@ struct Words {
     __device__ __forceinline__ unsigned word(int j, int i) const { return __shfl_sync(FULL, now, (j & 7) * 4 + i); }
 };
 
+// Where a wait ran out: the CTA's pieces (some may have been finished) are marked, so that the join leaves their rows alone.
+template <int TILES> __device__ __noinline__ void mark_unfinished(const AttendArgs &a, const AttendSeqs &sq)
+{
+    for (int k = 0, x; (x = item_at(k)) < sq.items; ++k) {
+        const Item it = item_of<TILES>(a, sq, x);
+        for (int row = it.r0 + threadIdx.x; it.part >= 0 && row < min(it.R, it.r0 + TILES * ROWS); row += blockDim.x)
+            a.part_ml[2 * (((size_t)it.part + (size_t)it.piece * it.m + row / a.G) * a.heads + it.kh * a.G + row % a.G)] = __int_as_float(0x7fffffff);
+    }
+}
+
 template <int HD, int TILES>
 __global__ void __launch_bounds__(Shape<HD, TILES>::THREADS, Shape<HD, TILES>::PER_SM)
 chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ AttendArgs a, const __grid_constant__ AttendSeqs sq)
@@ -246,8 +259,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(FULL, *tmem_slot, 0);
     bool ok = true;
-    // a CTA's items: there and back through the list, which begins with the longest
-    auto item_at = [&](int k) { return k * (int)gridDim.x + (k & 1 ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x); };
     pdl_launch_dependents();
 
     if (warp == COPY_WARP) {
@@ -379,16 +390,16 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
         const int t = warp >> 2, tid = threadIdx.x & (ROWS - 1);
         const uint32_t lanes = tmem + ((uint32_t)(tid & ~31) << 16), s_at = lanes + S_COL + t * KEYS, o_at = lanes + O_COL + t * HD;
         const float sc = a.scale * LOG2E;
-        // Up to this reference scores lose 2^-2 at most when they are rounded to its precision.  Beyond it the weights' argument, formed unrounded, would be off from
-        // the rounded reference by as much as that reference's last bits (2^7 at 2^32: weights of 0 or inf), so that scores are rounded first.
-        constexpr float FINE = 4194304.f;
+        // Scores of this size (in units of log 2) are 32 and more apart where they are not the same, so that a row's weights are 1 and next to nothing; the rounding of the
+        // reference may be more than fp32 has exponents.  They are taken with a power of two for a scale (at most sc, at least half of it), whose products are exact.
+        constexpr float FINE = 1073741824.f;
+        const float sc_pow2 = __uint_as_float(__float_as_uint(sc) & 0x7f800000u);
         uint32_t sph = 0, oph = 0;
-        int k = 0, x;
-        for (; (x = item_at(k)) < sq.items; ++k) {
+        for (int k = 0, x; (x = item_at(k)) < sq.items && ok; ++k) {
             const Item it = item_of<TILES>(a, sq, x);
             if (t >= it.tiles) continue;
             const int r0 = it.r0 + t * ROWS, row = min(r0 + tid, it.R - 1), tok_q = row / a.G, head = it.kh * a.G + row - tok_q * a.G, first = it.len - it.m;
-            float M = -INFINITY, L = 0.f;
+            float R = -INFINITY, L = 0.f;                            // the reference, a score before the scale, and the sum of the weights
             if (it.n_kv) {
                 // queries: every product that read the last item's is done (its results were waited for)
                 constexpr int PIECES = HD / 8, PER_STEP = 32 / PIECES, PP = C::SWZ / 16;     // rows that a warp copies in a step: its own
@@ -422,7 +433,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     };
                     // The weights of 32 columns, packed, and two times two sums of theirs.
                     uint64_t sums[2];
-                    auto weights = [&](const uint32_t *v, uint32_t *P, uint64_t ref2, uint64_t sc2) {
+                    auto weights = [&](const uint32_t *v, uint32_t *P, uint64_t sc2, uint64_t ref2) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             float p0, p1;
@@ -446,6 +457,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                     // the maximum of a tile is rarely asked for.
                     uint32_t P[64];
                     float sum = INFINITY;                                            // (an item's first tile: there is no reference yet)
+                    const float M = __fmul_rn(R, sc);                                // (rounded: off by up to 2^5 below FINE, a factor that all of the row's weights share)
                     if (j) {
                         const uint64_t ref2 = pk2(-M, -M);
                         uint32_t A[32], B[32];
@@ -458,18 +470,18 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         tmem_wait_ld();
                         tmem_ld32(s_at + 32, B);
                         if (!whole) hide(A, 0, w[0]);
-                        weights(A, P, ref2, sc2);
+                        weights(A, P, sc2, ref2);
                         tmem_wait_ld();
                         tmem_ld32(s_at + 64, A);
                         if (!whole) hide(B, 1, w[1]);
-                        weights(B, P + 16, ref2, sc2);
+                        weights(B, P + 16, sc2, ref2);
                         tmem_wait_ld();
                         tmem_ld32(s_at + 96, B);
                         if (!whole) hide(A, 2, w[2]);
-                        weights(A, P + 32, ref2, sc2);
+                        weights(A, P + 32, sc2, ref2);
                         tmem_wait_ld();
                         if (!whole) hide(B, 3, w[3]);
-                        weights(B, P + 48, ref2, sc2);
+                        weights(B, P + 48, sc2, ref2);
                         sum = total();
                     }
                     const bool redo = !(L + sum <= 65536.f) || !(fabsf(M) < FINE);  // (a NaN or no reference, too)
@@ -491,10 +503,14 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) part[k] = fmaxf(fmaxf(part[k], __uint_as_float(A[c + k])), __uint_as_float(A[c + 4 + k]));
                         }
-                        const float top = __fmul_rn(fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3])), sc);
-                        float f = redo && top > M ? ex2(M - top) : 1.f;              // (0 the first time)
-                        if (redo && top > M) M = top;
-                        if (redo && L * f > 32768.f) { const float up = M + 8.f; f *= ex2(M - up); M = up; }   // (this tile adds 128 at most)
+                        const float top = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+                        float f = 1.f;
+                        if (redo && top > R) { f = ex2((R - top) * sc); R = top; }   // (0 the first time)
+                        if (redo && L * f > 32768.f) {                               // (this tile adds 128 at most)
+                            const float up = fminf(R + a.up, 3.4028235e38f);
+                            f *= ex2((R - up) * sc);
+                            R = up;
+                        }
                         L *= f;
                         if (j)
 #pragma unroll 1
@@ -505,8 +521,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                                 for (int c = 0; c < 32; ++c) A[c] = __float_as_uint(__uint_as_float(A[c]) * f);
                                 tmem_st32(o_at + i * 32, A);
                             }
-                        const float ref = M == -INFINITY ? 0.f : M;                  // (a row that has seen nothing yet)
-                        const bool coarse = !(fabsf(ref) < FINE), any_coarse = __any_sync(FULL, coarse);
+                        float scw = sc, ref = __fmul_rn(R, sc);
+                        if (!(fabsf(ref) < FINE)) { scw = sc_pow2; ref = R * sc_pow2; }
+                        if (R == -INFINITY) ref = 0.f;                               // (a row that has seen nothing yet)
                         sums[0] = sums[1] = 0;
 #pragma unroll 1
                         for (int i = 0; i < 4; ++i) {
@@ -514,11 +531,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                             const unsigned w = words.word(j, i);
                             tmem_wait_ld();
                             if (!whole) hide(A, i, w);
-                            if (any_coarse)
-#pragma unroll
-                                for (int c = 0; c < 32; ++c)                         // (a score whose product with sc is the rounded one, relative to the reference)
-                                    if (coarse) A[c] = __float_as_uint(__fadd_rn(__fmul_rn(__uint_as_float(A[c]), sc), -ref));
-                            weights(A, P, coarse ? 0ull : pk2(-ref, -ref), coarse ? pk2(1.f, 1.f) : sc2);
+                            weights(A, P, pk2(scw, scw), pk2(-ref, -ref));
                             tmem_st16(s_at + i * 16, P);                             // (in place of scores that have been read)
                         }
                         sum = total();
@@ -535,6 +548,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                 tc_fence_after();
             }
             // the result: the output, or the piece's partial one
+            const float M = R * sc;
             const bool mine = r0 + tid < it.R, cut = a.split && it.part >= 0;
             const float inv = L == 0.f ? 0.f : 1.f / L;
             const size_t out_row = (size_t)it.row + tok_q;
@@ -567,13 +581,6 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
             if (mine && !cut && a.lse) a.lse[out_row * a.heads + head] = L == 0.f ? -INFINITY : (M + log2f(L)) * LN2;
             tc_fence_before();
         }
-        // Where a wait ran out: pieces that this warp did not finish are marked, so that the join leaves their rows alone.
-        for (; !ok && a.split && (x = item_at(k)) < sq.items; ++k) {
-            const Item it = item_of<TILES>(a, sq, x);
-            const int row = it.r0 + t * ROWS + tid, tok_q = row / a.G;
-            if (it.part >= 0 && row < it.R)
-                a.part_ml[2 * (((size_t)it.part + (size_t)it.piece * it.m + tok_q) * a.heads + it.kh * a.G + row - tok_q * a.G)] = __int_as_float(0x7fffffff);
-        }
     }
 
     // ---- teardown
@@ -583,6 +590,7 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag && a.split) mark_unfinished<TILES>(a, sq);
     if (*abort_flag && threadIdx.x == 0) {
         // give copies that were still in flight time to land before shared memory is released
         const unsigned long long t0 = gtimer();

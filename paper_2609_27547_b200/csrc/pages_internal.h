@@ -78,7 +78,7 @@ struct AttendArgs {
     char *out;
     long long q_stride, o_stride;                      // elements
     float *lse;
-    float scale;
+    float scale, up;                                   // up: what moves a score by 8 in units of log 2; the largest number where there is none (a subnormal scale)
     int causal, window;
     int split;                                         // tokens of a piece; 0: not cut
     int team;                                          // warps that share an item

@@ -81,14 +81,17 @@ def test_sums_of_large_values_stay_finite(hd, m):
 
 @pytest.mark.parametrize("hd", [128, 64])
 def test_many_tokens_of_one_weight(hd):
-    """More tokens than the bound of the sums: the reference leaves the largest score behind."""
+    """More tokens than the bound of the sums: the reference leaves the largest score behind.  No reference does so with a subnormal scale: sums are then as large as the
+    number of tokens, 2e5 * 1.5e33 = 3e38 at most."""
     lay = pg.Layout(1, 1, hd, 256, BF)
     n, m = 200_000, 130
     g = torch.Generator().manual_seed(hd)
-    cache = constant(lay, n, torch.zeros(n), 4e33 * (0.5 + 0.5 * torch.rand(n, generator=g)))
+    value = 0.5 + 0.5 * torch.rand(n, generator=g)
     q = torch.ones((m, 1, hd), dtype=BF, device="cuda")
-    out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [n], causal=False, split_tokens=-1)
-    check(cache, 0, q, [m], out, lse, causal=False)
+    for scale, size in ((0.125, 4e33), (1e38, 4e33), (1e-40, 1.5e33)):
+        cache = constant(lay, n, torch.zeros(n), size * value)
+        out, lse = pg.attend(lay, cache.pool, cache.table, q, [m], [n], scale=scale, causal=False, split_tokens=-1)
+        check(cache, 0, q, [m], out, lse, scale=scale, causal=False)
 
 
 @pytest.mark.parametrize("hd,m", [(128, 200), (128, 20), (64, 40), (32, 40)])
