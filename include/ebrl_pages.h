@@ -87,7 +87,7 @@ ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, i
  * ebrl_pages_attend_workspace bytes (of the same arguments) of DEVICE memory, 16-byte aligned, that no other call in flight uses (two captured graphs that
  * may run at once need one each); 0 bytes: workspace may be NULL.
  * bf16: products of bf16 operands, weights rounded to bf16.  fp32: operands and weights in two tf32 terms, three products
- * (21 bits; numbers next to the largest one, from 2^128 (1 - 2^-12) on, are no finite first terms).  Sums and softmax statistics are fp32.  Sums of weights times values
+ * (21 bits, fewer of values below 2^-118; numbers next to the largest one, from 2^128 (1 - 2^-12) on, are no finite first terms).  Sums and softmax statistics are fp32.  Sums of weights times values
  * are divided by the sum of the weights at the end; until then a row's are at most 2^16, or the number of tokens that it sees if that is more, times the largest value,
  * so that values above 2^112 (5e33; 2^128 / tokens if that is less) may overflow. */
 uint64_t ebrl_pages_attend_workspace(const ebrl_pages_layout_t *layout, int32_t n, const int32_t *new_tokens, const int32_t *len, int32_t n_heads,

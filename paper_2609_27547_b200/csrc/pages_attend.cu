@@ -12,7 +12,7 @@
 //   each 96, six with two 78; a team of two, an item each 105: a warp's chain of copies, products and exponentials takes 1.7 us a tile, so that the longest item is
 //   what is waited for).  1 x 256 tokens x 16 heads of 64: 6 us with teams of eight, 11.6 without.
 //   fp32: three tf32 products for each, a k-step's added up by themselves and then in registers (chained through, the tensor core's truncation made the result
-//   2.4e-6 wrong instead of 2.8e-7).  96 x 64 - 512 tokens x 4 heads of 64, 16 - 64 rows: 61 us, of which the products would take 17: eight warps of 255
+//   2.4e-6 wrong instead of 2.8e-7).  96 x 64 - 512 tokens x 4 heads of 64, 16 - 64 rows: 62 us, of which the products would take 17: eight warps of 255
 //   registers per SM issue an instruction every four cycles each, and no more of them fit.
 #include "pages_internal.h"
 #include "ptx_helpers.cuh"
@@ -335,6 +335,8 @@ attend_kernel(const __grid_constant__ AttendArgs a, const __grid_constant__ Atte
                         L[i][e] += sum;
                     }
                 if constexpr (!F32) {
+                    // Weights become bf16, because the values that they meet are (half a step is 2^-8 of a weight; the sum that divides them is not rounded): results are
+                    // 1.8e-3 to 2.0e-3 off, of which their own rounding is 1.7e-3.  Two terms would be half as many products again.
 #pragma unroll
                     for (int k = 0; k < TK / 16; ++k) {
                         uint32_t pa[MT][4];

@@ -17,7 +17,7 @@
 //   row nobody wrote) does not meet a weight of zero.
 //   All waits are bounded: when one runs out the CTA notes it, marks its pieces, lets its copies land, frees tensor memory and returns.
 //
-//   What bounds it: 4 x 2000 - 2048 new tokens over 8 - 16 k x 16 heads of 128 take 750 us, 1.1 PFLOP/s.  The products alone (softmax skipped) take 630: a
+//   What bounds it: 4 x 2000 - 2048 new tokens over 8 - 16 k x 16 heads of 128 take 755 us, 1.1 PFLOP/s.  The products alone (softmax skipped) take 630: a
 //   128 x 128 x 128 product from shared memory reads 128 bytes a cycle, all there are, and the copies want a quarter of that, too.  The rest is
 //   the softmax: its 128 exponentials a row keep the unit busy for 2064 of the 3500 cycles that two tiles take.
 //   Tried and not kept (same case): weights handed over in halves of 64 tokens 757, products of 64 tokens with their own barriers 884, two threads per row
@@ -431,7 +431,9 @@ chunk_kernel(const __grid_constant__ CUtensorMap tm, const __grid_constant__ Att
                         for (int c = 0; c < 32; ++c)
                             if (!((w >> c) & 1)) v[c] = 0xff800000u;
                     };
-                    // The weights of 32 columns, packed, and two times two sums of theirs.
+                    // The weights of 32 columns, packed, and two times two sums of theirs.  They become bf16, because the values that they meet are (half a step is 2^-8 of a
+                    // weight; the sums are not rounded): results are 2.0e-3 to 2.3e-3 off, of which their own rounding is 1.7e-3.  A second term would be half as many
+                    // products again and four more instructions for each pair, which has five.
                     uint64_t sums[2];
                     auto weights = [&](const uint32_t *v, uint32_t *P, uint64_t sc2, uint64_t ref2) {
 #pragma unroll
