@@ -89,7 +89,7 @@ ebrl_status_t ebrl_pages_append(const ebrl_pages_layout_t *layout, void *pool, i
  * bf16: products of bf16 operands, weights rounded to bf16.  fp32: operands and weights in two tf32 terms, three products
  * (21 bits, fewer of values below 2^-118; numbers next to the largest one, from 2^128 (1 - 2^-12) on, are no finite first terms).  Sums and softmax statistics are fp32.  Sums of weights times values
  * are divided by the sum of the weights at the end; until then a row's are at most 2^16, or the number of tokens that it sees if that is more, times the largest value,
- * so that values above 2^112 (5e33; 2^128 / tokens if that is less) may overflow. */
+ * so that values above 2^112 (5e33; 2^128 / tokens if that is less; with many bf16 rows whose scores are 2^26 and more up to 2^32 times less) may overflow. */
 uint64_t ebrl_pages_attend_workspace(const ebrl_pages_layout_t *layout, int32_t n, const int32_t *new_tokens, const int32_t *len, int32_t n_heads,
                                      int32_t causal, int32_t window, int32_t split_tokens, int32_t sm_quota);
 ebrl_status_t ebrl_pages_attend(const ebrl_pages_layout_t *layout, const void *pool, int32_t n_pages, int32_t n, const int32_t *table,
